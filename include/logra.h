@@ -59,6 +59,9 @@ typedef enum { LOGRA_F32 = 0, LOGRA_BF16 = 1, LOGRA_F64 = 2 } logra_dtype;
 #define LOGRA_MAX_GROUP 48       /* layers in one logra_project_layers call */
 #define LOGRA_MAX_PRECOND_D 8192 /* dimension of one preconditioner block */
 #define LOGRA_MAX_TOPK 1024
+#define LOGRA_MAX_ADAPTERS 1023       /* adapters of one plan */
+#define LOGRA_MAX_ADAPTER_RANK 128
+#define LOGRA_MAX_ADAPTER_ROWS 16777216
 
 const char *logra_last_error(void);
 const char *logra_version(void);
@@ -474,6 +477,117 @@ int logra_act_cov_accumulate(const void *a, int a_dtype, int B, int T, int n, co
 size_t logra_pca_ws_size(int n, int k);
 int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype, int64_t ld_p, float *eigvals,
                    void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Trying a choice of training data out.  What an influence score predicts is
+ * checked by training without the data it names (Sec. 4.1, the brittleness
+ * test and the linear datamodeling score: many models, each trained on its own
+ * subset).  The entry points below train and serve low-rank adapters of many
+ * subsets at once beside one frozen model: the rows (tokens) of a batch each
+ * name the adapter they go through.
+ *
+ * logra_adapter_plan groups the rows of a batch by adapter.  A plan depends on
+ *   row_adapter alone: make it once for a batch and use it for every layer, in
+ *   both directions.
+ *   row_adapter  device int32 [rows]: the adapter of each row, in any order; a
+ *                value outside [0, n_adapters) means that the row has none
+ *                (padding, masked tokens, requests to the bare model)
+ *   plan         device memory of logra_adapter_plan_size(rows, n_adapters)
+ *                bytes, 256-byte aligned; read-only afterwards, so streams
+ *                may share it once they are ordered behind this call
+ * rows <= LOGRA_MAX_ADAPTER_ROWS, 1 <= n_adapters <= LOGRA_MAX_ADAPTERS.
+ *
+ * logra_adapter_forward, for every row t with adapter a:
+ *
+ *     u_t = A_a drop(x_t),    y_t = base_t + scale_a B_a^T u_t
+ *
+ *   and y_t = base_t (u_t = 0) for a row without an adapter, whose x is not
+ *   read.  base is the shared projection's output.
+ *   x      [rows] rows of n_in at stride ld_x, dtype F32 or BF16
+ *   A      [n_adapters][rank][n_in], B [n_adapters][rank][n_out], dtype (the
+ *          layout of P_in and P_out; a factor kept as [n_out][rank] is
+ *          transposed once by the caller)
+ *   scale  device fp32 [n_adapters] or NULL (1)
+ *   base   rows of n_out at stride ld_base, or NULL (zeros); may be y itself
+ *          (with ld_base = ld_y): then rows without an adapter are not touched
+ *   y      rows of n_out at stride ld_y, dtype, rounded once from fp32
+ *   u      device fp32 [rows][rank] or NULL: u_t for the backward pass
+ *   drop_p, seed, offset: dropout of x as logra_dropout draws it for x
+ *          (drop_p = 0: none)
+ *
+ * logra_adapter_backward, with du_t = scale_a B_a dy_t:
+ *
+ *     dA_a (+)= sum_t du_t drop(x_t)^T      dB_a (+)= scale_a sum_t u_t dy_t^T
+ *     dx_t = base_t + drop'(A_a^T du_t)     (base_t for a row without an adapter)
+ *
+ *   x, dy, A, B, scale, u, drop_p, seed, offset: as in the forward call; x and dy
+ *   of rows without an adapter are not read.
+ *   dA     device fp32 [n_adapters][rank][n_in], dB fp32 [n_adapters][rank]
+ *          [n_out]; accumulate 0: overwritten (zeros for an adapter without
+ *          rows), 1: added to
+ *   dx     rows of n_in at stride ld_dx, dtype, or NULL (not wanted); base: rows
+ *          of n_in (what the shared projection sends back) or NULL; may be dx
+ * Sums are fp32, in an order that depends on the sizes and the rows' order
+ * alone: reruns are bitwise identical.  The rounding of u and du to matrix
+ * operands leaves 16 significant bits in y and dx, and all 24 in dA and dB.
+ *
+ * ws: logra_adapter_ws_size bytes for either call (contents on entry are
+ * ignored; calls that overlap need their own).  Limits: n_in, n_out multiples of
+ * 8 (bf16) or 4 (fp32), 1 <= rank <= LOGRA_MAX_ADAPTER_RANK.  rows = 0: y, u, dx
+ * have no rows; dA and dB are cleared unless accumulate.  A plan made for other
+ * rows or n_adapters is recognised on the device: nothing is written then.
+ * ---------------------------------------------------------------------- */
+size_t logra_adapter_plan_size(int64_t rows, int n_adapters);
+int logra_adapter_plan(const int32_t *row_adapter, int64_t rows, int n_adapters, void *plan, size_t plan_bytes,
+                       void *stream);
+size_t logra_adapter_ws_size(int64_t rows, int n_in, int n_out, int rank, int n_adapters);
+int logra_adapter_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, int n_in, int n_out, int rank,
+                          int n_adapters, const void *plan, size_t plan_bytes, const void *A, const void *B,
+                          const float *scale, const void *base, int64_t ld_base, void *y, int64_t ld_y, float *u,
+                          double drop_p, uint64_t seed, uint64_t offset, void *ws, size_t ws_bytes, void *stream);
+int logra_adapter_backward(const void *x, int64_t ld_x, const void *dy, int64_t ld_dy, int dtype, int64_t rows,
+                           int n_in, int n_out, int rank, int n_adapters, const void *plan, size_t plan_bytes,
+                           const void *A, const void *B, const float *scale, const float *u, const void *base,
+                           int64_t ld_base, void *dx, int64_t ld_dx, float *dA, float *dB, int accumulate,
+                           double drop_p, uint64_t seed, uint64_t offset, void *ws, size_t ws_bytes, void *stream);
+
+/* logra_dropout: out = residual + drop(x), with
+ *
+ *     drop(x)[t][j] = keep(t, j) ? x[t][j] / (1 - p) : 0
+ *
+ *   The mask is a function of (seed, offset, t, j) and is never stored: bit for
+ *   bit the same in every call, whatever the strides, dtype or residual, so the
+ *   backward pass is this call on the gradient without a residual.  keep(t, j):
+ *   Philox4x32 with 7 rounds (Salmon et al., SC'11) under the key `seed` (low,
+ *   high word) of the counter (j / 8, t, offset low, offset high) gives 4 words;
+ *   element j takes half j % 2 (low first) of word (j % 8) / 2 and is kept iff
+ *   that is >= round(65536 p).  1 - p above is exactly 1 - round(65536 p) / 65536.
+ *   Give every use (layer, step) its own offset.
+ *   x, residual (NULL: none), out: rows of cols elements of dtype F32 or BF16 at
+ *   strides ld_x, ld_res, ld_out; out may be x or residual.  A dropped element's
+ *   value does not matter (NaN included).  0 <= p < 1 with round(65536 p) < 65536.
+ *   Any cols; rows < 2^31; rows = 0 is a no-op. */
+int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols, double p, uint64_t seed,
+                  uint64_t offset, const void *residual, int64_t ld_res, void *out, int64_t ld_out, void *stream);
+
+/* logra_token_loss: cross-entropy of each token's logits and its gradient, the
+ * dy of the model's last layer that the logging and the adapters' backward
+ * start from (a summed loss, App. B.1):
+ *
+ *     loss[t] = w_t (log sum_j exp(z_tj) - z_t,target),  dlogits[t] = w_t (softmax(z_t) - onehot(target_t))
+ *
+ *   logits   rows of vocab elements of dtype F32 or BF16 at stride ld; any vocab
+ *   target   device int64 [rows]; outside [0, vocab): the token is masked, its
+ *            loss and gradient are zero and its logits are not read
+ *   weight   device fp32 [rows] or NULL (1); a weight of 0 masks the token
+ *   loss     device fp32 [rows]
+ *   dlogits  rows of vocab elements of dtype at stride ld_d, or NULL (losses
+ *            only); may be logits (with ld_d = ld)
+ * Logits of -inf (forbidden tokens) have probability zero; a token whose logits
+ * are all -inf has loss +inf and a zero gradient.  rows < 2^31; rows = 0 is a
+ * no-op. */
+int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, int vocab, const int64_t *target,
+                     const float *weight, float *loss, void *dlogits, int64_t ld_d, void *stream);
 
 #ifdef __cplusplus
 }

@@ -22,6 +22,8 @@ __all__ = [
     "logra_cov_accumulate_f64",
     "logra_precondition_ws_size", "logra_precondition", "logra_precondition_blocks", "logra_precondition_f64",
     "logra_influence_ws_size", "logra_influence_scores",
+    "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size", "logra_adapter_forward",
+    "logra_adapter_backward", "logra_dropout", "logra_token_loss",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -46,6 +48,8 @@ EXPORTED = (
     "logra_influence_stream_ws_size", "logra_influence_stream", "logra_offload_rows",
     "logra_store_read_rows", "logra_store_write_rows", "logra_influence_stream_file_ws_size",
     "logra_influence_stream_file", "logra_offload_rows_file",
+    "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size", "logra_adapter_forward",
+    "logra_adapter_backward", "logra_dropout", "logra_token_loss",
 )
 
 
@@ -129,6 +133,21 @@ def lib():
         L.logra_influence_stream_file.argtypes = [vp, i32, i64, i32, i32, i64, i32, i64, i32, i64, i32, vp, vp, vp,
                                                   sz, vp, sz, vp, vp]
         L.logra_offload_rows_file.argtypes = [vp, i64, i64, i64, i32, i64, vp, sz, vp, vp, vp, vp]
+        u64 = ctypes.c_uint64
+        L.logra_adapter_plan_size.argtypes = [i64, i32]
+        L.logra_adapter_plan_size.restype = sz
+        L.logra_adapter_plan.argtypes = [vp, i64, i32, vp, sz, vp]
+        L.logra_adapter_ws_size.argtypes = [i64, i32, i32, i32, i32]
+        L.logra_adapter_ws_size.restype = sz
+        L.logra_adapter_forward.argtypes = [vp, i64, i32, i64, i32, i32, i32, i32, vp, sz, vp, vp, vp, vp, i64, vp, i64,
+                                            vp, f64, u64, u64, vp, sz, vp]
+        L.logra_adapter_backward.argtypes = [vp, i64, vp, i64, i32, i64, i32, i32, i32, i32, vp, sz, vp, vp, vp, vp, vp,
+                                             i64, vp, i64, vp, vp, i32, f64, u64, u64, vp, sz, vp]
+        L.logra_dropout.argtypes = [vp, i64, i32, i64, i32, f64, u64, u64, vp, i64, vp, i64, vp]
+        L.logra_token_loss.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp, vp, i64, vp]
+        for name in ("logra_adapter_plan", "logra_adapter_forward", "logra_adapter_backward", "logra_dropout",
+                     "logra_token_loss"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("logra_store_read_rows", "logra_store_write_rows", "logra_influence_stream_file",
                      "logra_offload_rows_file", "logra_offload_rows", "logra_influence_stream", "logra_pca_topk", "logra_act_cov_accumulate", "logra_act_cov_accumulate_group", "logra_project_layer", "logra_project_layers", "logra_project_layers_noalloc", "logra_cov_accumulate",
                      "logra_cov_accumulate_blocks", "logra_cov_accumulate_blocks_lower", "logra_precondition",
@@ -528,3 +547,127 @@ def logra_offload_rows_file(src, fd: int, file_offset: int, host_buf, io_status=
     st = None if io_status is None else ctypes.byref(io_status)
     _check(lib().logra_offload_rows_file(_ptr(src), ld_src, rows, row_bytes, int(fd), int(file_offset), _ptr(host_buf),
                                          host_buf.numel() * host_buf.element_size(), st, _stream(stream), cs, ev))
+
+
+# ------------------------------------------- adapters, dropout, token loss --
+def logra_adapter_plan_size(rows, n_adapters) -> int:
+    return int(lib().logra_adapter_plan_size(rows, n_adapters))
+
+
+def logra_adapter_plan(row_adapter, n_adapters: int, plan=None, stream=None):
+    """Group the rows of a batch by adapter: row_adapter [rows] int32 (outside [0, n_adapters): no adapter).
+    Returns the plan, a uint8 tensor for logra_adapter_forward and _backward of every layer that the batch
+    goes through (or `plan` itself, filled anew, when given)."""
+    torch = _torch()
+    if row_adapter.dtype != torch.int32 or row_adapter.dim() != 1 or not row_adapter.is_contiguous():
+        raise TypeError("row_adapter must be a contiguous 1-D int32 tensor")
+    rows = row_adapter.shape[0]
+    if plan is None:
+        plan = torch.empty(logra_adapter_plan_size(rows, n_adapters), dtype=torch.uint8, device=row_adapter.device)
+    _check(lib().logra_adapter_plan(row_adapter.data_ptr(), rows, n_adapters, plan.data_ptr(), plan.numel(),
+                                    _stream(stream)))
+    return plan
+
+
+def logra_adapter_ws_size(rows, n_in, n_out, rank, n_adapters) -> int:
+    return int(lib().logra_adapter_ws_size(rows, n_in, n_out, rank, n_adapters))
+
+
+def _matrix(t, rows: int, width: int, dtype, name: str):
+    """(pointer, row stride) of a [rows, width] tensor of dtype whose rows are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.shape != (rows, width) or t.dtype != dtype:
+        raise ValueError(f"{name} must be [{rows}, {width}] of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    ld, step = t.stride()
+    if step != 1 and width > 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), ld if rows > 1 else -(-width // 8) * 8   # (a single row has no stride)
+
+
+def _packed(t, shape, dtype, name: str):
+    """Pointer of a contiguous tensor of exactly this shape and dtype; None for None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {tuple(shape)} of {dtype}")
+    return t.data_ptr()
+
+
+def _adapter_sizes(x, a, b):
+    rows, n_in = x.shape
+    n, rank, width = a.shape
+    if width != n_in or b.shape[:2] != (n, rank):
+        raise ValueError(f"x {tuple(x.shape)}, a {tuple(a.shape)} and b {tuple(b.shape)} do not fit together")
+    return rows, n_in, b.shape[2], rank, n
+
+
+def logra_adapter_forward(x, a, b, plan, y, base=None, scale=None, u=None, p: float = 0.0, seed: int = 0,
+                          offset: int = 0, ws=None, stream=None):
+    """y_t = base_t + scale_a b_a^T (a_a drop(x_t)) for the adapter a of each row, y_t = base_t without one.
+
+    x [rows, n_in], y and base [rows, n_out] (base None: zeros; may be y), a [n, rank, n_in] and
+    b [n, rank, n_out], all of one dtype; scale [n] fp32 or None; u [rows, rank] fp32 or None: a_a drop(x_t),
+    kept for the backward pass.  p, seed, offset: dropout as logra_dropout draws it for x.
+    """
+    torch = _torch()
+    rows, n_in, n_out, rank, n = _adapter_sizes(x, a, b)
+    dt, f32 = x.dtype, torch.float32
+    px, ld_x = _matrix(x, rows, n_in, dt, "x")
+    py, ld_y = _matrix(y, rows, n_out, dt, "y")
+    pb, ld_b = _matrix(base, rows, n_out, dt, "base")
+    if ws is None:
+        ws = torch.empty(logra_adapter_ws_size(rows, n_in, n_out, rank, n), dtype=torch.uint8, device=x.device)
+    _check(lib().logra_adapter_forward(
+        px, ld_x, _dtype_code(x), rows, n_in, n_out, rank, n, plan.data_ptr(), plan.numel(),
+        _packed(a, (n, rank, n_in), dt, "a"), _packed(b, (n, rank, n_out), dt, "b"), _packed(scale, (n,), f32, "scale"),
+        pb, ld_b, py, ld_y, _packed(u, (rows, rank), f32, "u"), p, seed, offset, ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def logra_adapter_backward(x, dy, a, b, plan, u, da, db, dx=None, base=None, scale=None, p: float = 0.0,
+                           seed: int = 0, offset: int = 0, accumulate: bool = False, ws=None, stream=None):
+    """Gradients of logra_adapter_forward: da [n, rank, n_in] and db [n, rank, n_out] fp32 (overwritten, or
+    added to with accumulate) and, unless dx is None, dx [rows, n_in] = base (None: zeros; may be dx) + what the
+    adapter of each row sends back.  u, scale, p, seed, offset: as in the forward call; dy [rows, n_out].
+    """
+    torch = _torch()
+    rows, n_in, n_out, rank, n = _adapter_sizes(x, a, b)
+    dt, f32 = x.dtype, torch.float32
+    px, ld_x = _matrix(x, rows, n_in, dt, "x")
+    pdy, ld_dy = _matrix(dy, rows, n_out, dt, "dy")
+    pdx, ld_dx = _matrix(dx, rows, n_in, dt, "dx")
+    pb, ld_b = _matrix(base, rows, n_in, dt, "base")
+    if ws is None:
+        ws = torch.empty(logra_adapter_ws_size(rows, n_in, n_out, rank, n), dtype=torch.uint8, device=x.device)
+    _check(lib().logra_adapter_backward(
+        px, ld_x, pdy, ld_dy, _dtype_code(x), rows, n_in, n_out, rank, n, plan.data_ptr(), plan.numel(),
+        _packed(a, (n, rank, n_in), dt, "a"), _packed(b, (n, rank, n_out), dt, "b"), _packed(scale, (n,), f32, "scale"),
+        _packed(u, (rows, rank), f32, "u"), pb, ld_b, pdx, ld_dx, _packed(da, (n, rank, n_in), f32, "da"),
+        _packed(db, (n, rank, n_out), f32, "db"), int(accumulate), p, seed, offset, ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def logra_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, stream=None):
+    """out = residual + drop(x) for x, residual (None: zeros) and out [rows, cols] of one dtype; the mask is a
+    function of (seed, offset, row, column) alone, so the backward pass is logra_dropout on the gradient."""
+    rows, cols = x.shape
+    px, ld_x = _matrix(x, rows, cols, x.dtype, "x")
+    po, ld_o = _matrix(out, rows, cols, x.dtype, "out")
+    pr, ld_r = _matrix(residual, rows, cols, x.dtype, "residual")
+    _check(lib().logra_dropout(px, ld_x, _dtype_code(x), rows, cols, p, seed, offset, pr, ld_r, po, ld_o,
+                               _stream(stream)))
+
+
+def logra_token_loss(logits, target, loss, dlogits=None, weight=None, stream=None):
+    """loss [rows] fp32 = weight (logsumexp(logits) - logits[target]) and, unless None, dlogits = its gradient,
+    for logits [rows, vocab] and target [rows] int64 (outside the vocabulary: masked, zeros); dlogits may be
+    logits."""
+    torch = _torch()
+    rows, vocab = logits.shape
+    pz, ld = _matrix(logits, rows, vocab, logits.dtype, "logits")
+    pd, ld_d = _matrix(dlogits, rows, vocab, logits.dtype, "dlogits")
+    _check(lib().logra_token_loss(pz, ld, _dtype_code(logits), rows, vocab,
+                                  _packed(target, (rows,), torch.int64, "target"),
+                                  _packed(weight, (rows,), torch.float32, "weight"),
+                                  _packed(loss, (rows,), torch.float32, "loss"), pd, ld_d, _stream(stream)))

@@ -3,6 +3,7 @@
 // HIP call; pointer checks follow (hipPointerGetAttributes); then launches.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -752,6 +753,198 @@ int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype
     hipError_t e = logra::launch_pca_topk(C, n, k, iters, P, P_dtype == LOGRA_BF16, ld_p, eigvals, ws,
                                           static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "pca launch");
+    return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------- adapters, dropout, token loss --
+namespace {
+
+// Sizes and strides of `rows` rows of `width` elements (checked before any HIP call).
+int check_stride(const char *name, int64_t ld, int width, int dtype) {
+    if (ld < width) return fail(LOGRA_ERR_INVALID_ARG, "the row stride of %s must be >= %d", name, width);
+    if (static_cast<uint64_t>(ld) * esize(dtype) % 16)
+        return fail(LOGRA_ERR_INVALID_ARG, "the row stride of %s must be a multiple of 16 bytes", name);
+    if (ld > (int64_t{1} << 40)) return fail(LOGRA_ERR_INVALID_ARG, "the row stride of %s exceeds device memory", name);
+    return LOGRA_OK;
+}
+
+// Device memory at the first and at the last element of the rows, so that a
+// wrong row stride is reported instead of faulting the kernel.
+int check_matrix(const void *p, const char *name, int64_t rows, int64_t ld, int width, int dtype) {
+    TRY(check_dev(p, name, 16));
+    if (rows <= 1) return LOGRA_OK;
+    const double span = (static_cast<double>(rows - 1) * static_cast<double>(ld) + width) * static_cast<double>(esize(dtype));
+    if (span > 281474976710656.0)   // 2^48 bytes: beyond any device allocation
+        return fail(LOGRA_ERR_INVALID_ARG, "the rows of %s exceed device memory", name);
+    return check_dev(static_cast<const char *>(p) + ((rows - 1) * ld + width - 1) * static_cast<int64_t>(esize(dtype)),
+                     name, 1);
+}
+
+int check_drop(double p) {
+    if (!(p >= 0.0 && p < 1.0) || std::nearbyint(p * 65536.0) >= 65536.0)
+        return fail(LOGRA_ERR_INVALID_ARG, "the drop probability must be in [0, 1 - 1/65536]");
+    return LOGRA_OK;
+}
+
+int check_adapter_group(int64_t rows, int n_adapters) {
+    if (rows < 0) return fail(LOGRA_ERR_INVALID_ARG, "rows must be >= 0");
+    if (n_adapters <= 0) return fail(LOGRA_ERR_INVALID_ARG, "n_adapters must be > 0");
+    if (n_adapters > LOGRA_MAX_ADAPTERS) return fail(LOGRA_ERR_UNSUPPORTED, "n_adapters must be <= %d", LOGRA_MAX_ADAPTERS);
+    if (rows > LOGRA_MAX_ADAPTER_ROWS) return fail(LOGRA_ERR_UNSUPPORTED, "rows must be <= %d", LOGRA_MAX_ADAPTER_ROWS);
+    return LOGRA_OK;
+}
+
+// Everything of an adapter call that needs no HIP call.
+int check_adapter_sizes(int dtype, int64_t rows, int n_in, int n_out, int rank, int n_adapters, double drop_p) {
+    if (!valid_dtype(dtype)) return fail(LOGRA_ERR_INVALID_ARG, "bad dtype");
+    TRY(check_adapter_group(rows, n_adapters));
+    if (n_in <= 0 || n_out <= 0 || rank <= 0) return fail(LOGRA_ERR_INVALID_ARG, "n_in, n_out, rank must be > 0");
+    const int vec = dtype == LOGRA_BF16 ? 8 : 4;
+    if (n_in % vec || n_out % vec) return fail(LOGRA_ERR_INVALID_ARG, "n_in and n_out must be multiples of %d", vec);
+    if (n_in > (1 << 20) || n_out > (1 << 20)) return fail(LOGRA_ERR_UNSUPPORTED, "n_in and n_out must be <= 1048576");
+    if (rank > LOGRA_MAX_ADAPTER_RANK) return fail(LOGRA_ERR_UNSUPPORTED, "rank must be <= %d", LOGRA_MAX_ADAPTER_RANK);
+    return check_drop(drop_p);
+}
+
+int check_plan(const void *plan, size_t plan_bytes, int64_t rows, int n_adapters) {
+    const size_t need = logra_adapter_plan_size(rows, n_adapters);
+    if (plan == nullptr || plan_bytes < need)
+        return fail(LOGRA_ERR_WORKSPACE, "the plan needs %zu bytes, got %zu", need, plan ? plan_bytes : 0);
+    return check_dev(plan, "plan", 256);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t logra_adapter_plan_size(int64_t rows, int n_adapters) {
+    if (rows <= 0 || n_adapters <= 0 || n_adapters > LOGRA_MAX_ADAPTERS || rows > LOGRA_MAX_ADAPTER_ROWS) return 0;
+    return round256(logra::adapter_plan_bytes(rows, n_adapters));
+}
+
+int logra_adapter_plan(const int32_t *row_adapter, int64_t rows, int n_adapters, void *plan, size_t plan_bytes,
+                       void *stream) {
+    TRY(check_adapter_group(rows, n_adapters));
+    if (rows == 0) return ok();
+    TRY(check_dev(row_adapter, "row_adapter", 4));
+    TRY(check_plan(plan, plan_bytes, rows, n_adapters));
+    const hipError_t e = logra::launch_adapter_plan(row_adapter, rows, n_adapters, plan, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "adapter plan launch");
+    return ok();
+}
+
+size_t logra_adapter_ws_size(int64_t rows, int n_in, int n_out, int rank, int n_adapters) {
+    if (rows <= 0 || n_in <= 0 || n_out <= 0 || rank <= 0 || n_adapters <= 0 || rows > LOGRA_MAX_ADAPTER_ROWS ||
+        rank > LOGRA_MAX_ADAPTER_RANK || n_adapters > LOGRA_MAX_ADAPTERS || n_in > (1 << 20) || n_out > (1 << 20))
+        return 0;
+    return round256(logra::adapter_ws_bytes(rows, n_in, n_out, rank, n_adapters));
+}
+
+int logra_adapter_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, int n_in, int n_out, int rank,
+                          int n_adapters, const void *plan, size_t plan_bytes, const void *A, const void *B,
+                          const float *scale, const void *base, int64_t ld_base, void *y, int64_t ld_y, float *u,
+                          double drop_p, uint64_t seed, uint64_t offset, void *ws, size_t ws_bytes, void *stream) {
+    TRY(check_adapter_sizes(dtype, rows, n_in, n_out, rank, n_adapters, drop_p));
+    if (rows == 0) return ok();
+    TRY(check_stride("x", ld_x, n_in, dtype));
+    TRY(check_stride("y", ld_y, n_out, dtype));
+    if (base) TRY(check_stride("base", ld_base, n_out, dtype));
+    if (base == y && ld_base != ld_y) return fail(LOGRA_ERR_INVALID_ARG, "base in place of y needs y's row stride");
+    TRY(check_matrix(x, "x", rows, ld_x, n_in, dtype));
+    TRY(check_dev(A, "A", 16));
+    TRY(check_dev(B, "B", 16));
+    if (scale) TRY(check_dev(scale, "scale", 4));
+    if (base) TRY(check_matrix(base, "base", rows, ld_base, n_out, dtype));
+    TRY(check_matrix(y, "y", rows, ld_y, n_out, dtype));
+    if (u) TRY(check_dev(u, "u", 4));
+    TRY(check_plan(plan, plan_bytes, rows, n_adapters));
+    TRY(check_ws(ws, ws_bytes, logra_adapter_ws_size(rows, n_in, n_out, rank, n_adapters)));
+    const logra::AdapterDims dims = {rows, n_in, n_out, rank, n_adapters};
+    const hipError_t e = logra::launch_adapter_forward(dims, dtype == LOGRA_BF16, plan, x, ld_x, A, B, scale, base, ld_base,
+                                                       y, ld_y, u, drop_p, seed, offset, ws,
+                                                       static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "adapter forward launch");
+    return ok();
+}
+
+int logra_adapter_backward(const void *x, int64_t ld_x, const void *dy, int64_t ld_dy, int dtype, int64_t rows,
+                           int n_in, int n_out, int rank, int n_adapters, const void *plan, size_t plan_bytes,
+                           const void *A, const void *B, const float *scale, const float *u, const void *base,
+                           int64_t ld_base, void *dx, int64_t ld_dx, float *dA, float *dB, int accumulate,
+                           double drop_p, uint64_t seed, uint64_t offset, void *ws, size_t ws_bytes, void *stream) {
+    TRY(check_adapter_sizes(dtype, rows, n_in, n_out, rank, n_adapters, drop_p));
+    if (base && !dx) return fail(LOGRA_ERR_INVALID_ARG, "base without dx");
+    if (rows > 0) {
+        TRY(check_stride("x", ld_x, n_in, dtype));
+        TRY(check_stride("dy", ld_dy, n_out, dtype));
+        if (dx) TRY(check_stride("dx", ld_dx, n_in, dtype));
+        if (base) TRY(check_stride("base", ld_base, n_in, dtype));
+        if (base && base == dx && ld_base != ld_dx)
+            return fail(LOGRA_ERR_INVALID_ARG, "base in place of dx needs dx's row stride");
+    }
+    TRY(check_dev(dA, "dA", 16));
+    TRY(check_dev(dB, "dB", 16));
+    if (rows > 0) {
+        TRY(check_matrix(x, "x", rows, ld_x, n_in, dtype));
+        TRY(check_matrix(dy, "dy", rows, ld_dy, n_out, dtype));
+        TRY(check_dev(A, "A", 16));
+        TRY(check_dev(B, "B", 16));
+        TRY(check_dev(u, "u", 4));
+        if (scale) TRY(check_dev(scale, "scale", 4));
+        if (dx) TRY(check_matrix(dx, "dx", rows, ld_dx, n_in, dtype));
+        if (base) TRY(check_matrix(base, "base", rows, ld_base, n_in, dtype));
+        TRY(check_plan(plan, plan_bytes, rows, n_adapters));
+        TRY(check_ws(ws, ws_bytes, logra_adapter_ws_size(rows, n_in, n_out, rank, n_adapters)));
+    }
+    const logra::AdapterDims dims = {rows, n_in, n_out, rank, n_adapters};
+    const hipError_t e = logra::launch_adapter_backward(dims, dtype == LOGRA_BF16, plan, x, ld_x, dy, ld_dy, A, B, scale, u,
+                                                        base, ld_base, dx, ld_dx, dA, dB, accumulate != 0, drop_p, seed,
+                                                        offset, ws, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "adapter backward launch");
+    return ok();
+}
+
+int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols, double p, uint64_t seed,
+                  uint64_t offset, const void *residual, int64_t ld_res, void *out, int64_t ld_out, void *stream) {
+    if (!valid_dtype(dtype)) return fail(LOGRA_ERR_INVALID_ARG, "bad dtype");
+    if (rows < 0 || cols <= 0) return fail(LOGRA_ERR_INVALID_ARG, "need rows >= 0 and cols > 0");
+    if (rows > INT32_MAX) return fail(LOGRA_ERR_UNSUPPORTED, "rows must be < 2^31");
+    TRY(check_drop(p));
+    if (rows == 0) return ok();
+    TRY(check_stride("x", ld_x, cols, dtype));
+    TRY(check_stride("out", ld_out, cols, dtype));
+    if (residual) TRY(check_stride("residual", ld_res, cols, dtype));
+    if ((x == out && ld_x != ld_out) || (residual == out && residual && ld_res != ld_out))
+        return fail(LOGRA_ERR_INVALID_ARG, "an input in place of out needs out's row stride");
+    TRY(check_matrix(x, "x", rows, ld_x, cols, dtype));
+    if (residual) TRY(check_matrix(residual, "residual", rows, ld_res, cols, dtype));
+    TRY(check_matrix(out, "out", rows, ld_out, cols, dtype));
+    const hipError_t e = logra::launch_dropout(x, ld_x, dtype == LOGRA_BF16, rows, cols, residual, ld_res, out, ld_out, p,
+                                               seed, offset, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "dropout launch");
+    return ok();
+}
+
+int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, int vocab, const int64_t *target,
+                     const float *weight, float *loss, void *dlogits, int64_t ld_d, void *stream) {
+    if (!valid_dtype(dtype)) return fail(LOGRA_ERR_INVALID_ARG, "bad dtype");
+    if (rows < 0 || vocab <= 0) return fail(LOGRA_ERR_INVALID_ARG, "need rows >= 0 and vocab > 0");
+    if (rows > INT32_MAX) return fail(LOGRA_ERR_UNSUPPORTED, "rows must be < 2^31");
+    if (vocab > (1 << 30)) return fail(LOGRA_ERR_UNSUPPORTED, "vocab must be <= 2^30");
+    if (rows == 0) return ok();
+    TRY(check_stride("logits", ld, vocab, dtype));
+    if (dlogits) TRY(check_stride("dlogits", ld_d, vocab, dtype));
+    if (dlogits == logits && ld_d != ld) return fail(LOGRA_ERR_INVALID_ARG, "dlogits in place of logits needs their row stride");
+    TRY(check_matrix(logits, "logits", rows, ld, vocab, dtype));
+    TRY(check_dev(target, "target", 8));
+    if (weight) TRY(check_dev(weight, "weight", 4));
+    TRY(check_dev(loss, "loss", 4));
+    if (dlogits) TRY(check_matrix(dlogits, "dlogits", rows, ld_d, vocab, dtype));
+    const hipError_t e = logra::launch_token_loss(logits, ld, dtype == LOGRA_BF16, rows, vocab, target, weight, loss,
+                                                  dlogits, ld_d, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "token loss launch");
     return ok();
 }
 

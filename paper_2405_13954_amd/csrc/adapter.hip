@@ -1,0 +1,1008 @@
+// Low-rank adapters of many requests at once, beside a shared projection:
+//
+//     u_t = A_a drop(x_t)                  y_t  = base_t + s_a B_a^T u_t
+//     du_t = s_a B_a dy_t                  dx_t = base_t + drop'(A_a^T du_t)
+//     dA_a = sum_t du_t drop(x_t)^T        dB_a = s_a sum_t u_t dy_t^T
+//
+// for rows t of x whose adapter is a (a row without one: y = base, dx = base),
+// A [n][rank][n_in] and B [n][rank][n_out], both with the long index
+// contiguous as the projections P_in and P_out of this library are.  So the
+// forward and the backward pass are made of the same three products:
+//
+//   k_shrink   U[t][r]  = sum_j W_a[r][j] v_t[j]            (x with A, dy with B)
+//   k_expand   out_t[j] = base_t[j] + sum_r U[t][r] W_a[r][j]   (B, then A)
+//   k_grad     dW_a[r][j] = sum_t U[t][r] v_t[j]            (dy with u, x with du)
+//
+// All are bound by memory (2 rank multiply-adds for each element of x or y):
+// the design keeps every element of x, dy, base, y read or written once by
+// each product, and the weights in L2.
+//
+//  0. k_plan_*: groups the rows of a batch by adapter, stably (so that sums run
+//     in row order, and reruns give the same bits).  Each group starts at a
+//     multiple of 32 in the order, and lists of its tiles of 16, 32, .. 512 rows
+//     let a workgroup find its rows with one load.  Kernels that get memory which
+//     is no plan for their sizes do nothing.
+//  1. k_shrink: a workgroup owns a tile of 16 M rows and a range of the long
+//     axis, its four waves taking 128-byte pieces of it in turn; the waves' sums
+//     are added through LDS.  Few rows: the axis is split over workgroups, whose
+//     partial sums the next kernel adds in order.
+//  2. k_expand: a workgroup owns 16 M rows and a slice of columns; W's slice is
+//     put in LDS once, U comes as MFMA operands straight from memory.  A bf16 W
+//     takes U as two bf16 halves (about 16 significant bits, so that U's rounding
+//     stays far below that of the output); rank 16 then fills the 32-deep
+//     contraction of one MFMA exactly.  fp32 uses fp32 MFMAs.
+//  3. k_prep (backward): sums the partial du, applies s_a, and for bf16 lays u and
+//     du out by rank as three bf16 thirds (24 significant bits: the gradients are
+//     fp32, so nothing of u and du may be lost), the operands of k_grad.
+//  4. k_grad: a workgroup owns a chunk of an adapter's rows and 256 columns; 32
+//     rows at a time go through LDS, where transposed reads (bf16:
+//     ds_read_b64_tr_b16) turn them into operands whose contraction runs over
+//     rows.  k_reduce adds the chunks' sums in order.
+#include "counter_rng.h"
+#include "internal.h"
+
+namespace logra {
+namespace {
+
+constexpr int kHeights = 6;          // tile lists of 16 << h rows
+constexpr int kSeg = 4096;           // rows of one workgroup of the plan's kernels
+constexpr int kPlanMagic = 0x4c6f4164;
+constexpr int kPad = 32;             // groups start at multiples of this
+
+struct PlanHead {
+    int magic, rows, n;
+    int tiles_used[kHeights];        // tiles of the adapters
+    int tiles_all[kHeights];         // and of the rows without one, which come last
+};
+struct Tile {
+    int group, p0, count, index;     // adapter, first place in the order, rows, number within the group
+};
+
+// The plan's memory: head, row of each place (-1: a pad), tile lists, each
+// group's first tile in them, and the segments' counts while it is made.
+struct PlanView {
+    PlanHead *head;
+    int *row_of;
+    Tile *tiles[kHeights];
+    int *first[kHeights];
+    int *start;                      // first place of each group, [n + 2]
+    int *hist;
+    int rows, n;
+};
+
+struct PlanLayout {
+    size_t row_of, tiles[kHeights], first[kHeights], start, hist, bytes;
+};
+
+inline int64_t plan_places(int64_t rows, int n) {
+    const int64_t groups = n + 1 < rows ? n + 1 : rows;
+    return (rows + (kPad - 1) * groups + kPad - 1) / kPad * kPad;
+}
+inline int64_t plan_max_tiles(int64_t rows, int n, int h) {
+    return (rows >> (4 + h)) + (n + 1 < rows ? n + 1 : rows);
+}
+
+PlanLayout plan_layout(int64_t rows, int n) {
+    PlanLayout l;
+    size_t at = align256(sizeof(PlanHead));
+    const auto take = [&](size_t b) {
+        const size_t here = at;
+        at += align256(b);
+        return here;
+    };
+    l.row_of = take(static_cast<size_t>(plan_places(rows, n)) * 4);
+    for (int h = 0; h < kHeights; ++h) l.tiles[h] = take(static_cast<size_t>(plan_max_tiles(rows, n, h)) * sizeof(Tile));
+    for (int h = 0; h < kHeights; ++h) l.first[h] = take(static_cast<size_t>(n + 2) * 4);
+    l.start = take(static_cast<size_t>(n + 2) * 4);
+    l.hist = take(static_cast<size_t>((rows + kSeg - 1) / kSeg) * (n + 1) * 4);
+    l.bytes = at;
+    return l;
+}
+
+PlanView plan_view(void *plan, int64_t rows, int n) {
+    const PlanLayout l = plan_layout(rows, n);
+    char *p = static_cast<char *>(plan);
+    PlanView v;
+    v.head = reinterpret_cast<PlanHead *>(p);
+    v.row_of = reinterpret_cast<int *>(p + l.row_of);
+    for (int h = 0; h < kHeights; ++h) {
+        v.tiles[h] = reinterpret_cast<Tile *>(p + l.tiles[h]);
+        v.first[h] = reinterpret_cast<int *>(p + l.first[h]);
+    }
+    v.start = reinterpret_cast<int *>(p + l.start);
+    v.hist = reinterpret_cast<int *>(p + l.hist);
+    v.rows = static_cast<int>(rows);
+    v.n = n;
+    return v;
+}
+
+// What a kernel needs of a plan: one tile list.
+struct TileList {
+    const PlanHead *head;
+    const Tile *tiles;
+    const int *row_of;
+    int rows, n, h;
+};
+TileList tile_list(const PlanView &v, int h) { return {v.head, v.tiles[h], v.row_of, v.rows, v.n, h}; }
+
+__device__ __forceinline__ bool is_plan(const PlanHead *h, int rows, int n) {
+    return h->magic == kPlanMagic && h->rows == rows && h->n == n;
+}
+__device__ __forceinline__ int tile_count(const TileList &l, bool all) {
+    if (!is_plan(l.head, l.rows, l.n)) return 0;
+    return all ? l.head->tiles_all[l.h] : l.head->tiles_used[l.h];
+}
+
+// ------------------------------------------------------------------- plan --
+__device__ __forceinline__ int group_of(const int *row_adapter, int row, int n) {
+    const int a = row_adapter[row];
+    return a >= 0 && a < n ? a : n;
+}
+
+__global__ __launch_bounds__(256) void k_plan_hist(const int *row_adapter, PlanView v) {
+    __shared__ int cnt[1024];
+    for (int g = threadIdx.x; g <= v.n; g += 256) cnt[g] = 0;
+    __syncthreads();
+    const int at = blockIdx.x * kSeg, end = v.rows - at < kSeg ? v.rows : at + kSeg;
+    for (int i = at + threadIdx.x; i < end; i += 256) atomicAdd(&cnt[group_of(row_adapter, i, v.n)], 1);
+    __syncthreads();
+    for (int g = threadIdx.x; g <= v.n; g += 256) v.hist[static_cast<int64_t>(blockIdx.x) * (v.n + 1) + g] = cnt[g];
+}
+
+// Exclusive sum over the workgroup's 1024 threads; `total` gets the whole sum.
+__device__ __forceinline__ int scan1024(int x, int *red, int *total) {
+    int v = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(v, d);
+        if ((threadIdx.x & 63) >= static_cast<unsigned>(d)) v += o;
+    }
+    if ((threadIdx.x & 63) == 63) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < 16; ++w) {
+        if (w < static_cast<int>(threadIdx.x >> 6)) before += red[w];
+        all += red[w];
+    }
+    __syncthreads();
+    *total = all;
+    return before + v - x;
+}
+
+// One thread per group: starts, tile lists, and the segments' counts turned
+// into the segments' first places within the group.
+__global__ __launch_bounds__(1024) void k_plan_scan(PlanView v, int segs) {
+    __shared__ int red[16], lds_first[1025], lds_start[1024], lds_count[1024];
+    const int g = threadIdx.x, groups = v.n + 1;
+    int count = 0;
+    if (g < groups)
+        for (int s = 0; s < segs; ++s) {
+            int *p = &v.hist[static_cast<int64_t>(s) * groups + g];
+            const int c = *p;
+            *p = count;
+            count += c;
+        }
+    int total;
+    const int start = scan1024((count + kPad - 1) / kPad * kPad, red, &total);
+    lds_start[g] = start;
+    lds_count[g] = count;
+    if (g < groups) {
+        v.start[g] = start;
+        for (int i = start + count; i < start + (count + kPad - 1) / kPad * kPad; ++i) v.row_of[i] = -1;
+    }
+    if (g == 0) {
+        v.start[groups] = total;
+        v.head->magic = kPlanMagic;
+        v.head->rows = v.rows;
+        v.head->n = v.n;
+    }
+    for (int h = 0; h < kHeights; ++h) {
+        const int height = 16 << h;
+        const int first = scan1024((count + height - 1) / height, red, &total);
+        lds_first[g] = first;
+        if (g < groups) v.first[h][g] = first;
+        if (g == v.n) v.head->tiles_used[h] = first;
+        if (g == 0) {
+            lds_first[1024] = total;
+            v.first[h][groups] = total;
+            v.head->tiles_all[h] = total;
+        }
+        __syncthreads();
+        for (int t = g; t < total; t += 1024) {
+            int lo = 0, hi = groups;   // the last group whose first tile is at or before t
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (lds_first[mid] <= t)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            const int i = t - lds_first[lo], left = lds_count[lo] - i * height;
+            v.tiles[h][t] = {lo, lds_start[lo] + i * height, left < height ? left : height, i};
+        }
+        __syncthreads();
+    }
+}
+
+// Places of the rows: each of the four waves takes 1024 consecutive rows, 64 at
+// a time; lanes of one group are ranked by their lane numbers, so a group's rows
+// keep their order.
+__global__ __launch_bounds__(256) void k_plan_scatter(const int *row_adapter, PlanView v) {
+    __shared__ int next[4][1024];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, groups = v.n + 1;
+    for (int i = threadIdx.x; i < 4 * 1024; i += 256) next[i >> 10][i & 1023] = 0;
+    __syncthreads();
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kSeg + wave * (kSeg / 4);
+    for (int i = 0; i < kSeg / 4; i += 64)
+        if (at + i + lane < v.rows) atomicAdd(&next[wave][group_of(row_adapter, static_cast<int>(at + i + lane), v.n)], 1);
+    __syncthreads();
+    for (int g = threadIdx.x; g < groups; g += 256) {
+        int p = v.start[g] + v.hist[static_cast<int64_t>(blockIdx.x) * groups + g];
+        for (int w = 0; w < 4; ++w) {
+            const int c = next[w][g];
+            next[w][g] = p;
+            p += c;
+        }
+    }
+    __syncthreads();
+    for (int i = 0; i < kSeg / 4; i += 64) {
+        const int64_t row = at + i + lane;
+        const bool live = row < v.rows;
+        const int g = live ? group_of(row_adapter, static_cast<int>(row), v.n) : -1;
+        uint64_t left = __ballot(live);
+        while (left) {   // one group of these 64 rows at a time
+            const int gl = __shfl(g, __ffsll(static_cast<unsigned long long>(left)) - 1);
+            const uint64_t same = __ballot(g == gl);
+            volatile int *slot = &next[wave][gl];
+            const int p = *slot;
+            __builtin_amdgcn_wave_barrier();
+            if (g == gl) v.row_of[p + __popcll(same & ((uint64_t{1} << lane) - 1))] = static_cast<int>(row);
+            if (lane == 0) *slot = p + __popcll(same);
+            __builtin_amdgcn_wave_barrier();
+            left &= ~same;
+        }
+    }
+}
+
+// ----------------------------------------------------------------- shrink --
+template <bool BF16>
+constexpr int kEs = BF16 ? 2 : 4;
+template <bool BF16>
+constexpr int kVec = BF16 ? 8 : 4;        // elements in 16 bytes
+
+// One 16-byte piece of both operands: contraction elements 8 (l / 16) .. + 7
+// (bf16) or 4 (l / 16) .. + 3 (fp32, one MFMA for each).
+template <bool BF16>
+__device__ __forceinline__ f32x4 mfma_piece(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (BF16) return mfma16_bf16(as_bf16x8(a), as_bf16x8(b), c);
+    const f32x4 fa = as_f32x4(a), fb = as_f32x4(b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = mfma16_f32(fa[e], fb[e], c);
+    return c;
+}
+
+template <bool BF16>
+__device__ __forceinline__ u32x4 drop_piece(const DropArgs &d, u32x4 v, uint32_t row, int col) {
+    if constexpr (BF16) return drop8_bf16(d, v, row, static_cast<uint32_t>(col) >> 3);
+    return drop4_f32(d, v, row, static_cast<uint32_t>(col));
+}
+
+// part[split][place][16 RT] = sum over the split's range of W_a[r][j] drop(v_t[j]) f
+template <bool BF16, int M, int RT, bool DROP>
+__global__ __launch_bounds__(256) void k_shrink(TileList list, const char *v, int64_t ld, int width, const char *W,
+                                                int rank, float *part, int64_t places, int per_split, DropArgs d) {
+    constexpr int kRp = 16 * RT, kUnit = 8 * kVec<BF16>;   // 128 bytes of a row
+    __shared__ float red[4][16 * M][kRp];
+    if (static_cast<int>(blockIdx.x) >= tile_count(list, false)) return;
+    const Tile tile = list.tiles[blockIdx.x];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
+    const int begin = blockIdx.y * per_split;
+    const int end = width - begin < per_split ? width : begin + per_split;
+
+    int row[M];
+    const char *vp[M];
+    const char *wp[RT];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        const int i = 16 * m + t;
+        row[m] = list.row_of[tile.p0 + (i < tile.count ? i : 0)];
+        vp[m] = v + row[m] * ld * kEs<BF16> + 16 * g;
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int i = 16 * r + t;
+        wp[r] = W + (static_cast<int64_t>(tile.group) * rank + (i < rank ? i : rank - 1)) * width * kEs<BF16> + 16 * g;
+    }
+    f32x4 acc[M][RT];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[m][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    struct Piece {
+        u32x4 x[2][M], w[2][RT];
+    };
+    // the 128-byte piece at column j; `whole`: it ends inside the row
+    const auto load = [&](Piece &p, int j, bool whole) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t off = static_cast<int64_t>(j) * kEs<BF16> + 64 * h;
+            const bool in = whole || j + (4 * h + g) * kVec<BF16> < end;
+#pragma unroll
+            for (int m = 0; m < M; ++m) p.x[h][m] = in ? ld128(vp[m] + off) : u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < RT; ++r) p.w[h][r] = in ? ld128(wp[r] + off) : u32x4{0, 0, 0, 0};
+        }
+    };
+    const auto multiply = [&](Piece &p, int j) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (DROP) {
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+                    p.x[h][m] = drop_piece<BF16>(d, p.x[h][m], static_cast<uint32_t>(row[m]), j + (4 * h + g) * kVec<BF16>);
+            }
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[m][r] = mfma_piece<BF16>(p.w[h][r], p.x[h][m], acc[m][r]);
+        }
+    };
+    int j = begin + wave * kUnit;
+    if (j + kUnit <= end) {
+        Piece now;
+        load(now, j, true);
+        for (; j + 5 * kUnit <= end; j += 4 * kUnit) {   // the next piece is on its way while this one is multiplied
+            Piece next;
+            load(next, j + 4 * kUnit, true);
+            multiply(now, j);
+            now = next;
+        }
+        multiply(now, j);
+        j += 4 * kUnit;
+    }
+    if (j < end) {
+        Piece last;
+        load(last, j, false);
+        multiply(last, j);
+    }
+
+    // lane holds ranks 16 r + 4 g .. + 3 of row 16 m + t
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4 *>(&red[wave][16 * m + t][16 * r + 4 * g]) = acc[m][r];
+    __syncthreads();
+    const float f = DROP ? d.scale : 1.f;
+    float *out = part + (static_cast<int64_t>(blockIdx.y) * places + tile.p0) * kRp;
+    for (int i = threadIdx.x; i < 16 * M * kRp / 4; i += 256) {
+        const int slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
+        if (slot >= tile.count) break;
+        f32x4 s = *reinterpret_cast<f32x4 *>(&red[0][slot][r]);
+#pragma unroll
+        for (int w = 1; w < 4; ++w) s += *reinterpret_cast<f32x4 *>(&red[w][slot][r]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = r + e < rank ? s[e] * f : 0.f;
+        *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(slot) * kRp + r) = s;
+    }
+}
+
+// ----------------------------------------------------------------- expand --
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+// What rounding f to bf16 leaves over (0 beside an infinity or a NaN, which the
+// rounded part carries alone).
+__device__ __forceinline__ float left_over(float f) {
+    const float h = static_cast<float>(static_cast<__bf16>(f));
+    return __builtin_isfinite(h) ? f - h : 0.f;
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ __forceinline__ s16x4 read_tr(uint32_t at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at);
+}
+
+// Columns of one wave in k_expand: as many as keep W's slice within 40 KB of LDS.
+template <bool BF16, int RT>
+constexpr int kCols = BF16 ? (RT <= 4 ? 64 : 32) : (RT <= 2 ? 64 : RT <= 4 ? 32 : 16);
+
+struct ExpandArgs {
+    const float *part;        // [splits][places][16 RT]
+    int splits;
+    int64_t places;
+    const float *scale;       // [n] or null
+    const char *W;
+    int rank, width;
+    const char *base;
+    int64_t ld_b;
+    char *out;
+    int64_t ld_o;
+    float *u_out;             // [rows][rank] or null: the sum of the partials, unscaled
+};
+
+template <bool BF16, int M, int RT, bool DROP>
+__global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, DropArgs d) {
+    constexpr int kRp = 16 * RT, kNw = kCols<BF16, RT>, kSlice = 4 * kNw, kPitch = kSlice * kEs<BF16> + (BF16 ? 32 : 16);
+    __shared__ __align__(16) char lds_w[kRp * kPitch];
+    if (static_cast<int>(blockIdx.x) >= tile_count(list, true)) return;
+    const Tile tile = list.tiles[blockIdx.x];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.y * kSlice;
+    constexpr int kV = kVec<BF16>;
+
+    if (tile.group == list.n) {   // rows without an adapter
+        if (a.u_out && blockIdx.y == 0)
+            for (int i = threadIdx.x; i < tile.count * a.rank; i += 256)
+                a.u_out[static_cast<int64_t>(list.row_of[tile.p0 + i / a.rank]) * a.rank + i % a.rank] = 0.f;
+        if (a.out == a.base && a.ld_o == a.ld_b) return;
+        for (int i = threadIdx.x; i < tile.count * (kSlice / kV); i += 256) {
+            const int64_t row = list.row_of[tile.p0 + i / (kSlice / kV)];
+            const int col = n0 + i % (kSlice / kV) * kV;
+            if (col >= a.width) continue;
+            const u32x4 b = a.base ? ld128(a.base + (row * a.ld_b + col) * kEs<BF16>) : u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4 *>(a.out + (row * a.ld_o + col) * kEs<BF16>) = b;
+        }
+        return;
+    }
+
+    // W's slice, zeros beyond the rank and the width
+    for (int i = threadIdx.x; i < kRp * (kSlice / kV); i += 256) {
+        const int r = i / (kSlice / kV), c = i % (kSlice / kV) * kV;
+        const bool in = r < a.rank && n0 + c < a.width;
+        const u32x4 w = in ? ld128(a.W + ((static_cast<int64_t>(tile.group) * a.rank + r) * a.width + n0 + c) * kEs<BF16>)
+                           : u32x4{0, 0, 0, 0};
+        *reinterpret_cast<u32x4 *>(lds_w + r * kPitch + c * kEs<BF16>) = w;
+    }
+    // the rows' base, while the rest is fetched; lane: 16 bytes of row 16 m + t at column kV g of each piece
+    constexpr int kPieces = kNw / (4 * kV);
+    const int w0 = n0 + wave * kNw;
+    int row[M];
+    u32x4 base[M][kPieces];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        const int i = 16 * m + t;
+        row[m] = i < tile.count ? list.row_of[tile.p0 + i] : -1;
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const int col = w0 + (4 * q + g) * kV;
+            base[m][q] = a.base && row[m] >= 0 && col < a.width ? ld128_nt(a.base + (row[m] * a.ld_b + col) * kEs<BF16>)
+                                                               : u32x4{0, 0, 0, 0};
+        }
+    }
+    const float s = a.scale ? a.scale[tile.group] : 1.f;
+    __syncthreads();
+
+    // MFMA operands from W.  bf16: lane i of the 16 holds the column whose result row is i; result rows 4 g .. + 3
+    // of an even and the next odd block are columns 8 g .. + 3 and 8 g + 4 .. + 7 of a 32-column piece, so that a
+    // lane ends up with eight neighbouring columns.  Contraction: lanes g = 0, 1 ranks 0-7 and 8-15 with U's upper
+    // half, g = 2, 3 the same ranks with its lower half.
+    constexpr int kBlocks = kNw / 16;
+    u32x4 wf[BF16 ? kBlocks : 1][RT];
+    if constexpr (BF16) {
+        const uint32_t l0 = lds_addr(lds_w) + static_cast<uint32_t>(wave * kNw * 2);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const uint32_t at = l0 + static_cast<uint32_t>((16 * r + 8 * (g & 1) + (t >> 2)) * kPitch +
+                                                               (32 * (b >> 1) + 8 * (t & 3) + 4 * (b & 1)) * 2);
+                const s16x4 v8[2] = {read_tr(at), read_tr(at + 4 * kPitch)};
+                wf[b][r] = __builtin_bit_cast(u32x4, v8);
+            }
+    }
+    const int c_own = BF16 ? 8 * (g & 1) : 4 * g;   // first of the lane's ranks within 16
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        if (16 * m >= tile.count) break;
+        const int i = 16 * m + t;
+        // U: the lane's ranks of its row, summed over the splits
+        constexpr int kU = BF16 ? 8 : 4;
+        f32x4 u[RT][kU / 4];
+        const float *up = a.part + (static_cast<int64_t>(tile.p0) + (i < tile.count ? i : 0)) * kRp + c_own;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < kU / 4; ++e) u[r][e] = *reinterpret_cast<const f32x4 *>(up + 16 * r + 4 * e);
+        for (int k = 1; k < a.splits; ++k) {
+            up += a.places * kRp;
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int e = 0; e < kU / 4; ++e) u[r][e] += *reinterpret_cast<const f32x4 *>(up + 16 * r + 4 * e);
+        }
+        if (a.u_out && blockIdx.y == 0 && wave == 0 && row[m] >= 0 && (!BF16 || g < 2)) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int e = 0; e < kU; ++e)
+                    if (16 * r + c_own + e < a.rank)
+                        a.u_out[static_cast<int64_t>(row[m]) * a.rank + 16 * r + c_own + e] = u[r][e >> 2][e & 3];
+        }
+        f32x4 acc[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            if constexpr (BF16) {
+                u32x4 uf;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float lo = u[r][e >> 1][2 * (e & 1)] * s, hi = u[r][e >> 1][2 * (e & 1) + 1] * s;
+                    if (g >= 2) {
+                        lo = left_over(lo);
+                        hi = left_over(hi);
+                    }
+                    uf[e] = pack2(lo, hi);
+                }
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) acc[b] = mfma16_bf16(as_bf16x8(wf[b][r]), as_bf16x8(uf), acc[b]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const char *lw = lds_w + (16 * r + 4 * g + e) * kPitch + (wave * kNw + t) * 4;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b)
+                        acc[b] = mfma16_f32(*reinterpret_cast<const float *>(lw + 64 * b), u[r][0][e] * s, acc[b]);
+                }
+            }
+        }
+        if (row[m] < 0) continue;
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const int col = w0 + (4 * q + g) * kV;
+            if (col >= a.width) continue;
+            float y[kV];
+#pragma unroll
+            for (int e = 0; e < kV; ++e) y[e] = BF16 ? acc[2 * q + (e >> 2)][e & 3] : acc[q][e];
+            if constexpr (DROP) {
+                const u32x4 w = drop_bits(d, static_cast<uint32_t>(row[m]), static_cast<uint32_t>(col) >> 3);
+#pragma unroll
+                for (int e = 0; e < kV; ++e) {
+                    uint32_t word;
+                    if constexpr (BF16)
+                        word = w[e >> 1];
+                    else
+                        word = (col & 4) ? w[2 + (e >> 1)] : w[e >> 1];
+                    y[e] = ((word >> (16 * (e & 1))) & 0xFFFFu) >= d.thr ? y[e] * d.scale : 0.f;
+                }
+            }
+            u32x4 o;
+            if constexpr (BF16) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    o[e] = pack2(y[2 * e] + __uint_as_float(base[m][q][e] << 16),
+                                 y[2 * e + 1] + __uint_as_float(base[m][q][e] & 0xFFFF0000u));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(y[e] + __uint_as_float(base[m][q][e]));
+            }
+            *reinterpret_cast<u32x4 *>(a.out + (row[m] * a.ld_o + col) * kEs<BF16>) = o;
+        }
+    }
+}
+
+// ------------------------------------------------------------------- prep --
+// Operands of k_grad for 32 places: u gathered from its rows, du summed over the
+// splits and scaled.  fp32: [place][rp] both.  bf16: [third][rp][place], and du
+// also as [place][rp] in fp32 for k_expand.
+struct PrepArgs {
+    const float *u;           // [rows][rank]
+    const float *part;        // [splits][places][rp]
+    int splits, rank, rp;
+    int64_t places;
+    const float *scale;
+    float *du;                // [places][rp]
+    float *uS;                // fp32: [places][rp]
+    bf16_bits *uT, *duT;      // bf16: [3][rp][places]
+};
+
+__global__ __launch_bounds__(256) void k_prep(TileList list, PrepArgs a) {
+    if (static_cast<int>(blockIdx.x) >= tile_count(list, false)) return;
+    const Tile tile = list.tiles[blockIdx.x];
+    __shared__ int row[32];
+    __shared__ float vals[2][32][129];   // u and du of the 32 places
+    if (threadIdx.x < 32)
+        row[threadIdx.x] = static_cast<int>(threadIdx.x) < tile.count ? list.row_of[tile.p0 + threadIdx.x] : -1;
+    __syncthreads();
+    const float s = a.scale ? a.scale[tile.group] : 1.f;
+    for (int i = threadIdx.x; i < 32 * a.rp; i += 256) {
+        const int slot = i / a.rp, r = i % a.rp;
+        const int64_t at = (static_cast<int64_t>(tile.p0) + slot) * a.rp + r;
+        float u = 0.f, du = 0.f;
+        if (row[slot] >= 0) {
+            if (r < a.rank) u = a.u[static_cast<int64_t>(row[slot]) * a.rank + r];
+            for (int k = 0; k < a.splits; ++k) du += a.part[k * a.places * a.rp + at];
+            du *= s;
+        }
+        a.du[at] = du;
+        if (a.uS) a.uS[at] = u;
+        vals[0][slot][r] = u;
+        vals[1][slot][r] = du;
+    }
+    if (!a.uT) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.rp * 4; i += 256) {   // (matrix, rank, eight places)
+        const int oct = i & 3, r = (i >> 2) % a.rp, which = (i >> 2) / a.rp;
+        bf16_bits *out = (which ? a.duT : a.uT) + r * a.places + tile.p0 + 8 * oct;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = vals[which][8 * oct + e][r];
+#pragma unroll
+        for (int third = 0; third < 3; ++third) {
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
+            *reinterpret_cast<u32x4 *>(out + third * a.rp * a.places) = w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = left_over(v[e]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------- grad --
+struct GradJob {
+    const char *v;            // rows x or dy
+    int64_t ld;
+    int width, slices;
+    const void *U;            // bf16: [3][rp][places]; fp32: [places][rp]
+    float *part;              // [tiles][rp][width]
+    uint32_t thr;             // dropout of v
+};
+struct GradArgs {
+    GradJob job[2];
+    int64_t places;
+};
+
+constexpr int kGradCols = 256;
+
+template <bool BF16, int RT>
+__global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArgs d) {
+    constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kGradCols * kEs<BF16> + 32;
+    constexpr int kLoads = 32 * (kGradCols / kV) / 256;      // 16-byte loads of a thread for 32 rows
+    constexpr int kRowsPer = 32 / kLoads;                     // rows that the workgroup loads at once
+    __shared__ __align__(16) char lds_v[32 * kPitch];
+    __shared__ int lds_row[512];
+    if (static_cast<int>(blockIdx.x) >= tile_count(list, false)) return;
+    const Tile tile = list.tiles[blockIdx.x];
+    const int which = static_cast<int>(blockIdx.y) >= a.job[0].slices;
+    const GradJob job = which ? a.job[1] : a.job[0];
+    const int n0 = (blockIdx.y - (which ? a.job[0].slices : 0)) * kGradCols;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
+    const int steps = (tile.count + 31) / 32;
+    for (int i = threadIdx.x; i < 32 * steps; i += 256) lds_row[i] = i < tile.count ? list.row_of[tile.p0 + i] : -1;
+    __syncthreads();
+
+    const int lr = threadIdx.x / (kGradCols / kV), lc = threadIdx.x % (kGradCols / kV) * kV;
+    const bool in = n0 + lc < job.width;
+    u32x4 v[kLoads];
+    const auto load = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = lds_row[32 * step + kRowsPer * i + lr];
+            v[i] = in && row >= 0 ? ld128_nt(job.v + (row * job.ld + n0 + lc) * kEs<BF16>) : u32x4{0, 0, 0, 0};
+        }
+    };
+    f32x4 acc[4][RT];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[b][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    load(0);
+    for (int step = 0; step < steps; ++step) {
+        if (step) __syncthreads();   // the waves are done with the rows before
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int slot = kRowsPer * i + lr;
+            if (job.thr) v[i] = drop_piece<BF16>(d, v[i], static_cast<uint32_t>(lds_row[32 * step + slot]), n0 + lc);
+            *reinterpret_cast<u32x4 *>(lds_v + slot * kPitch + lc * kEs<BF16>) = v[i];
+        }
+        __syncthreads();
+        if (step + 1 < steps) load(step + 1);
+        const int64_t p = static_cast<int64_t>(tile.p0) + 32 * step;
+        if constexpr (BF16) {
+            const bf16_bits *U = static_cast<const bf16_bits *>(job.U) + p + 8 * g;
+            u32x4 vf[4];
+            const uint32_t l0 = lds_addr(lds_v) + static_cast<uint32_t>((8 * g + (t >> 2)) * kPitch + (wave * 64 + 4 * (t & 3)) * 2);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const s16x4 v8[2] = {read_tr(l0 + 32 * b), read_tr(l0 + 32 * b + 4 * kPitch)};
+                vf[b] = __builtin_bit_cast(u32x4, v8);
+            }
+#pragma unroll
+            for (int third = 0; third < 3; ++third)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const u32x4 uf = ld128(U + (static_cast<int64_t>(third) * kRp + 16 * r + t) * a.places);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) acc[b][r] = mfma16_bf16(as_bf16x8(vf[b]), as_bf16x8(uf), acc[b][r]);
+                }
+        } else {
+            const float *U = static_cast<const float *>(job.U) + p * kRp + t;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float uf[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) uf[r] = U[(4 * k + g) * kRp + 16 * r];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const float vf = *reinterpret_cast<const float *>(lds_v + (4 * k + g) * kPitch + (wave * 64 + 16 * b + t) * 4);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) acc[b][r] = mfma16_f32(vf, uf[r], acc[b][r]);
+                }
+            }
+        }
+    }
+    // lane holds columns 4 g .. + 3 of block b for rank 16 r + t
+    float *out = job.part + static_cast<int64_t>(blockIdx.x) * kRp * job.width;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const int col = n0 + wave * 64 + 16 * b + 4 * g;
+        if (col >= job.width) continue;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+            *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(16 * r + t) * job.width + col) = acc[b][r];
+    }
+}
+
+struct ReduceJob {
+    const float *part;        // [tiles][rp][width]
+    float *dW;                // [n][rank][width]
+    const float *scale;       // [n] or null
+    float f;
+    int width, slices;
+};
+struct ReduceArgs {
+    ReduceJob job[2];
+    const PlanHead *head;
+    const int *first;
+    int rows, n, rank, rp, accumulate;
+};
+
+// dW_a[r] (+)= f s_a times the sum of its tiles' parts, in their order; zeros
+// for an adapter without rows.
+__global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
+    if (!is_plan(a.head, a.rows, a.n)) return;
+    const int which = static_cast<int>(blockIdx.y) >= a.job[0].slices;
+    const ReduceJob job = which ? a.job[1] : a.job[0];
+    const int col = ((blockIdx.y - (which ? a.job[0].slices : 0)) * 256 + threadIdx.x) * 4;
+    if (col >= job.width) return;
+    const int ad = blockIdx.x / a.rank, r = blockIdx.x % a.rank;
+    const int t0 = a.first[ad], t1 = a.first[ad + 1];
+    const float *p = job.part + (static_cast<int64_t>(t0) * a.rp + r) * job.width + col;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int t = t0; t < t1; ++t) {
+        s += *reinterpret_cast<const f32x4 *>(p);
+        p += static_cast<int64_t>(a.rp) * job.width;
+    }
+    s *= job.f * (job.scale ? job.scale[ad] : 1.f);
+    float *out = job.dW + static_cast<int64_t>(blockIdx.x) * job.width + col;
+    if (a.accumulate) s += *reinterpret_cast<const f32x4 *>(out);
+    *reinterpret_cast<f32x4 *>(out) = s;
+}
+
+__global__ __launch_bounds__(256) void k_zero(float *p, int64_t quads) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i < quads) reinterpret_cast<f32x4 *>(p)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// ------------------------------------------------------------------- host --
+int rank_tiles(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8; }
+
+// Launch shapes, functions of the sizes alone.
+struct Shape {
+    int rt, rp;
+    int64_t places;
+    int h_shrink, h_expand;       // list heights
+    int h_grad;
+};
+
+// Rows per tile: 16 where an adapter has few rows on average (decoding), else as
+// many as share one read of its weights.
+Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
+    Shape s;
+    s.rt = rank_tiles(rank);
+    s.rp = 16 * s.rt;
+    s.places = plan_places(rows, n);
+    const bool few = rows < static_cast<int64_t>(32) * n || rows <= 32;
+    s.h_shrink = few ? 0 : (s.rt == 2 || s.rt == 4) ? 2 : 1;
+    s.h_expand = few ? 0 : 2;
+    // chunks of the gradient: long ones leave few partial sums, short ones give every CU two workgroups
+    const int64_t slices = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
+    s.h_grad = 5;
+    while (s.h_grad > 1 && (rows >> (4 + s.h_grad)) * slices < 512) --s.h_grad;
+    return s;
+}
+
+// Ranges of the long axis in k_shrink: enough workgroups for two on each CU.
+int shrink_splits(const Shape &s, int64_t rows, int n, int width, int *per) {
+    const int64_t tiles = (rows >> (4 + s.h_shrink)) + (n < rows ? n : rows);
+    int64_t want = (512 + tiles - 1) / tiles;
+    const int64_t most = (width + 511) / 512;
+    if (want > most) want = most;
+    if (want > 8) want = 8;
+    if (want < 1) want = 1;
+    *per = static_cast<int>(((width + want - 1) / want + 255) / 256 * 256);
+    return (width + *per - 1) / *per;
+}
+
+struct WsLayout {
+    size_t part, du, u_op, du_op, part_a, part_b, bytes;
+};
+WsLayout ws_layout(const Shape &s, int64_t rows, int n_in, int n_out, int n) {
+    WsLayout l;
+    size_t at = 0;
+    const auto take = [&](size_t b) {
+        const size_t here = at;
+        at += align256(b);
+        return here;
+    };
+    int per;
+    const int sf = shrink_splits(s, rows, n, n_in, &per), sb = shrink_splits(s, rows, n, n_out, &per);
+    const size_t u = static_cast<size_t>(s.places) * s.rp;
+    const size_t tiles = static_cast<size_t>(plan_max_tiles(rows, n, s.h_grad));
+    l.part = take(u * 4 * (sf > sb ? sf : sb));
+    l.du = take(u * 4);
+    l.u_op = take(u * 6);
+    l.du_op = take(u * 6);
+    l.part_a = take(tiles * s.rp * n_in * 4);
+    l.part_b = take(tiles * s.rp * n_out * 4);
+    l.bytes = at;
+    return l;
+}
+
+template <bool BF16, bool DROP, typename F>
+void with_rank(int rt, F f) {
+    switch (rt) {
+        case 1: f(std::integral_constant<int, 1>{}); break;
+        case 2: f(std::integral_constant<int, 2>{}); break;
+        case 4: f(std::integral_constant<int, 4>{}); break;
+        default: f(std::integral_constant<int, 8>{}); break;
+    }
+}
+
+template <bool BF16, bool DROP>
+void run_shrink(const Shape &s, const PlanView &pv, const void *v, int64_t ld, int width, const void *W, int rank,
+                float *part, int splits, int per, const DropArgs &d, hipStream_t st) {
+    const TileList list = tile_list(pv, s.h_shrink);
+    const dim3 grid(static_cast<unsigned>(plan_max_tiles(pv.rows, pv.n, s.h_shrink)), static_cast<unsigned>(splits));
+    with_rank<BF16, DROP>(s.rt, [&](auto rt) {
+        constexpr int RT = decltype(rt)::value, M = RT == 2 || RT == 4 ? 4 : 2;
+        const auto go = [&](auto kernel) {
+            kernel<<<grid, 256, 0, st>>>(list, static_cast<const char *>(v), ld, width, static_cast<const char *>(W), rank,
+                                         part, s.places, per, d);
+        };
+        s.h_shrink == 0 ? go(k_shrink<BF16, 1, RT, DROP>) : go(k_shrink<BF16, M, RT, DROP>);
+    });
+}
+
+template <bool BF16, bool DROP>
+void run_expand(const Shape &s, const PlanView &pv, const ExpandArgs &a, const DropArgs &d, hipStream_t st) {
+    const TileList list = tile_list(pv, s.h_expand);
+    with_rank<BF16, DROP>(s.rt, [&](auto rt) {
+        constexpr int RT = decltype(rt)::value, kSlice = 4 * kCols<BF16, RT>;
+        const dim3 grid(static_cast<unsigned>(plan_max_tiles(pv.rows, pv.n, s.h_expand)),
+                        static_cast<unsigned>((a.width + kSlice - 1) / kSlice));
+        s.h_expand == 0 ? k_expand<BF16, 1, RT, DROP><<<grid, 256, 0, st>>>(list, a, d)
+                        : k_expand<BF16, 4, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
+    });
+}
+
+}  // namespace
+
+size_t adapter_plan_bytes(int64_t rows, int n) { return plan_layout(rows, n).bytes; }
+
+hipError_t launch_adapter_plan(const int *row_adapter, int64_t rows, int n, void *plan, hipStream_t s) {
+    const PlanView v = plan_view(plan, rows, n);
+    const int segs = static_cast<int>((rows + kSeg - 1) / kSeg);
+    k_plan_hist<<<segs, 256, 0, s>>>(row_adapter, v);
+    k_plan_scan<<<1, 1024, 0, s>>>(v, segs);
+    k_plan_scatter<<<segs, 256, 0, s>>>(row_adapter, v);
+    return hipGetLastError();
+}
+
+size_t adapter_ws_bytes(int64_t rows, int n_in, int n_out, int rank, int n) {
+    return ws_layout(shape_of(rows, n_in, n_out, rank, n), rows, n_in, n_out, n).bytes;
+}
+
+hipError_t launch_adapter_forward(const AdapterDims &m, bool bf16, const void *plan, const void *x, int64_t ld_x,
+                                  const void *A, const void *B, const float *scale, const void *base, int64_t ld_b,
+                                  void *y, int64_t ld_y, float *u, double p, uint64_t seed, uint64_t offset, void *ws,
+                                  hipStream_t st) {
+    const DropArgs d = drop_args(p, seed, offset);
+    const PlanView pv = plan_view(const_cast<void *>(plan), m.rows, m.n);
+    const Shape s = shape_of(m.rows, m.n_in, m.n_out, m.rank, m.n);
+    const WsLayout l = ws_layout(s, m.rows, m.n_in, m.n_out, m.n);
+    float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
+    int per;
+    const int splits = shrink_splits(s, m.rows, m.n, m.n_in, &per);
+    const ExpandArgs e = {part, splits, s.places, scale, static_cast<const char *>(B), m.rank, m.n_out,
+                          static_cast<const char *>(base), ld_b, static_cast<char *>(y), ld_y, u};
+    const auto go = [&](auto b) {
+        constexpr bool BF16 = decltype(b)::value;
+        if (d.thr)
+            run_shrink<BF16, true>(s, pv, x, ld_x, m.n_in, A, m.rank, part, splits, per, d, st);
+        else
+            run_shrink<BF16, false>(s, pv, x, ld_x, m.n_in, A, m.rank, part, splits, per, d, st);
+        run_expand<BF16, false>(s, pv, e, d, st);
+    };
+    bf16 ? go(std::true_type{}) : go(std::false_type{});
+    return hipGetLastError();
+}
+
+hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *plan, const void *x, int64_t ld_x,
+                                   const void *dy, int64_t ld_dy, const void *A, const void *B, const float *scale,
+                                   const float *u, const void *base, int64_t ld_b, void *dx, int64_t ld_dx, float *dA,
+                                   float *dB, bool accumulate, double drop_p, uint64_t seed, uint64_t offset, void *ws,
+                                   hipStream_t st) {
+    const DropArgs d = drop_args(drop_p, seed, offset);
+    if (m.rows == 0) {   // sums over nothing
+        if (!accumulate) {
+            const int64_t na = static_cast<int64_t>(m.n) * m.rank * m.n_in / 4, nb = static_cast<int64_t>(m.n) * m.rank * m.n_out / 4;
+            k_zero<<<static_cast<unsigned>((na + 255) / 256), 256, 0, st>>>(dA, na);
+            k_zero<<<static_cast<unsigned>((nb + 255) / 256), 256, 0, st>>>(dB, nb);
+        }
+        return hipGetLastError();
+    }
+    const PlanView pv = plan_view(const_cast<void *>(plan), m.rows, m.n);
+    const Shape s = shape_of(m.rows, m.n_in, m.n_out, m.rank, m.n);
+    const WsLayout l = ws_layout(s, m.rows, m.n_in, m.n_out, m.n);
+    char *w = static_cast<char *>(ws);
+    float *part = reinterpret_cast<float *>(w + l.part), *du = reinterpret_cast<float *>(w + l.du);
+    int per;
+    const int splits = shrink_splits(s, m.rows, m.n, m.n_out, &per);
+    const auto go = [&](auto b) {
+        constexpr bool BF16 = decltype(b)::value;
+        run_shrink<BF16, false>(s, pv, dy, ld_dy, m.n_out, B, m.rank, part, splits, per, d, st);
+        PrepArgs p = {};
+        p.u = u;
+        p.part = part;
+        p.splits = splits;
+        p.rank = m.rank;
+        p.rp = s.rp;
+        p.places = s.places;
+        p.scale = scale;
+        p.du = du;
+        if (BF16) {
+            p.uT = reinterpret_cast<bf16_bits *>(w + l.u_op);
+            p.duT = reinterpret_cast<bf16_bits *>(w + l.du_op);
+        } else {
+            p.uS = reinterpret_cast<float *>(w + l.u_op);
+        }
+        k_prep<<<static_cast<unsigned>(plan_max_tiles(m.rows, m.n, 1)), 256, 0, st>>>(tile_list(pv, 1), p);
+        GradArgs ga = {};
+        ga.places = s.places;
+        ga.job[0] = {static_cast<const char *>(dy), ld_dy, m.n_out, (m.n_out + kGradCols - 1) / kGradCols, w + l.u_op,
+                     reinterpret_cast<float *>(w + l.part_b), 0};
+        ga.job[1] = {static_cast<const char *>(x), ld_x, m.n_in, (m.n_in + kGradCols - 1) / kGradCols,
+                     BF16 ? static_cast<const void *>(w + l.du_op) : du, reinterpret_cast<float *>(w + l.part_a), d.thr};
+        const dim3 grid(static_cast<unsigned>(plan_max_tiles(m.rows, m.n, s.h_grad)),
+                        static_cast<unsigned>(ga.job[0].slices + ga.job[1].slices));
+        with_rank<BF16, false>(s.rt, [&](auto rt) {
+            k_grad<BF16, decltype(rt)::value><<<grid, 256, 0, st>>>(tile_list(pv, s.h_grad), ga, d);
+        });
+        ReduceArgs r = {};
+        r.job[0] = {ga.job[0].part, dB, scale, 1.f, m.n_out, (m.n_out + 1023) / 1024};
+        r.job[1] = {ga.job[1].part, dA, nullptr, d.scale, m.n_in, (m.n_in + 1023) / 1024};
+        r.head = pv.head;
+        r.first = pv.first[s.h_grad];
+        r.rows = pv.rows;
+        r.n = m.n;
+        r.rank = m.rank;
+        r.rp = s.rp;
+        r.accumulate = accumulate;
+        k_reduce<<<dim3(static_cast<unsigned>(m.n * m.rank), static_cast<unsigned>(r.job[0].slices + r.job[1].slices)), 256, 0,
+                   st>>>(r);
+        if (dx) {
+            const ExpandArgs e = {du, 1, s.places, nullptr, static_cast<const char *>(A), m.rank, m.n_in,
+                                  static_cast<const char *>(base), ld_b, static_cast<char *>(dx), ld_dx, nullptr};
+            d.thr ? run_expand<BF16, true>(s, pv, e, d, st) : run_expand<BF16, false>(s, pv, e, d, st);
+        }
+    };
+    bf16 ? go(std::true_type{}) : go(std::false_type{});
+    return hipGetLastError();
+}
+
+}  // namespace logra

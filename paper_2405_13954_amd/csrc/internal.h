@@ -159,4 +159,32 @@ hipError_t launch_topk_filtered(const float *s, int64_t ld_s, int Q, int64_t N, 
                                 float *val, int64_t *idx, const int *cnt, const float *cval,
                                 const int *cidx, int cap, hipStream_t st);
 
+// Dropout, adapters and the token loss (adapter.hip, dropout.hip, loss.hip).
+struct DropArgs;                         // counter_rng.h
+constexpr int kMaxAdapters = 1023;       // with the rows that have none, 1024 groups: one thread each
+constexpr int kMaxAdapterRank = 128;
+constexpr int64_t kMaxAdapterRows = 1 << 24;
+struct AdapterDims {
+    int64_t rows;
+    int n_in, n_out, rank, n;
+};
+size_t adapter_plan_bytes(int64_t rows, int n);
+hipError_t launch_adapter_plan(const int *row_adapter, int64_t rows, int n, void *plan, hipStream_t s);
+size_t adapter_ws_bytes(int64_t rows, int n_in, int n_out, int rank, int n);
+hipError_t launch_adapter_forward(const AdapterDims &m, bool bf16, const void *plan, const void *x, int64_t ld_x,
+                                  const void *A, const void *B, const float *scale, const void *base, int64_t ld_b,
+                                  void *y, int64_t ld_y, float *u, double p, uint64_t seed, uint64_t offset, void *ws,
+                                  hipStream_t st);
+hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *plan, const void *x, int64_t ld_x,
+                                   const void *dy, int64_t ld_dy, const void *A, const void *B, const float *scale,
+                                   const float *u, const void *base, int64_t ld_b, void *dx, int64_t ld_dx, float *dA,
+                                   float *dB, bool accumulate, double p, uint64_t seed, uint64_t offset, void *ws,
+                                   hipStream_t st);
+DropArgs drop_args(double p, uint64_t seed, uint64_t offset);
+hipError_t launch_dropout(const void *x, int64_t ld_x, bool bf16, int64_t rows, int cols, const void *res,
+                          int64_t ld_r, void *out, int64_t ld_o, double p, uint64_t seed, uint64_t offset,
+                          hipStream_t s);
+hipError_t launch_token_loss(const void *logits, int64_t ld, bool bf16, int64_t rows, int vocab, const int64_t *target,
+                             const float *weight, float *loss, void *dlogits, int64_t ld_d, hipStream_t s);
+
 }  // namespace logra
