@@ -44,6 +44,9 @@
 namespace logra {
 namespace {
 
+#ifndef SPLIT_TARGET
+#define SPLIT_TARGET 512
+#endif
 constexpr int kHeights = 6;          // tile lists of 16 << h rows
 constexpr int kSeg = 4096;           // rows of one workgroup of the plan's kernels
 constexpr int kPlanMagic = 0x4c6f4164;
@@ -264,6 +267,40 @@ __global__ __launch_bounds__(256) void k_plan_scatter(const int *row_adapter, Pl
     }
 }
 
+// Memory and matrix operands want different lanes.  An operand or result of a
+// 16-row block has row t = l % 16 in lane l, and 16 bytes of column group
+// g = l / 16: 64-byte pieces of 16 rows.  Memory streams best in 128-byte pieces
+// of 8 rows (read + write at 5.6 TB/s against 4.4 to 4.9 for 64-byte ones).  Two
+// neighbouring 64-byte pieces of the block, a and b, and the 128-byte pieces of
+// its rows 0-7 and 8-15 are turned into each other by one exchange between lanes
+// l and l ^ 8.
+__device__ __forceinline__ void swap8(u32x4 &a, u32x4 &b) {
+    const bool low = (threadIdx.x & 8) == 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t send = low ? b[e] : a[e];
+        const uint32_t got = static_cast<uint32_t>(
+            __builtin_amdgcn_mov_dpp(static_cast<int>(send), 0x128 /* rotate 16 lanes by 8 */, 0xf, 0xf, false));
+        if (low)
+            b[e] = got;
+        else
+            a[e] = got;
+    }
+}
+// The lane's place in such a pair: row of the first piece (the second's is 8
+// more) and its 16-byte column within the 128 bytes.
+__device__ __forceinline__ int pair_row() { return threadIdx.x & 7; }
+__device__ __forceinline__ int pair_col() { return ((threadIdx.x >> 3) & 1) * 4 + ((threadIdx.x >> 4) & 3); }
+
+// Tiles are the slow index of a grid, so that workgroups that run together work
+// on the same rows (4.4 TB/s with the rows as the fast one); beyond 2^15 tiles
+// they go on in z.
+__device__ __forceinline__ int tile_index() { return blockIdx.y + gridDim.y * blockIdx.z; }
+inline dim3 tile_grid(int64_t fast, int64_t tiles) {
+    const int64_t y = tiles < (1 << 15) ? tiles : (1 << 15);
+    return dim3(static_cast<unsigned>(fast), static_cast<unsigned>(y), static_cast<unsigned>((tiles + y - 1) / y));
+}
+
 // ----------------------------------------------------------------- shrink --
 template <bool BF16>
 constexpr int kEs = BF16 ? 2 : 4;
@@ -293,21 +330,25 @@ __global__ __launch_bounds__(256) void k_shrink(TileList list, const char *v, in
                                                 int rank, float *part, int64_t places, int per_split, DropArgs d) {
     constexpr int kRp = 16 * RT, kUnit = 8 * kVec<BF16>;   // 128 bytes of a row
     __shared__ float red[4][16 * M][kRp];
-    if (static_cast<int>(blockIdx.x) >= tile_count(list, false)) return;
-    const Tile tile = list.tiles[blockIdx.x];
+    const int at = tile_index();
+    if (at >= tile_count(list, false)) return;
+    const Tile tile = list.tiles[at];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
-    const int begin = blockIdx.y * per_split;
+    const int begin = blockIdx.x * per_split;
     const int end = width - begin < per_split ? width : begin + per_split;
 
-    int row[M];
-    const char *vp[M];
+    // rows of the two 128-byte pieces of each 16-row block
+    int row[M][2];
+    const char *vp[M][2];
     const char *wp[RT];
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-        const int i = 16 * m + t;
-        row[m] = list.row_of[tile.p0 + (i < tile.count ? i : 0)];
-        vp[m] = v + row[m] * ld * kEs<BF16> + 16 * g;
-    }
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = 16 * m + 8 * h + pair_row();
+            row[m][h] = list.row_of[tile.p0 + (i < tile.count ? i : 0)];
+            vp[m][h] = v + row[m][h] * ld * kEs<BF16> + 16 * pair_col();
+        }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int i = 16 * r + t;
@@ -326,22 +367,26 @@ __global__ __launch_bounds__(256) void k_shrink(TileList list, const char *v, in
     const auto load = [&](Piece &p, int j, bool whole) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t off = static_cast<int64_t>(j) * kEs<BF16> + 64 * h;
-            const bool in = whole || j + (4 * h + g) * kVec<BF16> < end;
+            const int64_t off = static_cast<int64_t>(j) * kEs<BF16>;
+            const bool in_x = whole || j + pair_col() * kVec<BF16> < end, in_w = whole || j + (4 * h + g) * kVec<BF16> < end;
 #pragma unroll
-            for (int m = 0; m < M; ++m) p.x[h][m] = in ? ld128(vp[m] + off) : u32x4{0, 0, 0, 0};
+            for (int m = 0; m < M; ++m) p.x[h][m] = in_x ? ld128_nt(vp[m][h] + off) : u32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < RT; ++r) p.w[h][r] = in ? ld128(wp[r] + off) : u32x4{0, 0, 0, 0};
+            for (int r = 0; r < RT; ++r) p.w[h][r] = in_w ? ld128(wp[r] + off + 64 * h) : u32x4{0, 0, 0, 0};
         }
     };
     const auto multiply = [&](Piece &p, int j) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int m = 0; m < M; ++m) {
             if constexpr (DROP) {
 #pragma unroll
-                for (int m = 0; m < M; ++m)
-                    p.x[h][m] = drop_piece<BF16>(d, p.x[h][m], static_cast<uint32_t>(row[m]), j + (4 * h + g) * kVec<BF16>);
+                for (int h = 0; h < 2; ++h)
+                    p.x[h][m] = drop_piece<BF16>(d, p.x[h][m], static_cast<uint32_t>(row[m][h]), j + pair_col() * kVec<BF16>);
             }
+            swap8(p.x[0][m], p.x[1][m]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
@@ -374,7 +419,7 @@ __global__ __launch_bounds__(256) void k_shrink(TileList list, const char *v, in
         for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4 *>(&red[wave][16 * m + t][16 * r + 4 * g]) = acc[m][r];
     __syncthreads();
     const float f = DROP ? d.scale : 1.f;
-    float *out = part + (static_cast<int64_t>(blockIdx.y) * places + tile.p0) * kRp;
+    float *out = part + (static_cast<int64_t>(blockIdx.x) * places + tile.p0) * kRp;
     for (int i = threadIdx.x; i < 16 * M * kRp / 4; i += 256) {
         const int slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
         if (slot >= tile.count) break;
@@ -423,18 +468,21 @@ struct ExpandArgs {
     float *u_out;             // [rows][rank] or null: the sum of the partials, unscaled
 };
 
+// One workgroup: 16 M rows and four waves' columns.
 template <bool BF16, int M, int RT, bool DROP>
 __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, DropArgs d) {
     constexpr int kRp = 16 * RT, kNw = kCols<BF16, RT>, kSlice = 4 * kNw, kPitch = kSlice * kEs<BF16> + (BF16 ? 32 : 16);
+    constexpr int kV = kVec<BF16>, kUPitch = 4 * kRp + 16;   // a row of U: bf16 upper halves then lower halves, or fp32
     __shared__ __align__(16) char lds_w[kRp * kPitch];
-    if (static_cast<int>(blockIdx.x) >= tile_count(list, true)) return;
-    const Tile tile = list.tiles[blockIdx.x];
+    __shared__ __align__(16) char lds_u[16 * M * kUPitch];
+    const int at = tile_index();
+    if (at >= tile_count(list, true)) return;
+    const Tile tile = list.tiles[at];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.y * kSlice;
-    constexpr int kV = kVec<BF16>;
+    const int n0 = blockIdx.x * kSlice;
 
     if (tile.group == list.n) {   // rows without an adapter
-        if (a.u_out && blockIdx.y == 0)
+        if (a.u_out && blockIdx.x == 0)
             for (int i = threadIdx.x; i < tile.count * a.rank; i += 256)
                 a.u_out[static_cast<int64_t>(list.row_of[tile.p0 + i / a.rank]) * a.rank + i % a.rank] = 0.f;
         if (a.out == a.base && a.ld_o == a.ld_b) return;
@@ -442,11 +490,33 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
             const int64_t row = list.row_of[tile.p0 + i / (kSlice / kV)];
             const int col = n0 + i % (kSlice / kV) * kV;
             if (col >= a.width) continue;
-            const u32x4 b = a.base ? ld128(a.base + (row * a.ld_b + col) * kEs<BF16>) : u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(a.out + (row * a.ld_o + col) * kEs<BF16>) = b;
+            const u32x4 b = a.base ? ld128_nt(a.base + (row * a.ld_b + col) * kEs<BF16>) : u32x4{0, 0, 0, 0};
+            __builtin_nontemporal_store(b, reinterpret_cast<u32x4 *>(a.out + (row * a.ld_o + col) * kEs<BF16>));
         }
         return;
     }
+
+    // The rows' base first: it is on its way while the operands are put together.  128-byte pieces of 8 rows (64-byte
+    // pieces of 16 rows where the wave has only 64 bytes of columns).
+    constexpr int kPairs = kNw * kEs<BF16> / 128, kLoads = kPairs ? 2 : 1;
+    const int w0 = n0 + wave * kNw;
+    int row[M][kLoads];
+    u32x4 base[M][kPairs ? kPairs : 1][kLoads];
+    const int col0 = w0 + (kPairs ? pair_col() : g) * kV;
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < kLoads; ++h) {
+            const int i = 16 * m + (kPairs ? 8 * h + pair_row() : t);
+            row[m][h] = i < tile.count ? list.row_of[tile.p0 + i] : -1;
+#pragma unroll
+            for (int q = 0; q < (kPairs ? kPairs : 1); ++q) {
+                const int col = col0 + 8 * q * kV;
+                base[m][q][h] = a.base && row[m][h] >= 0 && col < a.width
+                                    ? ld128_nt(a.base + (row[m][h] * a.ld_b + col) * kEs<BF16>)
+                                    : u32x4{0, 0, 0, 0};
+            }
+        }
 
     // W's slice, zeros beyond the rank and the width
     for (int i = threadIdx.x; i < kRp * (kSlice / kV); i += 256) {
@@ -456,23 +526,34 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
                            : u32x4{0, 0, 0, 0};
         *reinterpret_cast<u32x4 *>(lds_w + r * kPitch + c * kEs<BF16>) = w;
     }
-    // the rows' base, while the rest is fetched; lane: 16 bytes of row 16 m + t at column kV g of each piece
-    constexpr int kPieces = kNw / (4 * kV);
-    const int w0 = n0 + wave * kNw;
-    int row[M];
-    u32x4 base[M][kPieces];
+    // U: the splits' sums, scaled, as operands
+    const float s = a.scale ? a.scale[tile.group] : 1.f;
+    for (int i = threadIdx.x; i < 16 * M * kRp / 4; i += 256) {
+        const int slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
+        if (slot >= tile.count) break;
+        const float *up = a.part + (static_cast<int64_t>(tile.p0) + slot) * kRp + r;
+        f32x4 u = *reinterpret_cast<const f32x4 *>(up);
+        for (int k = 1; k < a.splits; ++k) {
+            up += a.places * kRp;
+            u += *reinterpret_cast<const f32x4 *>(up);
+        }
+        if (a.u_out && blockIdx.x == 0) {
+            float *o = a.u_out + static_cast<int64_t>(list.row_of[tile.p0 + slot]) * a.rank + r;
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-        const int i = 16 * m + t;
-        row[m] = i < tile.count ? list.row_of[tile.p0 + i] : -1;
-#pragma unroll
-        for (int q = 0; q < kPieces; ++q) {
-            const int col = w0 + (4 * q + g) * kV;
-            base[m][q] = a.base && row[m] >= 0 && col < a.width ? ld128_nt(a.base + (row[m] * a.ld_b + col) * kEs<BF16>)
-                                                               : u32x4{0, 0, 0, 0};
+            for (int e = 0; e < 4; ++e)
+                if (r + e < a.rank) o[e] = u[e];
+        }
+        u *= s;
+        if constexpr (BF16) {
+            uint32_t *o = reinterpret_cast<uint32_t *>(lds_u + slot * kUPitch + 2 * r);
+            o[0] = pack2(u[0], u[1]);
+            o[1] = pack2(u[2], u[3]);
+            o[kRp / 2] = pack2(left_over(u[0]), left_over(u[1]));
+            o[kRp / 2 + 1] = pack2(left_over(u[2]), left_over(u[3]));
+        } else {
+            *reinterpret_cast<f32x4 *>(lds_u + slot * kUPitch + 4 * r) = u;
         }
     }
-    const float s = a.scale ? a.scale[tile.group] : 1.f;
     __syncthreads();
 
     // MFMA operands from W.  bf16: lane i of the 16 holds the column whose result row is i; result rows 4 g .. + 3
@@ -487,78 +568,45 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const uint32_t at = l0 + static_cast<uint32_t>((16 * r + 8 * (g & 1) + (t >> 2)) * kPitch +
-                                                               (32 * (b >> 1) + 8 * (t & 3) + 4 * (b & 1)) * 2);
-                const s16x4 v8[2] = {read_tr(at), read_tr(at + 4 * kPitch)};
+                const uint32_t p = l0 + static_cast<uint32_t>((16 * r + 8 * (g & 1) + (t >> 2)) * kPitch +
+                                                              (32 * (b >> 1) + 8 * (t & 3) + 4 * (b & 1)) * 2);
+                const s16x4 v8[2] = {read_tr(p), read_tr(p + 4 * kPitch)};
                 wf[b][r] = __builtin_bit_cast(u32x4, v8);
             }
     }
-    const int c_own = BF16 ? 8 * (g & 1) : 4 * g;   // first of the lane's ranks within 16
 #pragma unroll
     for (int m = 0; m < M; ++m) {
         if (16 * m >= tile.count) break;
-        const int i = 16 * m + t;
-        // U: the lane's ranks of its row, summed over the splits
-        constexpr int kU = BF16 ? 8 : 4;
-        f32x4 u[RT][kU / 4];
-        const float *up = a.part + (static_cast<int64_t>(tile.p0) + (i < tile.count ? i : 0)) * kRp + c_own;
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int e = 0; e < kU / 4; ++e) u[r][e] = *reinterpret_cast<const f32x4 *>(up + 16 * r + 4 * e);
-        for (int k = 1; k < a.splits; ++k) {
-            up += a.places * kRp;
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int e = 0; e < kU / 4; ++e) u[r][e] += *reinterpret_cast<const f32x4 *>(up + 16 * r + 4 * e);
-        }
-        if (a.u_out && blockIdx.y == 0 && wave == 0 && row[m] >= 0 && (!BF16 || g < 2)) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int e = 0; e < kU; ++e)
-                    if (16 * r + c_own + e < a.rank)
-                        a.u_out[static_cast<int64_t>(row[m]) * a.rank + 16 * r + c_own + e] = u[r][e >> 2][e & 3];
-        }
         f32x4 acc[kBlocks];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const char *lu = lds_u + (16 * m + t) * kUPitch;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             if constexpr (BF16) {
-                u32x4 uf;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float lo = u[r][e >> 1][2 * (e & 1)] * s, hi = u[r][e >> 1][2 * (e & 1) + 1] * s;
-                    if (g >= 2) {
-                        lo = left_over(lo);
-                        hi = left_over(hi);
-                    }
-                    uf[e] = pack2(lo, hi);
-                }
+                const u32x4 uf = *reinterpret_cast<const u32x4 *>(lu + (g >> 1) * 2 * kRp + (16 * r + 8 * (g & 1)) * 2);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) acc[b] = mfma16_bf16(as_bf16x8(wf[b][r]), as_bf16x8(uf), acc[b]);
             } else {
+                const f32x4 uf = *reinterpret_cast<const f32x4 *>(lu + (16 * r + 4 * g) * 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const char *lw = lds_w + (16 * r + 4 * g + e) * kPitch + (wave * kNw + t) * 4;
 #pragma unroll
                     for (int b = 0; b < kBlocks; ++b)
-                        acc[b] = mfma16_f32(*reinterpret_cast<const float *>(lw + 64 * b), u[r][0][e] * s, acc[b]);
+                        acc[b] = mfma16_f32(*reinterpret_cast<const float *>(lw + 64 * b), uf[e], acc[b]);
                 }
             }
         }
-        if (row[m] < 0) continue;
-#pragma unroll
-        for (int q = 0; q < kPieces; ++q) {
-            const int col = w0 + (4 * q + g) * kV;
-            if (col >= a.width) continue;
+        // block row t, 64-byte piece q: the lane's kV columns at w0 + (4 q + g) kV
+        const int own = DROP && 16 * m + t < tile.count ? list.row_of[tile.p0 + 16 * m + t] : 0;
+        const auto finish = [&](int q, u32x4 b) {
             float y[kV];
 #pragma unroll
             for (int e = 0; e < kV; ++e) y[e] = BF16 ? acc[2 * q + (e >> 2)][e & 3] : acc[q][e];
             if constexpr (DROP) {
-                const u32x4 w = drop_bits(d, static_cast<uint32_t>(row[m]), static_cast<uint32_t>(col) >> 3);
+                const int col = w0 + (4 * q + g) * kV;
+                const u32x4 w = drop_bits(d, static_cast<uint32_t>(own), static_cast<uint32_t>(col) >> 3);
 #pragma unroll
                 for (int e = 0; e < kV; ++e) {
                     uint32_t word;
@@ -573,13 +621,29 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
             if constexpr (BF16) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    o[e] = pack2(y[2 * e] + __uint_as_float(base[m][q][e] << 16),
-                                 y[2 * e + 1] + __uint_as_float(base[m][q][e] & 0xFFFF0000u));
+                    o[e] = pack2(y[2 * e] + __uint_as_float(b[e] << 16), y[2 * e + 1] + __uint_as_float(b[e] & 0xFFFF0000u));
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(y[e] + __uint_as_float(base[m][q][e]));
+                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(y[e] + __uint_as_float(b[e]));
             }
-            *reinterpret_cast<u32x4 *>(a.out + (row[m] * a.ld_o + col) * kEs<BF16>) = o;
+            return o;
+        };
+#pragma unroll
+        for (int q = 0; q < (kPairs ? kPairs : 1); ++q) {
+            u32x4 o[2];
+            if constexpr (kPairs > 0) {
+                swap8(base[m][q][0], base[m][q][1]);
+                o[0] = finish(2 * q, base[m][q][0]);
+                o[1] = finish(2 * q + 1, base[m][q][1]);
+                swap8(o[0], o[1]);
+            } else {
+                o[0] = finish(0, base[m][0][0]);
+            }
+            const int col = col0 + 8 * q * kV;
+#pragma unroll
+            for (int h = 0; h < kLoads; ++h)
+                if (row[m][h] >= 0 && col < a.width)
+                    __builtin_nontemporal_store(o[h], reinterpret_cast<u32x4 *>(a.out + (row[m][h] * a.ld_o + col) * kEs<BF16>));
         }
     }
 }
@@ -665,11 +729,12 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
     constexpr int kRowsPer = 32 / kLoads;                     // rows that the workgroup loads at once
     __shared__ __align__(16) char lds_v[32 * kPitch];
     __shared__ int lds_row[512];
-    if (static_cast<int>(blockIdx.x) >= tile_count(list, false)) return;
-    const Tile tile = list.tiles[blockIdx.x];
-    const int which = static_cast<int>(blockIdx.y) >= a.job[0].slices;
+    const int at = tile_index();
+    if (at >= tile_count(list, false)) return;
+    const Tile tile = list.tiles[at];
+    const int which = static_cast<int>(blockIdx.x) >= a.job[0].slices;
     const GradJob job = which ? a.job[1] : a.job[0];
-    const int n0 = (blockIdx.y - (which ? a.job[0].slices : 0)) * kGradCols;
+    const int n0 = (blockIdx.x - (which ? a.job[0].slices : 0)) * kGradCols;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
     const int steps = (tile.count + 31) / 32;
     for (int i = threadIdx.x; i < 32 * steps; i += 256) lds_row[i] = i < tile.count ? list.row_of[tile.p0 + i] : -1;
@@ -736,7 +801,7 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
         }
     }
     // lane holds columns 4 g .. + 3 of block b for rank 16 r + t
-    float *out = job.part + static_cast<int64_t>(blockIdx.x) * kRp * job.width;
+    float *out = job.part + static_cast<int64_t>(at) * kRp * job.width;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const int col = n0 + wave * 64 + 16 * b + 4 * g;
@@ -795,8 +860,7 @@ int rank_tiles(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ?
 struct Shape {
     int rt, rp;
     int64_t places;
-    int h_shrink, h_expand;       // list heights
-    int h_grad;
+    int h_shrink, h_grad;         // list heights
 };
 
 // Rows per tile: 16 where an adapter has few rows on average (decoding), else as
@@ -808,7 +872,6 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     s.places = plan_places(rows, n);
     const bool few = rows < static_cast<int64_t>(32) * n || rows <= 32;
     s.h_shrink = few ? 0 : (s.rt == 2 || s.rt == 4) ? 2 : 1;
-    s.h_expand = few ? 0 : 2;
     // chunks of the gradient: long ones leave few partial sums, short ones give every CU two workgroups
     const int64_t slices = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
     s.h_grad = 5;
@@ -819,7 +882,7 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
 // Ranges of the long axis in k_shrink: enough workgroups for two on each CU.
 int shrink_splits(const Shape &s, int64_t rows, int n, int width, int *per) {
     const int64_t tiles = (rows >> (4 + s.h_shrink)) + (n < rows ? n : rows);
-    int64_t want = (512 + tiles - 1) / tiles;
+    int64_t want = (SPLIT_TARGET + tiles - 1) / tiles;
     const int64_t most = (width + 511) / 512;
     if (want > most) want = most;
     if (want > 8) want = 8;
@@ -867,7 +930,7 @@ template <bool BF16, bool DROP>
 void run_shrink(const Shape &s, const PlanView &pv, const void *v, int64_t ld, int width, const void *W, int rank,
                 float *part, int splits, int per, const DropArgs &d, hipStream_t st) {
     const TileList list = tile_list(pv, s.h_shrink);
-    const dim3 grid(static_cast<unsigned>(plan_max_tiles(pv.rows, pv.n, s.h_shrink)), static_cast<unsigned>(splits));
+    const dim3 grid = tile_grid(splits, plan_max_tiles(pv.rows, pv.n, s.h_shrink));
     with_rank<BF16, DROP>(s.rt, [&](auto rt) {
         constexpr int RT = decltype(rt)::value, M = RT == 2 || RT == 4 ? 4 : 2;
         const auto go = [&](auto kernel) {
@@ -880,13 +943,20 @@ void run_shrink(const Shape &s, const PlanView &pv, const void *v, int64_t ld, i
 
 template <bool BF16, bool DROP>
 void run_expand(const Shape &s, const PlanView &pv, const ExpandArgs &a, const DropArgs &d, hipStream_t st) {
-    const TileList list = tile_list(pv, s.h_expand);
     with_rank<BF16, DROP>(s.rt, [&](auto rt) {
         constexpr int RT = decltype(rt)::value, kSlice = 4 * kCols<BF16, RT>;
-        const dim3 grid(static_cast<unsigned>(plan_max_tiles(pv.rows, pv.n, s.h_expand)),
-                        static_cast<unsigned>((a.width + kSlice - 1) / kSlice));
-        s.h_expand == 0 ? k_expand<BF16, 1, RT, DROP><<<grid, 256, 0, st>>>(list, a, d)
-                        : k_expand<BF16, 4, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
+        // the tallest tiles that leave two workgroups for each CU (64 rows, 32 at rank 128, whose operands fill LDS)
+        const int64_t slices = (a.width + kSlice - 1) / kSlice;
+        int h = RT == 8 ? 1 : 2;
+        while (h > 0 && (static_cast<int64_t>(pv.rows) >> (4 + h)) * slices < 512) --h;
+        const TileList list = tile_list(pv, h);
+        const dim3 grid = tile_grid(slices, plan_max_tiles(pv.rows, pv.n, h));
+        if (h == 0)
+            k_expand<BF16, 1, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
+        else if (RT == 8 || h == 1)
+            k_expand<BF16, 2, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
+        else
+            k_expand<BF16, RT == 8 ? 2 : 4, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
     });
 }
 
@@ -978,8 +1048,7 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
                      reinterpret_cast<float *>(w + l.part_b), 0};
         ga.job[1] = {static_cast<const char *>(x), ld_x, m.n_in, (m.n_in + kGradCols - 1) / kGradCols,
                      BF16 ? static_cast<const void *>(w + l.du_op) : du, reinterpret_cast<float *>(w + l.part_a), d.thr};
-        const dim3 grid(static_cast<unsigned>(plan_max_tiles(m.rows, m.n, s.h_grad)),
-                        static_cast<unsigned>(ga.job[0].slices + ga.job[1].slices));
+        const dim3 grid = tile_grid(ga.job[0].slices + ga.job[1].slices, plan_max_tiles(m.rows, m.n, s.h_grad));
         with_rank<BF16, false>(s.rt, [&](auto rt) {
             k_grad<BF16, decltype(rt)::value><<<grid, 256, 0, st>>>(tile_list(pv, s.h_grad), ga, d);
         });
