@@ -45,7 +45,13 @@ namespace logra {
 namespace {
 
 #ifndef SPLIT_TARGET
-#define SPLIT_TARGET 512
+#define SPLIT_TARGET 2048
+#endif
+#ifndef GRUNS
+#define GRUNS 1024
+#endif
+#ifndef EXP_H
+#define EXP_H 2
 #endif
 constexpr int kHeights = 6;          // tile lists of 16 << h rows
 constexpr int kSeg = 4096;           // rows of one workgroup of the plan's kernels
@@ -496,62 +502,81 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
         return;
     }
 
-    // The rows' base first: it is on its way while the operands are put together.  128-byte pieces of 8 rows (64-byte
-    // pieces of 16 rows where the wave has only 64 bytes of columns).
-    constexpr int kPairs = kNw * kEs<BF16> / 128, kLoads = kPairs ? 2 : 1;
-    const int w0 = n0 + wave * kNw;
-    int row[M][kLoads];
-    u32x4 base[M][kPairs ? kPairs : 1][kLoads];
-    const int col0 = w0 + (kPairs ? pair_col() : g) * kV;
+    // Loads return in the order in which they are issued: first what the operands are made of (it comes from L2), then
+    // the rows' base (from memory), which is on its way while the operands are put together.
+    constexpr int kWVecs = kRp * (kSlice / kV) / 256, kItems = (16 * M * kRp / 4 + 255) / 256, kAhead = kItems == 1 ? 4 : kItems == 2 ? 2 : 1;
+    constexpr int kPairs = kNw * kEs<BF16> / 128, kLoads = kPairs ? 2 : 1, kQ = kPairs ? kPairs : 1;
+    int row[M][kLoads];   // 128-byte pieces of 8 rows (64-byte pieces of 16 rows where the wave has only 64 bytes of columns)
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
         for (int h = 0; h < kLoads; ++h) {
             const int i = 16 * m + (kPairs ? 8 * h + pair_row() : t);
             row[m][h] = i < tile.count ? list.row_of[tile.p0 + i] : -1;
+        }
+    u32x4 w[kWVecs];      // W's slice, zeros beyond the rank and the width
 #pragma unroll
-            for (int q = 0; q < (kPairs ? kPairs : 1); ++q) {
+    for (int k = 0; k < kWVecs; ++k) {
+        const int i = threadIdx.x + 256 * k, r = i / (kSlice / kV), c = i % (kSlice / kV) * kV;
+        const bool in = r < a.rank && n0 + c < a.width;
+        w[k] = in ? ld128(a.W + ((static_cast<int64_t>(tile.group) * a.rank + r) * a.width + n0 + c) * kEs<BF16>)
+                  : u32x4{0, 0, 0, 0};
+    }
+    f32x4 u[kItems][kAhead];   // four ranks of a row, of the first splits
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const int i = threadIdx.x + 256 * k, slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
+        const float *up = a.part + (static_cast<int64_t>(tile.p0) + slot) * kRp + r;
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c)
+            u[k][c] = slot < tile.count && c < a.splits ? *reinterpret_cast<const f32x4 *>(up + c * a.places * kRp)
+                                                        : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = kAhead; c < a.splits; ++c)
+            if (slot < tile.count) u[k][0] += *reinterpret_cast<const f32x4 *>(up + c * a.places * kRp);
+    }
+    const float s = a.scale ? a.scale[tile.group] : 1.f;
+    const int w0 = n0 + wave * kNw, col0 = w0 + (kPairs ? pair_col() : g) * kV;
+    u32x4 base[M][kQ][kLoads];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < kLoads; ++h)
+#pragma unroll
+            for (int q = 0; q < kQ; ++q) {
                 const int col = col0 + 8 * q * kV;
                 base[m][q][h] = a.base && row[m][h] >= 0 && col < a.width
                                     ? ld128_nt(a.base + (row[m][h] * a.ld_b + col) * kEs<BF16>)
                                     : u32x4{0, 0, 0, 0};
             }
-        }
 
-    // W's slice, zeros beyond the rank and the width
-    for (int i = threadIdx.x; i < kRp * (kSlice / kV); i += 256) {
-        const int r = i / (kSlice / kV), c = i % (kSlice / kV) * kV;
-        const bool in = r < a.rank && n0 + c < a.width;
-        const u32x4 w = in ? ld128(a.W + ((static_cast<int64_t>(tile.group) * a.rank + r) * a.width + n0 + c) * kEs<BF16>)
-                           : u32x4{0, 0, 0, 0};
-        *reinterpret_cast<u32x4 *>(lds_w + r * kPitch + c * kEs<BF16>) = w;
+#pragma unroll
+    for (int k = 0; k < kWVecs; ++k) {
+        const int i = threadIdx.x + 256 * k, r = i / (kSlice / kV), c = i % (kSlice / kV) * kV;
+        *reinterpret_cast<u32x4 *>(lds_w + r * kPitch + c * kEs<BF16>) = w[k];
     }
     // U: the splits' sums, scaled, as operands
-    const float s = a.scale ? a.scale[tile.group] : 1.f;
-    for (int i = threadIdx.x; i < 16 * M * kRp / 4; i += 256) {
-        const int slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const int i = threadIdx.x + 256 * k, slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
         if (slot >= tile.count) break;
-        const float *up = a.part + (static_cast<int64_t>(tile.p0) + slot) * kRp + r;
-        f32x4 u = *reinterpret_cast<const f32x4 *>(up);
-        for (int k = 1; k < a.splits; ++k) {
-            up += a.places * kRp;
-            u += *reinterpret_cast<const f32x4 *>(up);
-        }
+        f32x4 v = u[k][0];
+#pragma unroll
+        for (int c = 1; c < kAhead; ++c) v += u[k][c];
         if (a.u_out && blockIdx.x == 0) {
             float *o = a.u_out + static_cast<int64_t>(list.row_of[tile.p0 + slot]) * a.rank + r;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (r + e < a.rank) o[e] = u[e];
+                if (r + e < a.rank) o[e] = v[e];
         }
-        u *= s;
+        v *= s;
         if constexpr (BF16) {
             uint32_t *o = reinterpret_cast<uint32_t *>(lds_u + slot * kUPitch + 2 * r);
-            o[0] = pack2(u[0], u[1]);
-            o[1] = pack2(u[2], u[3]);
-            o[kRp / 2] = pack2(left_over(u[0]), left_over(u[1]));
-            o[kRp / 2 + 1] = pack2(left_over(u[2]), left_over(u[3]));
+            o[0] = pack2(v[0], v[1]);
+            o[1] = pack2(v[2], v[3]);
+            o[kRp / 2] = pack2(left_over(v[0]), left_over(v[1]));
+            o[kRp / 2 + 1] = pack2(left_over(v[2]), left_over(v[3]));
         } else {
-            *reinterpret_cast<f32x4 *>(lds_u + slot * kUPitch + 4 * r) = u;
+            *reinterpret_cast<f32x4 *>(lds_u + slot * kUPitch + 4 * r) = v;
         }
     }
     __syncthreads();
@@ -629,7 +654,7 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
             return o;
         };
 #pragma unroll
-        for (int q = 0; q < (kPairs ? kPairs : 1); ++q) {
+        for (int q = 0; q < kQ; ++q) {
             u32x4 o[2];
             if constexpr (kPairs > 0) {
                 swap8(base[m][q][0], base[m][q][1]);
@@ -648,76 +673,45 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
     }
 }
 
-// ------------------------------------------------------------------- prep --
-// Operands of k_grad for 32 places: u gathered from its rows, du summed over the
-// splits and scaled.  fp32: [place][rp] both.  bf16: [third][rp][place], and du
-// also as [place][rp] in fp32 for k_expand.
-struct PrepArgs {
-    const float *u;           // [rows][rank]
-    const float *part;        // [splits][places][rp]
-    int splits, rank, rp;
-    int64_t places;
-    const float *scale;
-    float *du;                // [places][rp]
-    float *uS;                // fp32: [places][rp]
-    bf16_bits *uT, *duT;      // bf16: [3][rp][places]
-};
-
-__global__ __launch_bounds__(256) void k_prep(TileList list, PrepArgs a) {
-    if (static_cast<int>(blockIdx.x) >= tile_count(list, false)) return;
-    const Tile tile = list.tiles[blockIdx.x];
-    __shared__ int row[32];
-    __shared__ float vals[2][32][129];   // u and du of the 32 places
-    if (threadIdx.x < 32)
-        row[threadIdx.x] = static_cast<int>(threadIdx.x) < tile.count ? list.row_of[tile.p0 + threadIdx.x] : -1;
-    __syncthreads();
-    const float s = a.scale ? a.scale[tile.group] : 1.f;
-    for (int i = threadIdx.x; i < 32 * a.rp; i += 256) {
-        const int slot = i / a.rp, r = i % a.rp;
-        const int64_t at = (static_cast<int64_t>(tile.p0) + slot) * a.rp + r;
-        float u = 0.f, du = 0.f;
-        if (row[slot] >= 0) {
-            if (r < a.rank) u = a.u[static_cast<int64_t>(row[slot]) * a.rank + r];
-            for (int k = 0; k < a.splits; ++k) du += a.part[k * a.places * a.rp + at];
-            du *= s;
-        }
-        a.du[at] = du;
-        if (a.uS) a.uS[at] = u;
-        vals[0][slot][r] = u;
-        vals[1][slot][r] = du;
-    }
-    if (!a.uT) return;
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.rp * 4; i += 256) {   // (matrix, rank, eight places)
-        const int oct = i & 3, r = (i >> 2) % a.rp, which = (i >> 2) / a.rp;
-        bf16_bits *out = (which ? a.duT : a.uT) + r * a.places + tile.p0 + 8 * oct;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = vals[which][8 * oct + e][r];
-#pragma unroll
-        for (int third = 0; third < 3; ++third) {
-            u32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
-            *reinterpret_cast<u32x4 *>(out + third * a.rp * a.places) = w;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = left_over(v[e]);
-        }
+// ------------------------------------------------------------------- join --
+// du[place][rp] = s_a times the sum of the splits' parts.
+__global__ __launch_bounds__(256) void k_join(TileList list, const float *part, int splits, int64_t places, int rp,
+                                              const float *scale, float *du) {
+    const int at = tile_index();
+    if (at >= tile_count(list, false)) return;
+    const Tile tile = list.tiles[at];
+    const float s = scale ? scale[tile.group] : 1.f;
+    for (int i = threadIdx.x * 4; i < tile.count * rp; i += 1024) {
+        const int64_t p = static_cast<int64_t>(tile.p0) * rp + i;
+        f32x4 v = *reinterpret_cast<const f32x4 *>(part + p);
+        for (int k = 1; k < splits; ++k) v += *reinterpret_cast<const f32x4 *>(part + k * places * rp + p);
+        *reinterpret_cast<f32x4 *>(du + p) = v * s;
     }
 }
 
 // ------------------------------------------------------------------- grad --
+// The blocks of 32 places (the tile list of 32 rows) are shared evenly among the
+// workgroups of a column slice: run i of n has the blocks from T i / n on.  A run
+// may pass from one adapter to the next; each (run, adapter) pair that meets is a
+// part of the adapter's sum.  Runs and adapters both only increase, so run +
+// adapter numbers the parts, an adapter's parts one after the other.
+__device__ __forceinline__ int run_begin(int64_t blocks, int i, int n) { return static_cast<int>(blocks * i / n); }
+__device__ __forceinline__ int run_of(int64_t blocks, int j, int n) {
+    return static_cast<int>(((j + int64_t{1}) * n - 1) / blocks);
+}
+
 struct GradJob {
     const char *v;            // rows x or dy
     int64_t ld;
     int width, slices;
-    const void *U;            // bf16: [3][rp][places]; fp32: [places][rp]
-    float *part;              // [tiles][rp][width]
+    const float *U;           // by_row: u [rows][rank]; else du [places][rp]
+    int by_row;
+    float *part;              // [runs + n][rp][width]
     uint32_t thr;             // dropout of v
 };
 struct GradArgs {
     GradJob job[2];
-    int64_t places;
+    int rank;
 };
 
 constexpr int kGradCols = 256;
@@ -726,94 +720,150 @@ template <bool BF16, int RT>
 __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArgs d) {
     constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kGradCols * kEs<BF16> + 32;
     constexpr int kLoads = 32 * (kGradCols / kV) / 256;      // 16-byte loads of a thread for 32 rows
-    constexpr int kRowsPer = 32 / kLoads;                     // rows that the workgroup loads at once
+    constexpr int kRowsPer = 32 / kLoads;                    // rows that the workgroup loads at once
+    // U of 32 places.  bf16: [third][rank][place]; fp32: [place][rank]
+    constexpr int kUPitch = BF16 ? 80 : 4 * kRp + 16, kUThird = kRp * kUPitch;
+    constexpr int kChunk = 32;                               // blocks whose rows are looked up together
     __shared__ __align__(16) char lds_v[32 * kPitch];
-    __shared__ int lds_row[512];
-    const int at = tile_index();
-    if (at >= tile_count(list, false)) return;
-    const Tile tile = list.tiles[at];
+    __shared__ __align__(16) char lds_u[BF16 ? 3 * kUThird : 32 * kUPitch];
+    __shared__ int lds_row[kChunk * 32];
+    __shared__ Tile lds_tile[kChunk];
+    const int64_t blocks = tile_count(list, false);
     const int which = static_cast<int>(blockIdx.x) >= a.job[0].slices;
     const GradJob job = which ? a.job[1] : a.job[0];
     const int n0 = (blockIdx.x - (which ? a.job[0].slices : 0)) * kGradCols;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
-    const int steps = (tile.count + 31) / 32;
-    for (int i = threadIdx.x; i < 32 * steps; i += 256) lds_row[i] = i < tile.count ? list.row_of[tile.p0 + i] : -1;
-    __syncthreads();
+    const int end = run_begin(blocks, blockIdx.y + 1, gridDim.y);
 
     const int lr = threadIdx.x / (kGradCols / kV), lc = threadIdx.x % (kGradCols / kV) * kV;
     const bool in = n0 + lc < job.width;
+    const int ur = threadIdx.x & 15, up = threadIdx.x >> 4;   // rank within 16 and pair of places that the thread loads
+    float u[RT][2];
     u32x4 v[kLoads];
-    const auto load = [&](int step) {
+    const auto load = [&](int i) {   // U first: it comes from L2, and loads return in order
+        const int p0 = lds_tile[i].p0;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int row = lds_row[32 * step + kRowsPer * i + lr];
-            v[i] = in && row >= 0 ? ld128_nt(job.v + (row * job.ld + n0 + lc) * kEs<BF16>) : u32x4{0, 0, 0, 0};
+        for (int e = 0; e < 2; ++e) {
+            const int row = lds_row[32 * i + 2 * up + e];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const int k = 16 * r + ur;
+                u[r][e] = row >= 0 && k < a.rank
+                              ? job.U[job.by_row ? static_cast<int64_t>(row) * a.rank + k
+                                                 : (static_cast<int64_t>(p0) + 2 * up + e) * kRp + k]
+                              : 0.f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int row = lds_row[32 * i + kRowsPer * k + lr];
+            v[k] = in && row >= 0 ? ld128_nt(job.v + (row * job.ld + n0 + lc) * kEs<BF16>) : u32x4{0, 0, 0, 0};
         }
     };
     f32x4 acc[4][RT];
+    const auto clear = [&] {
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) acc[b][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    load(0);
-    for (int step = 0; step < steps; ++step) {
-        if (step) __syncthreads();   // the waves are done with the rows before
+            for (int r = 0; r < RT; ++r) acc[b][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    // lane holds columns 4 g .. + 3 of block b for rank 16 r + t
+    const auto flush = [&](int group) {
+        float *out = job.part + (static_cast<int64_t>(blockIdx.y) + group) * kRp * job.width;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int slot = kRowsPer * i + lr;
-            if (job.thr) v[i] = drop_piece<BF16>(d, v[i], static_cast<uint32_t>(lds_row[32 * step + slot]), n0 + lc);
-            *reinterpret_cast<u32x4 *>(lds_v + slot * kPitch + lc * kEs<BF16>) = v[i];
+        for (int b = 0; b < 4; ++b) {
+            const int col = n0 + wave * 64 + 16 * b + 4 * g;
+            if (col >= job.width) continue;
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+                *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(16 * r + t) * job.width + col) = acc[b][r];
+        }
+    };
+    clear();
+    int group = -1;
+    for (int chunk = run_begin(blocks, blockIdx.y, gridDim.y); chunk < end; chunk += kChunk) {
+        const int count = end - chunk < kChunk ? end - chunk : kChunk;
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) < count) lds_tile[threadIdx.x] = list.tiles[chunk + threadIdx.x];
+        __syncthreads();
+        for (int i = threadIdx.x; i < count * 32; i += 256) {
+            const Tile tile = lds_tile[i / 32];
+            lds_row[i] = i % 32 < tile.count ? list.row_of[tile.p0 + i % 32] : -1;
         }
         __syncthreads();
-        if (step + 1 < steps) load(step + 1);
-        const int64_t p = static_cast<int64_t>(tile.p0) + 32 * step;
-        if constexpr (BF16) {
-            const bf16_bits *U = static_cast<const bf16_bits *>(job.U) + p + 8 * g;
-            u32x4 vf[4];
-            const uint32_t l0 = lds_addr(lds_v) + static_cast<uint32_t>((8 * g + (t >> 2)) * kPitch + (wave * 64 + 4 * (t & 3)) * 2);
+        load(0);
+        for (int i = 0; i < count; ++i) {
+            if (lds_tile[i].group != group) {
+                if (group >= 0) {
+                    flush(group);
+                    clear();
+                }
+                group = lds_tile[i].group;
+            }
+            if (i) __syncthreads();   // the waves are done with the block before
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const s16x4 v8[2] = {read_tr(l0 + 32 * b), read_tr(l0 + 32 * b + 4 * kPitch)};
-                vf[b] = __builtin_bit_cast(u32x4, v8);
+            for (int r = 0; r < RT; ++r) {
+                if constexpr (BF16) {
+                    float lo = u[r][0], hi = u[r][1];
+#pragma unroll
+                    for (int third = 0; third < 3; ++third) {
+                        *reinterpret_cast<uint32_t *>(lds_u + third * kUThird + (16 * r + ur) * kUPitch + 4 * up) = pack2(lo, hi);
+                        lo = left_over(lo);
+                        hi = left_over(hi);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        *reinterpret_cast<float *>(lds_u + (2 * up + e) * kUPitch + (16 * r + ur) * 4) = u[r][e];
+                }
             }
 #pragma unroll
-            for (int third = 0; third < 3; ++third)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const u32x4 uf = ld128(U + (static_cast<int64_t>(third) * kRp + 16 * r + t) * a.places);
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) acc[b][r] = mfma16_bf16(as_bf16x8(vf[b]), as_bf16x8(uf), acc[b][r]);
-                }
-        } else {
-            const float *U = static_cast<const float *>(job.U) + p * kRp + t;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                float uf[RT];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) uf[r] = U[(4 * k + g) * kRp + 16 * r];
+            for (int k = 0; k < kLoads; ++k) {
+                const int slot = kRowsPer * k + lr;
+                if (job.thr) v[k] = drop_piece<BF16>(d, v[k], static_cast<uint32_t>(lds_row[32 * i + slot]), n0 + lc);
+                *reinterpret_cast<u32x4 *>(lds_v + slot * kPitch + lc * kEs<BF16>) = v[k];
+            }
+            __syncthreads();
+            if (i + 1 < count) load(i + 1);
+            if constexpr (BF16) {
+                u32x4 vf[4];
+                const uint32_t l0 = lds_addr(lds_v) + static_cast<uint32_t>((8 * g + (t >> 2)) * kPitch + (wave * 64 + 4 * (t & 3)) * 2);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const float vf = *reinterpret_cast<const float *>(lds_v + (4 * k + g) * kPitch + (wave * 64 + 16 * b + t) * 4);
+                    const s16x4 v8[2] = {read_tr(l0 + 32 * b), read_tr(l0 + 32 * b + 4 * kPitch)};
+                    vf[b] = __builtin_bit_cast(u32x4, v8);
+                }
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) acc[b][r] = mfma16_f32(vf, uf[r], acc[b][r]);
+                for (int third = 0; third < 3; ++third)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        const u32x4 uf =
+                            *reinterpret_cast<const u32x4 *>(lds_u + third * kUThird + (16 * r + t) * kUPitch + 16 * g);
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) acc[b][r] = mfma16_bf16(as_bf16x8(vf[b]), as_bf16x8(uf), acc[b][r]);
+                    }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    float uf[RT];
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        uf[r] = *reinterpret_cast<const float *>(lds_u + (4 * k + g) * kUPitch + (16 * r + t) * 4);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const float vf = *reinterpret_cast<const float *>(lds_v + (4 * k + g) * kPitch + (wave * 64 + 16 * b + t) * 4);
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) acc[b][r] = mfma16_f32(vf, uf[r], acc[b][r]);
+                    }
                 }
             }
         }
     }
-    // lane holds columns 4 g .. + 3 of block b for rank 16 r + t
-    float *out = job.part + static_cast<int64_t>(at) * kRp * job.width;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const int col = n0 + wave * 64 + 16 * b + 4 * g;
-        if (col >= job.width) continue;
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-            *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(16 * r + t) * job.width + col) = acc[b][r];
-    }
+    if (group >= 0) flush(group);
 }
 
 struct ReduceJob {
-    const float *part;        // [tiles][rp][width]
+    const float *part;        // [runs + n][rp][width]
     float *dW;                // [n][rank][width]
     const float *scale;       // [n] or null
     float f;
@@ -822,11 +872,11 @@ struct ReduceJob {
 struct ReduceArgs {
     ReduceJob job[2];
     const PlanHead *head;
-    const int *first;
-    int rows, n, rank, rp, accumulate;
+    const int *first;         // first block of 32 places of each group
+    int rows, n, rank, rp, runs, accumulate;
 };
 
-// dW_a[r] (+)= f s_a times the sum of its tiles' parts, in their order; zeros
+// dW_a[r] (+)= f s_a times the sum of the adapter's parts, in their order; zeros
 // for an adapter without rows.
 __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
     if (!is_plan(a.head, a.rows, a.n)) return;
@@ -835,12 +885,14 @@ __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
     const int col = ((blockIdx.y - (which ? a.job[0].slices : 0)) * 256 + threadIdx.x) * 4;
     if (col >= job.width) return;
     const int ad = blockIdx.x / a.rank, r = blockIdx.x % a.rank;
-    const int t0 = a.first[ad], t1 = a.first[ad + 1];
-    const float *p = job.part + (static_cast<int64_t>(t0) * a.rp + r) * job.width + col;
+    const int j0 = a.first[ad], j1 = a.first[ad + 1], blocks = a.first[a.n];
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int t = t0; t < t1; ++t) {
-        s += *reinterpret_cast<const f32x4 *>(p);
-        p += static_cast<int64_t>(a.rp) * job.width;
+    if (j1 > j0) {
+        const int i0 = run_of(blocks, j0, a.runs), i1 = run_of(blocks, j1 - 1, a.runs);
+        const float *p = job.part + (static_cast<int64_t>(i0 + ad) * a.rp + r) * job.width + col;
+        const int64_t step = static_cast<int64_t>(a.rp) * job.width;
+        for (int i = i0; i <= i1; ++i, p += step)   // (where runs outnumber blocks, some have none)
+            if (run_begin(blocks, i, a.runs) < run_begin(blocks, i + 1, a.runs)) s += *reinterpret_cast<const f32x4 *>(p);
     }
     s *= job.f * (job.scale ? job.scale[ad] : 1.f);
     float *out = job.dW + static_cast<int64_t>(blockIdx.x) * job.width + col;
@@ -860,7 +912,8 @@ int rank_tiles(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ?
 struct Shape {
     int rt, rp;
     int64_t places;
-    int h_shrink, h_grad;         // list heights
+    int h_shrink;                 // list height
+    int runs;                     // of k_grad
 };
 
 // Rows per tile: 16 where an adapter has few rows on average (decoding), else as
@@ -872,10 +925,11 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     s.places = plan_places(rows, n);
     const bool few = rows < static_cast<int64_t>(32) * n || rows <= 32;
     s.h_shrink = few ? 0 : (s.rt == 2 || s.rt == 4) ? 2 : 1;
-    // chunks of the gradient: long ones leave few partial sums, short ones give every CU two workgroups
+    // runs of k_grad: two workgroups for each CU, a run of two blocks at least
     const int64_t slices = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
-    s.h_grad = 5;
-    while (s.h_grad > 1 && (rows >> (4 + s.h_grad)) * slices < 512) --s.h_grad;
+    const int64_t most = (plan_max_tiles(rows, n, 1) + 1) / 2;
+    int64_t runs = GRUNS / slices;
+    s.runs = static_cast<int>(runs < 1 ? 1 : runs > most ? most : runs);
     return s;
 }
 
@@ -892,7 +946,7 @@ int shrink_splits(const Shape &s, int64_t rows, int n, int width, int *per) {
 }
 
 struct WsLayout {
-    size_t part, du, u_op, du_op, part_a, part_b, bytes;
+    size_t part, du, part_a, part_b, bytes;
 };
 WsLayout ws_layout(const Shape &s, int64_t rows, int n_in, int n_out, int n) {
     WsLayout l;
@@ -905,13 +959,11 @@ WsLayout ws_layout(const Shape &s, int64_t rows, int n_in, int n_out, int n) {
     int per;
     const int sf = shrink_splits(s, rows, n, n_in, &per), sb = shrink_splits(s, rows, n, n_out, &per);
     const size_t u = static_cast<size_t>(s.places) * s.rp;
-    const size_t tiles = static_cast<size_t>(plan_max_tiles(rows, n, s.h_grad));
+    const size_t parts = static_cast<size_t>(s.runs) + n;
     l.part = take(u * 4 * (sf > sb ? sf : sb));
     l.du = take(u * 4);
-    l.u_op = take(u * 6);
-    l.du_op = take(u * 6);
-    l.part_a = take(tiles * s.rp * n_in * 4);
-    l.part_b = take(tiles * s.rp * n_out * 4);
+    l.part_a = take(parts * s.rp * n_in * 4);
+    l.part_b = take(parts * s.rp * n_out * 4);
     l.bytes = at;
     return l;
 }
@@ -947,7 +999,7 @@ void run_expand(const Shape &s, const PlanView &pv, const ExpandArgs &a, const D
         constexpr int RT = decltype(rt)::value, kSlice = 4 * kCols<BF16, RT>;
         // the tallest tiles that leave two workgroups for each CU (64 rows, 32 at rank 128, whose operands fill LDS)
         const int64_t slices = (a.width + kSlice - 1) / kSlice;
-        int h = RT == 8 ? 1 : 2;
+        int h = RT == 8 ? 1 : EXP_H;
         while (h > 0 && (static_cast<int64_t>(pv.rows) >> (4 + h)) * slices < 512) --h;
         const TileList list = tile_list(pv, h);
         const dim3 grid = tile_grid(slices, plan_max_tiles(pv.rows, pv.n, h));
@@ -1026,37 +1078,24 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
     const auto go = [&](auto b) {
         constexpr bool BF16 = decltype(b)::value;
         run_shrink<BF16, false>(s, pv, dy, ld_dy, m.n_out, B, m.rank, part, splits, per, d, st);
-        PrepArgs p = {};
-        p.u = u;
-        p.part = part;
-        p.splits = splits;
-        p.rank = m.rank;
-        p.rp = s.rp;
-        p.places = s.places;
-        p.scale = scale;
-        p.du = du;
-        if (BF16) {
-            p.uT = reinterpret_cast<bf16_bits *>(w + l.u_op);
-            p.duT = reinterpret_cast<bf16_bits *>(w + l.du_op);
-        } else {
-            p.uS = reinterpret_cast<float *>(w + l.u_op);
-        }
-        k_prep<<<static_cast<unsigned>(plan_max_tiles(m.rows, m.n, 1)), 256, 0, st>>>(tile_list(pv, 1), p);
+        k_join<<<tile_grid(1, plan_max_tiles(m.rows, m.n, 2)), 256, 0, st>>>(tile_list(pv, 2), part, splits, s.places, s.rp,
+                                                                            scale, du);
         GradArgs ga = {};
-        ga.places = s.places;
-        ga.job[0] = {static_cast<const char *>(dy), ld_dy, m.n_out, (m.n_out + kGradCols - 1) / kGradCols, w + l.u_op,
+        ga.rank = m.rank;
+        ga.job[0] = {static_cast<const char *>(dy), ld_dy, m.n_out, (m.n_out + kGradCols - 1) / kGradCols, u, 1,
                      reinterpret_cast<float *>(w + l.part_b), 0};
-        ga.job[1] = {static_cast<const char *>(x), ld_x, m.n_in, (m.n_in + kGradCols - 1) / kGradCols,
-                     BF16 ? static_cast<const void *>(w + l.du_op) : du, reinterpret_cast<float *>(w + l.part_a), d.thr};
-        const dim3 grid = tile_grid(ga.job[0].slices + ga.job[1].slices, plan_max_tiles(m.rows, m.n, s.h_grad));
+        ga.job[1] = {static_cast<const char *>(x), ld_x, m.n_in, (m.n_in + kGradCols - 1) / kGradCols, du, 0,
+                     reinterpret_cast<float *>(w + l.part_a), d.thr};
+        const dim3 grid(static_cast<unsigned>(ga.job[0].slices + ga.job[1].slices), static_cast<unsigned>(s.runs));
         with_rank<BF16, false>(s.rt, [&](auto rt) {
-            k_grad<BF16, decltype(rt)::value><<<grid, 256, 0, st>>>(tile_list(pv, s.h_grad), ga, d);
+            k_grad<BF16, decltype(rt)::value><<<grid, 256, 0, st>>>(tile_list(pv, 1), ga, d);
         });
         ReduceArgs r = {};
         r.job[0] = {ga.job[0].part, dB, scale, 1.f, m.n_out, (m.n_out + 1023) / 1024};
         r.job[1] = {ga.job[1].part, dA, nullptr, d.scale, m.n_in, (m.n_in + 1023) / 1024};
         r.head = pv.head;
-        r.first = pv.first[s.h_grad];
+        r.first = pv.first[1];
+        r.runs = s.runs;
         r.rows = pv.rows;
         r.n = m.n;
         r.rank = m.rank;
