@@ -44,15 +44,6 @@
 namespace logra {
 namespace {
 
-#ifndef SPLIT_TARGET
-#define SPLIT_TARGET 2048
-#endif
-#ifndef GRUNS
-#define GRUNS 1024
-#endif
-#ifndef EXP_H
-#define EXP_H 2
-#endif
 constexpr int kHeights = 6;          // tile lists of 16 << h rows
 constexpr int kSeg = 4096;           // rows of one workgroup of the plan's kernels
 constexpr int kPlanMagic = 0x4c6f4164;
@@ -694,11 +685,11 @@ __global__ __launch_bounds__(256) void k_join(TileList list, const float *part, 
 // workgroups of a column slice: run i of n has the blocks from T i / n on.  A run
 // may pass from one adapter to the next; each (run, adapter) pair that meets is a
 // part of the adapter's sum.  Runs and adapters both only increase, so run +
-// adapter numbers the parts, an adapter's parts one after the other.
-__device__ __forceinline__ int run_begin(int64_t blocks, int i, int n) { return static_cast<int>(blocks * i / n); }
-__device__ __forceinline__ int run_of(int64_t blocks, int j, int n) {
-    return static_cast<int>(((j + int64_t{1}) * n - 1) / blocks);
-}
+// adapter numbers the parts, an adapter's parts one after the other.  No run is
+// empty: there are at most as many as blocks.
+constexpr uint32_t kMaxRuns = 1024;   // with the 2^19 + 1023 blocks at most, products fit 32 bits
+__device__ __forceinline__ uint32_t run_begin(uint32_t blocks, uint32_t i, uint32_t n) { return blocks * i / n; }
+__device__ __forceinline__ uint32_t run_of(uint32_t blocks, uint32_t j, uint32_t n) { return ((j + 1) * n - 1) / blocks; }
 
 struct GradJob {
     const char *v;            // rows x or dy
@@ -728,12 +719,13 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
     __shared__ __align__(16) char lds_u[BF16 ? 3 * kUThird : 32 * kUPitch];
     __shared__ int lds_row[kChunk * 32];
     __shared__ Tile lds_tile[kChunk];
-    const int64_t blocks = tile_count(list, false);
+    const uint32_t blocks = tile_count(list, false), runs = blocks < gridDim.y ? blocks : gridDim.y;
+    if (blockIdx.y >= runs) return;
     const int which = static_cast<int>(blockIdx.x) >= a.job[0].slices;
     const GradJob job = which ? a.job[1] : a.job[0];
     const int n0 = (blockIdx.x - (which ? a.job[0].slices : 0)) * kGradCols;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
-    const int end = run_begin(blocks, blockIdx.y + 1, gridDim.y);
+    const int end = run_begin(blocks, blockIdx.y + 1, runs);
 
     const int lr = threadIdx.x / (kGradCols / kV), lc = threadIdx.x % (kGradCols / kV) * kV;
     const bool in = n0 + lc < job.width;
@@ -781,7 +773,7 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
     };
     clear();
     int group = -1;
-    for (int chunk = run_begin(blocks, blockIdx.y, gridDim.y); chunk < end; chunk += kChunk) {
+    for (int chunk = run_begin(blocks, blockIdx.y, runs); chunk < end; chunk += kChunk) {
         const int count = end - chunk < kChunk ? end - chunk : kChunk;
         __syncthreads();
         if (static_cast<int>(threadIdx.x) < count) lds_tile[threadIdx.x] = list.tiles[chunk + threadIdx.x];
@@ -885,14 +877,21 @@ __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
     const int col = ((blockIdx.y - (which ? a.job[0].slices : 0)) * 256 + threadIdx.x) * 4;
     if (col >= job.width) return;
     const int ad = blockIdx.x / a.rank, r = blockIdx.x % a.rank;
-    const int j0 = a.first[ad], j1 = a.first[ad + 1], blocks = a.first[a.n];
+    const uint32_t j0 = a.first[ad], j1 = a.first[ad + 1], blocks = a.first[a.n];
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (j1 > j0) {
-        const int i0 = run_of(blocks, j0, a.runs), i1 = run_of(blocks, j1 - 1, a.runs);
+        const uint32_t runs = blocks < static_cast<uint32_t>(a.runs) ? blocks : a.runs;
+        const int i0 = run_of(blocks, j0, runs), i1 = run_of(blocks, j1 - 1, runs);
         const float *p = job.part + (static_cast<int64_t>(i0 + ad) * a.rp + r) * job.width + col;
         const int64_t step = static_cast<int64_t>(a.rp) * job.width;
-        for (int i = i0; i <= i1; ++i, p += step)   // (where runs outnumber blocks, some have none)
-            if (run_begin(blocks, i, a.runs) < run_begin(blocks, i + 1, a.runs)) s += *reinterpret_cast<const f32x4 *>(p);
+        for (int i = i0; i <= i1; i += 8) {   // eight loads on their way, added in order
+            f32x4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = i + k <= i1 ? *reinterpret_cast<const f32x4 *>(p + k * step) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+            p += 8 * step;
+        }
     }
     s *= job.f * (job.scale ? job.scale[ad] : 1.f);
     float *out = job.dW + static_cast<int64_t>(blockIdx.x) * job.width + col;
@@ -925,10 +924,11 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     s.places = plan_places(rows, n);
     const bool few = rows < static_cast<int64_t>(32) * n || rows <= 32;
     s.h_shrink = few ? 0 : (s.rt == 2 || s.rt == 4) ? 2 : 1;
-    // runs of k_grad: two workgroups for each CU, a run of two blocks at least
+    // runs of k_grad: four workgroups for each CU (all resident; two took 68 us, four 52 for 16,384 rows of 4096 +
+    // 4096 columns at rank 16, and with six the parts cost more than the occupancy gains)
     const int64_t slices = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
-    const int64_t most = (plan_max_tiles(rows, n, 1) + 1) / 2;
-    int64_t runs = GRUNS / slices;
+    const int64_t most = plan_max_tiles(rows, n, 1);
+    int64_t runs = 1024 / slices;
     s.runs = static_cast<int>(runs < 1 ? 1 : runs > most ? most : runs);
     return s;
 }
@@ -936,7 +936,7 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
 // Ranges of the long axis in k_shrink: enough workgroups for two on each CU.
 int shrink_splits(const Shape &s, int64_t rows, int n, int width, int *per) {
     const int64_t tiles = (rows >> (4 + s.h_shrink)) + (n < rows ? n : rows);
-    int64_t want = (SPLIT_TARGET + tiles - 1) / tiles;
+    int64_t want = (2048 + tiles - 1) / tiles;
     const int64_t most = (width + 511) / 512;
     if (want > most) want = most;
     if (want > 8) want = 8;
@@ -999,7 +999,7 @@ void run_expand(const Shape &s, const PlanView &pv, const ExpandArgs &a, const D
         constexpr int RT = decltype(rt)::value, kSlice = 4 * kCols<BF16, RT>;
         // the tallest tiles that leave two workgroups for each CU (64 rows, 32 at rank 128, whose operands fill LDS)
         const int64_t slices = (a.width + kSlice - 1) / kSlice;
-        int h = RT == 8 ? 1 : EXP_H;
+        int h = RT == 8 ? 1 : 2;
         while (h > 0 && (static_cast<int64_t>(pv.rows) >> (4 + h)) * slices < 512) --h;
         const TileList list = tile_list(pv, h);
         const dim3 grid = tile_grid(slices, plan_max_tiles(pv.rows, pv.n, h));
