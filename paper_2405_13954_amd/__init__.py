@@ -182,7 +182,11 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        return ctypes.c_void_p(_torch().cuda.current_stream().cuda_stream)
+        torch = _torch()
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # what current_stream() wraps in 2.6 us of Python
+        if raw is not None:
+            return ctypes.c_void_p(raw(torch.cuda.current_device()))
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
