@@ -927,7 +927,9 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     // runs of k_grad: four workgroups for each CU (all resident; two took 68 us, four 52 for 16,384 rows of 4096 +
     // 4096 columns at rank 16, and with six the parts cost more than the occupancy gains)
     const int64_t slices = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
-    const int64_t most = plan_max_tiles(rows, n, 1);
+    // a part costs what rank / 16 blocks do: runs of at least 1.5 times that many (2,047 rows at rank 64: runs of one
+    // block took 21 us and their sum 12, runs of six 17 and 6)
+    const int64_t least = s.rt == 1 ? 1 : s.rt * 3 / 2, most = (plan_max_tiles(rows, n, 1) + least - 1) / least;
     int64_t runs = 1024 / slices;
     s.runs = static_cast<int>(runs < 1 ? 1 : runs > most ? most : runs);
     return s;
