@@ -2,12 +2,11 @@
 //
 //     loss_t = w_t (lse(z_t) - z_t[target_t]),   dz_t = w_t (softmax(z_t) - onehot(target_t))
 //
-// One workgroup per token.  The token's logits are read once and stay packed in
-// registers (NV 16-byte vectors a thread) through the three passes over them:
-// the maximum, the sum of exp(z - max), and the gradient, so memory sees one
-// read and one write of the vocabulary, which is what bounds it.  Vocabularies
-// beyond the registers of 1024 threads are read a second time for the gradient,
-// maximum and sum being kept as a running pair in the first pass.
+// One workgroup per token.  A thread keeps NV of its 16-byte vectors of the
+// vocabulary packed in registers; the others go by once for the statistics and once more, out of the cache, for the gradient.  So
+// memory sees one read of the logits and one write of the gradient, which is what
+// bounds it.  The statistics are one pass: a running maximum and the sum of
+// exp(z - max), brought to a new maximum once per four vectors.
 // Maximum, sum and gradient are fp32; z - max is formed before the product with
 // log2(e), so that the likely tokens keep their full precision.
 #include "common.h"
@@ -101,13 +100,13 @@ __device__ __forceinline__ float row_loss(float top, float total, float w, float
     return total == 0.f ? __builtin_inff() : w * (logf(total) + (top - zt));
 }
 
-// NV = 0: the vocabulary does not stay in registers.
-template <bool BF16, int TH, int NV>
-__global__ __launch_bounds__(TH) void k_token_loss(const char *logits, int64_t ld, int64_t rows, int vocab,
+// MINW: waves on a SIMD that the registers leave room for.
+template <bool BF16, int TH, int NV, int MINW>
+__global__ __launch_bounds__(TH, MINW) void k_token_loss(const char *logits, int64_t ld, int64_t rows, int vocab,
                                                    const int64_t *target, const float *weight, float *loss,
                                                    char *dlogits, int64_t ld_d) {
     using V = Vec<BF16>;
-    constexpr int kEs = BF16 ? 2 : 4;
+    constexpr int kEs = BF16 ? 2 : 4, kGroup = 4;
     constexpr float kNone = -__builtin_inff();
     __shared__ float red[TH / 64];
     const int64_t row = blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y;
@@ -133,7 +132,6 @@ __global__ __launch_bounds__(TH) void k_token_loss(const char *logits, int64_t l
         zt = reinterpret_cast<const float *>(z)[t];
     const int n_full = vocab / V::kN, odd = vocab - n_full * V::kN;   // whole vectors; logits of the last, partial one
     const bool tail = odd > 0 && tid == n_full % TH;                  // the thread that has it
-    const char *zk = z + static_cast<int64_t>(tid) * 16;
     const auto maximum = [&](u32x4 v, float m) {
 #pragma unroll
         for (int e = 0; e < V::kN; ++e) m = fmaxf(m, V::get(v, e));
@@ -145,67 +143,73 @@ __global__ __launch_bounds__(TH) void k_token_loss(const char *logits, int64_t l
         for (int e = 0; e < V::kN; ++e) q += exp_from(V::get(v, e), m);
         return q;
     };
-    const auto gradient = [&](u32x4 v, int i, float m, float f, float hot) {
-        float g[V::kN];
-        const int hit = static_cast<int>(t) - i * V::kN;
+    // the packed logits are what is kept between the uses of a vector, not their fp32 values or exponentials, which the
+    // compiler would otherwise carry over at two registers for each one
+    const auto again = [](u32x4 &v) { asm volatile("" : "+v"(v)); };
+    const auto load = [&](int i) { return i < n_full ? ld128(z + static_cast<int64_t>(i) * 16) : V::none(); };
+    float top = kNone, total = 0.f;   // of the thread's own vectors, a running pair
+    const auto take = [&](u32x4 (&v)[kGroup]) {
+        float m = top;
 #pragma unroll
-        for (int e = 0; e < V::kN; ++e) {
-            g[e] = exp_from(V::get(v, e), m) * f;
-            if (e == hit) g[e] -= hot;
+        for (int j = 0; j < kGroup; ++j) m = maximum(v[j], m);
+        const float base = m == kNone ? 0.f : m;
+        total *= exp_from(top, base);
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            again(v[j]);
+            total += sum(v[j], base);
+        }
+        top = m;
+    };
+    u32x4 keep[NV / kGroup][kGroup];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) keep[k / kGroup][k % kGroup] = load(k * TH + tid);
+    u32x4 last = V::none();
+    if (tail) last = V::load(z + static_cast<int64_t>(n_full) * 16, odd);
+    for (int i = NV * TH + tid; i < n_full; i += kGroup * TH) {
+        u32x4 v[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) v[j] = load(i + j * TH);
+        take(v);
+    }
+#pragma unroll
+    for (int k = 0; k < NV / kGroup; ++k) take(keep[k]);
+    {
+        u32x4 v[kGroup] = {last, V::none(), V::none(), V::none()};
+        if (tail) take(v);
+    }
+    const float mine = top;
+    top = group_reduce<TH, true>(mine, red);
+    if (top == kNone) top = 0.f;
+    total = group_reduce<TH, false>(total * exp_from(mine, top), red);
+    if (tid == 0) loss[row] = row_loss(top, total, w, zt);
+    if (!dz) return;
+    const float f = total == 0.f ? 0.f : w / total, hot = total == 0.f ? 0.f : w;
+    const auto gradient = [&](u32x4 v, int i) {
+        float g[V::kN];
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) g[e] = exp_from(V::get(v, e), top) * f;
+        const int hit = static_cast<int>(t) - i * V::kN;
+        if (hit >= 0 && hit < V::kN) {   // one vector of the whole token
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) g[e] -= e == hit ? hot : 0.f;
         }
         V::store(dz + static_cast<int64_t>(i) * 16, g, vocab - i * V::kN);
     };
-    u32x4 last = V::none();
-    if (tail) last = V::load(z + static_cast<int64_t>(n_full) * 16, odd);
-    float top = maximum(last, kNone), total = 0.f;
-    if constexpr (NV > 0) {
-        u32x4 v[NV];
-        // between the passes: the packed logits are what is kept, not their fp32 values or exponentials, which
-        // the compiler would otherwise carry over at two registers for each one
-        const auto again = [&](u32x4 (&x)[NV]) {
-            asm volatile("" : "+v"(top));
-            if constexpr (BF16) {
 #pragma unroll
-                for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(x[k]));
-            }
-        };
-#pragma unroll
-        for (int k = 0; k < NV; ++k) v[k] = k * TH + tid < n_full ? ld128_nt(zk + static_cast<int64_t>(k) * TH * 16) : V::none();
-#pragma unroll
-        for (int k = 0; k < NV; ++k) top = maximum(v[k], top);
-        top = group_reduce<TH, true>(top, red);
-        if (top == kNone) top = 0.f;
-        again(v);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) total += sum(v[k], top);
-        total = group_reduce<TH, false>(total + sum(last, top), red);
-        if (tid == 0) loss[row] = row_loss(top, total, w, zt);
-        if (!dz) return;
-        const float f = total == 0.f ? 0.f : w / total, hot = total == 0.f ? 0.f : w;
-        again(v);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k * TH + tid < n_full) gradient(v[k], k * TH + tid, top, f, hot);
-        if (tail) gradient(last, n_full, top, f, hot);
-    } else {
-        // each thread keeps the running maximum and sum of its own vectors
-        float mine = top;
-        total = mine == kNone ? 0.f : sum(last, mine);
-        for (int i = tid; i < n_full; i += TH) {
-            const u32x4 v = ld128(z + static_cast<int64_t>(i) * 16);
-            const float m = maximum(v, mine), base = m == kNone ? 0.f : m;
-            total = total * exp_from(mine, base) + sum(v, base);
-            mine = m;
-        }
-        top = group_reduce<TH, true>(mine, red);
-        if (top == kNone) top = 0.f;
-        total = group_reduce<TH, false>(total * exp_from(mine, top), red);
-        if (tid == 0) loss[row] = row_loss(top, total, w, zt);
-        if (!dz) return;
-        const float f = total == 0.f ? 0.f : w / total, hot = total == 0.f ? 0.f : w;
-        for (int i = tid; i < n_full; i += TH) gradient(ld128(z + static_cast<int64_t>(i) * 16), i, top, f, hot);
-        if (tail) gradient(last, n_full, top, f, hot);
+    for (int k = 0; k < NV; ++k) {
+        again(keep[k / kGroup][k % kGroup]);
+        if (k * TH + tid < n_full) gradient(keep[k / kGroup][k % kGroup], k * TH + tid);
     }
+    for (int i = NV * TH + tid; i < n_full; i += kGroup * TH) {
+        u32x4 v[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) v[j] = i + j * TH < n_full ? ld128_nt(z + static_cast<int64_t>(i + j * TH) * 16) : V::none();
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j)
+            if (i + j * TH < n_full) gradient(v[j], i + j * TH);
+    }
+    if (tail) gradient(last, n_full);
 }
 
 }  // namespace
@@ -221,12 +225,14 @@ hipError_t launch_token_loss(const void *logits, int64_t ld, bool bf16, int64_t 
     const int64_t vec = (static_cast<int64_t>(vocab) + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4);
     const auto pick = [&](auto b) {
         constexpr bool B = decltype(b)::value;
-        if (vec <= 256 * 4) go(k_token_loss<B, 256, 4>, 256);
-        else if (vec <= 256 * 8) go(k_token_loss<B, 256, 8>, 256);
-        else if (vec <= 512 * 8) go(k_token_loss<B, 512, 8>, 512);
-        else if (vec <= 1024 * 8) go(k_token_loss<B, 1024, 8>, 1024);
-        else if (vec <= 1024 * 16) go(k_token_loss<B, 1024, 16>, 1024);
-        else go(k_token_loss<B, 1024, 0>, 1024);
+        // Many tokens of a large vocabulary: two workgroups of 1024 threads on a CU, so that one loads or stores while
+        // the other computes (2,048 tokens of 128,000 bf16 logits: 202 us; one workgroup with all of the token in its
+        // registers 222).  Few tokens: as much as one workgroup has registers for (61 tokens of 50,001 fp32
+        // logits: 11 against 16 us).
+        if (vec <= 256 * 4) go(k_token_loss<B, 256, 4, 8>, 256);
+        else if (vec <= 512 * 4) go(k_token_loss<B, 512, 4, 8>, 512);
+        else if (vec <= 1024 * 4 || rows > 256) go(k_token_loss<B, 1024, 4, 8>, 1024);
+        else go(k_token_loss<B, 1024, 12, 4>, 1024);
     };
     if (bf16)
         pick(std::true_type{});
