@@ -289,13 +289,13 @@ __device__ __forceinline__ void swap8(u32x4 &a, u32x4 &b) {
 __device__ __forceinline__ int pair_row() { return threadIdx.x & 7; }
 __device__ __forceinline__ int pair_col() { return ((threadIdx.x >> 3) & 1) * 4 + ((threadIdx.x >> 4) & 3); }
 
-// Tiles are the slow index of a grid, so that workgroups that run together work
-// on the same rows (4.4 TB/s with the rows as the fast one); beyond 2^15 tiles
-// they go on in z.
-__device__ __forceinline__ int tile_index() { return blockIdx.y + gridDim.y * blockIdx.z; }
-inline dim3 tile_grid(int64_t fast, int64_t tiles) {
-    const int64_t y = tiles < (1 << 15) ? tiles : (1 << 15);
-    return dim3(static_cast<unsigned>(fast), static_cast<unsigned>(y), static_cast<unsigned>((tiles + y - 1) / y));
+// Grids are lists of blocks in which the tiles are the slow index, so that
+// workgroups that run together work on the same rows (4.4 TB/s with the rows as
+// the fast one); beyond 2^22 blocks a list goes on in y.
+__device__ __forceinline__ uint32_t block_index() { return blockIdx.x + gridDim.x * blockIdx.y; }
+inline dim3 block_grid(int64_t blocks) {
+    const int64_t x = blocks < (1 << 22) ? blocks : (1 << 22);
+    return dim3(static_cast<unsigned>(x), static_cast<unsigned>((blocks + x - 1) / x));
 }
 
 // ----------------------------------------------------------------- shrink --
@@ -321,18 +321,34 @@ __device__ __forceinline__ u32x4 drop_piece(const DropArgs &d, u32x4 v, uint32_t
     return drop4_f32(d, v, row, static_cast<uint32_t>(col));
 }
 
-// part[split][place][16 RT] = sum over the split's range of W_a[r][j] drop(v_t[j]) f
+struct ShrinkArgs {
+    const char *v;
+    int64_t ld;
+    int width;
+    const char *W;
+    int rank;
+    float *part;              // [splits][places][16 RT]
+    int64_t places;
+    int splits, per_split;
+};
+template <int M, int RT>
+constexpr int kShrinkLds = 4 * 16 * M * 16 * RT * 4;
+
+// Block `index`: tile and range of the long axis; part = the sum over the range
+// of W_a[r][j] drop(v_t[j]).
 template <bool BF16, int M, int RT, bool DROP>
-__global__ __launch_bounds__(256) void k_shrink(TileList list, const char *v, int64_t ld, int width, const char *W,
-                                                int rank, float *part, int64_t places, int per_split, DropArgs d) {
+__device__ __forceinline__ void shrink(const TileList &list, const ShrinkArgs &a, const DropArgs &d, uint32_t index, char *lds) {
     constexpr int kRp = 16 * RT, kUnit = 8 * kVec<BF16>;   // 128 bytes of a row
-    __shared__ float red[4][16 * M][kRp];
-    const int at = tile_index();
+    float(*red)[16 * M][kRp] = reinterpret_cast<float(*)[16 * M][kRp]>(lds);
+    const int at = index / a.splits, split = index - at * a.splits;
     if (at >= tile_count(list, false)) return;
     const Tile tile = list.tiles[at];
+    const char *v = a.v, *W = a.W;
+    const int64_t ld = a.ld;
+    const int width = a.width, rank = a.rank;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
-    const int begin = blockIdx.x * per_split;
-    const int end = width - begin < per_split ? width : begin + per_split;
+    const int begin = split * a.per_split;
+    const int end = width - begin < a.per_split ? width : begin + a.per_split;
 
     // rows of the two 128-byte pieces of each 16-row block
     int row[M][2];
@@ -416,7 +432,7 @@ __global__ __launch_bounds__(256) void k_shrink(TileList list, const char *v, in
         for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4 *>(&red[wave][16 * m + t][16 * r + 4 * g]) = acc[m][r];
     __syncthreads();
     const float f = DROP ? d.scale : 1.f;
-    float *out = part + (static_cast<int64_t>(blockIdx.x) * places + tile.p0) * kRp;
+    float *out = a.part + (static_cast<int64_t>(split) * a.places + tile.p0) * kRp;
     for (int i = threadIdx.x; i < 16 * M * kRp / 4; i += 256) {
         const int slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
         if (slot >= tile.count) break;
@@ -427,6 +443,12 @@ __global__ __launch_bounds__(256) void k_shrink(TileList list, const char *v, in
         for (int e = 0; e < 4; ++e) s[e] = r + e < rank ? s[e] * f : 0.f;
         *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(slot) * kRp + r) = s;
     }
+}
+
+template <bool BF16, int M, int RT, bool DROP>
+__global__ __launch_bounds__(256) void k_shrink(TileList list, ShrinkArgs a, DropArgs d) {
+    __shared__ __align__(16) char lds[kShrinkLds<M, RT>];
+    shrink<BF16, M, RT, DROP>(list, a, d, block_index(), lds);
 }
 
 // ----------------------------------------------------------------- expand --
@@ -463,23 +485,33 @@ struct ExpandArgs {
     char *out;
     int64_t ld_o;
     float *u_out;             // [rows][rank] or null: the sum of the partials, unscaled
+    int slices;               // of kSlice columns
 };
 
-// One workgroup: 16 M rows and four waves' columns.
+template <bool BF16, int RT>
+constexpr int kSliceCols = 4 * kCols<BF16, RT>;
+template <bool BF16, int RT>
+constexpr int kWPitch = kSliceCols<BF16, RT> * kEs<BF16> + (BF16 ? 32 : 16);
+// A row of U: bf16 upper halves then lower halves, or fp32.
+template <int RT>
+constexpr int kURow = 64 * RT + 16;
+template <bool BF16, int M, int RT>
+constexpr int kExpandLds = 16 * RT * kWPitch<BF16, RT> + 16 * M * kURow<RT>;
+
+// Block `index`: tile of 16 M rows and slice of four waves' columns.
 template <bool BF16, int M, int RT, bool DROP>
-__global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, DropArgs d) {
-    constexpr int kRp = 16 * RT, kNw = kCols<BF16, RT>, kSlice = 4 * kNw, kPitch = kSlice * kEs<BF16> + (BF16 ? 32 : 16);
-    constexpr int kV = kVec<BF16>, kUPitch = 4 * kRp + 16;   // a row of U: bf16 upper halves then lower halves, or fp32
-    __shared__ __align__(16) char lds_w[kRp * kPitch];
-    __shared__ __align__(16) char lds_u[16 * M * kUPitch];
-    const int at = tile_index();
+__device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a, const DropArgs &d, uint32_t index, char *lds) {
+    constexpr int kRp = 16 * RT, kNw = kCols<BF16, RT>, kSlice = kSliceCols<BF16, RT>, kPitch = kWPitch<BF16, RT>;
+    constexpr int kV = kVec<BF16>, kUPitch = kURow<RT>;
+    char *lds_w = lds, *lds_u = lds + kRp * kPitch;
+    const int at = index / a.slices, slice = index - at * a.slices;
     if (at >= tile_count(list, true)) return;
     const Tile tile = list.tiles[at];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * kSlice;
+    const int n0 = slice * kSlice;
 
     if (tile.group == list.n) {   // rows without an adapter
-        if (a.u_out && blockIdx.x == 0)
+        if (a.u_out && slice == 0)
             for (int i = threadIdx.x; i < tile.count * a.rank; i += 256)
                 a.u_out[static_cast<int64_t>(list.row_of[tile.p0 + i / a.rank]) * a.rank + i % a.rank] = 0.f;
         if (a.out == a.base && a.ld_o == a.ld_b) return;
@@ -553,7 +585,7 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
         f32x4 v = u[k][0];
 #pragma unroll
         for (int c = 1; c < kAhead; ++c) v += u[k][c];
-        if (a.u_out && blockIdx.x == 0) {
+        if (a.u_out && slice == 0) {
             float *o = a.u_out + static_cast<int64_t>(list.row_of[tile.p0 + slot]) * a.rank + r;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -664,20 +696,10 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
     }
 }
 
-// ------------------------------------------------------------------- join --
-// du[place][rp] = s_a times the sum of the splits' parts.
-__global__ __launch_bounds__(256) void k_join(TileList list, const float *part, int splits, int64_t places, int rp,
-                                              const float *scale, float *du) {
-    const int at = tile_index();
-    if (at >= tile_count(list, false)) return;
-    const Tile tile = list.tiles[at];
-    const float s = scale ? scale[tile.group] : 1.f;
-    for (int i = threadIdx.x * 4; i < tile.count * rp; i += 1024) {
-        const int64_t p = static_cast<int64_t>(tile.p0) * rp + i;
-        f32x4 v = *reinterpret_cast<const f32x4 *>(part + p);
-        for (int k = 1; k < splits; ++k) v += *reinterpret_cast<const f32x4 *>(part + k * places * rp + p);
-        *reinterpret_cast<f32x4 *>(du + p) = v * s;
-    }
+template <bool BF16, int M, int RT, bool DROP>
+__global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, DropArgs d) {
+    __shared__ __align__(16) char lds[kExpandLds<BF16, M, RT>];
+    expand<BF16, M, RT, DROP>(list, a, d, block_index(), lds);
 }
 
 // ------------------------------------------------------------------- grad --
@@ -691,65 +713,83 @@ constexpr uint32_t kMaxRuns = 1024;   // with the 2^19 + 1023 blocks at most, pr
 __device__ __forceinline__ uint32_t run_begin(uint32_t blocks, uint32_t i, uint32_t n) { return blocks * i / n; }
 __device__ __forceinline__ uint32_t run_of(uint32_t blocks, uint32_t j, uint32_t n) { return ((j + 1) * n - 1) / blocks; }
 
-struct GradJob {
+struct GradArgs {
     const char *v;            // rows x or dy
     int64_t ld;
     int width, slices;
-    const float *U;           // by_row: u [rows][rank]; else du [places][rp]
-    int by_row;
-    float *part;              // [runs + n][rp][width]
-    uint32_t thr;             // dropout of v
-};
-struct GradArgs {
-    GradJob job[2];
+    const float *U;           // splits = 0: u [rows][rank]; else du in parts [splits][places][rp]
+    int splits;
+    int64_t places;
     int rank;
+    float *part;              // [runs + n][rp][width]
+    int runs;
 };
 
 constexpr int kGradCols = 256;
 
+// Parts of du that are fetched one by one, and so the splits of the backward
+// pass's k_shrink.
+__host__ __device__ constexpr int parts_of(int rt) { return rt == 1 ? 4 : 2; }
+template <int RT>
+constexpr int kParts = parts_of(RT);
+constexpr int kGradChunk = 32;   // blocks whose rows are looked up together
+template <bool BF16>
+constexpr int kVPitch = kGradCols * kEs<BF16> + 32;
 template <bool BF16, int RT>
-__global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArgs d) {
-    constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kGradCols * kEs<BF16> + 32;
+constexpr int kULds = BF16 ? 3 * 16 * RT * 80 : 32 * (64 * RT + 16);
+template <bool BF16, int RT>
+constexpr int kGradLds = 32 * kVPitch<BF16> + kULds<BF16, RT> + kGradChunk * (32 * 4 + 16);
+
+// Block `index`: run and slice of kGradCols columns of v.
+template <bool BF16, int RT, bool DROP>
+__device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, const DropArgs &d, uint32_t index, char *lds) {
+    constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kVPitch<BF16>;
     constexpr int kLoads = 32 * (kGradCols / kV) / 256;      // 16-byte loads of a thread for 32 rows
     constexpr int kRowsPer = 32 / kLoads;                    // rows that the workgroup loads at once
     // U of 32 places.  bf16: [third][rank][place]; fp32: [place][rank]
-    constexpr int kUPitch = BF16 ? 80 : 4 * kRp + 16, kUThird = kRp * kUPitch;
-    constexpr int kChunk = 32;                               // blocks whose rows are looked up together
-    __shared__ __align__(16) char lds_v[32 * kPitch];
-    __shared__ __align__(16) char lds_u[BF16 ? 3 * kUThird : 32 * kUPitch];
-    __shared__ int lds_row[kChunk * 32];
-    __shared__ Tile lds_tile[kChunk];
-    const uint32_t blocks = tile_count(list, false), runs = blocks < gridDim.y ? blocks : gridDim.y;
-    if (blockIdx.y >= runs) return;
-    const int which = static_cast<int>(blockIdx.x) >= a.job[0].slices;
-    const GradJob job = which ? a.job[1] : a.job[0];
-    const int n0 = (blockIdx.x - (which ? a.job[0].slices : 0)) * kGradCols;
+    constexpr int kUPitch = BF16 ? 80 : 4 * kRp + 16, kUThird = kRp * kUPitch, kChunk = kGradChunk;
+    char *lds_v = lds, *lds_u = lds + 32 * kPitch;
+    int *lds_row = reinterpret_cast<int *>(lds_u + kULds<BF16, RT>);
+    Tile *lds_tile = reinterpret_cast<Tile *>(lds_row + 32 * kChunk);
+    const uint32_t blocks = tile_count(list, false), runs = blocks < static_cast<uint32_t>(a.runs) ? blocks : a.runs;
+    const uint32_t run = index / a.slices, slice = index - run * a.slices;
+    if (run >= runs) return;
+    const int n0 = slice * kGradCols;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
-    const int end = run_begin(blocks, blockIdx.y + 1, runs);
+    const int end = run_begin(blocks, run + 1, runs);
 
     const int lr = threadIdx.x / (kGradCols / kV), lc = threadIdx.x % (kGradCols / kV) * kV;
-    const bool in = n0 + lc < job.width;
+    const bool in = n0 + lc < a.width;
     const int ur = threadIdx.x & 15, up = threadIdx.x >> 4;   // rank within 16 and pair of places that the thread loads
-    float u[RT][2];
-    u32x4 v[kLoads];
-    const auto load = [&](int i) {   // U first: it comes from L2, and loads return in order
-        const int p0 = lds_tile[i].p0;
+    // The next block is on its way while one is multiplied (two ahead measured the same).  Every lane loads: for a pad, and beyond the rank or the width, something
+    // of the block's first row or the first column, which is put aside when it is used.
+    struct Fetch {
+        float u[kParts<RT>][RT][2];
+        u32x4 v[kLoads];
+    } ahead;
+    const int64_t col_bytes = static_cast<int64_t>(in ? n0 + lc : 0) * kEs<BF16>;
+    const auto load = [&](Fetch &f, int i) {   // U first: it comes from L2, and loads return in order
+        const int first = lds_row[32 * i];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int row = lds_row[32 * i + 2 * up + e];
+            const int64_t place = static_cast<int64_t>(lds_tile[i].p0) + (row < 0 ? 0 : 2 * up + e);
+            const float *q = a.splits ? a.U + place * kRp + ur : a.U + static_cast<int64_t>(row < 0 ? first : row) * a.rank;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const int k = 16 * r + ur;
-                u[r][e] = row >= 0 && k < a.rank
-                              ? job.U[job.by_row ? static_cast<int64_t>(row) * a.rank + k
-                                                 : (static_cast<int64_t>(p0) + 2 * up + e) * kRp + k]
-                              : 0.f;
+                const int k = 16 * r + ur, known = k < a.rank ? k : 0;
+                f.u[0][r][e] = a.splits ? q[16 * r] : q[known];
+#pragma unroll
+                for (int c = 1; c < kParts<RT>; ++c) {
+                    f.u[c][r][e] = 0.f;
+                    if (a.splits > c) f.u[c][r][e] = q[16 * r + c * a.places * kRp];
+                }
             }
         }
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             const int row = lds_row[32 * i + kRowsPer * k + lr];
-            v[k] = in && row >= 0 ? ld128_nt(job.v + (row * job.ld + n0 + lc) * kEs<BF16>) : u32x4{0, 0, 0, 0};
+            f.v[k] = ld128_nt(a.v + (row < 0 ? first : row) * a.ld * kEs<BF16> + col_bytes);
         }
     };
     f32x4 acc[4][RT];
@@ -761,19 +801,19 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
     };
     // lane holds columns 4 g .. + 3 of block b for rank 16 r + t
     const auto flush = [&](int group) {
-        float *out = job.part + (static_cast<int64_t>(blockIdx.y) + group) * kRp * job.width;
+        float *out = a.part + (static_cast<int64_t>(run) + group) * kRp * a.width;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const int col = n0 + wave * 64 + 16 * b + 4 * g;
-            if (col >= job.width) continue;
+            if (col >= a.width) continue;
 #pragma unroll
             for (int r = 0; r < RT; ++r)
-                *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(16 * r + t) * job.width + col) = acc[b][r];
+                *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(16 * r + t) * a.width + col) = acc[b][r];
         }
     };
     clear();
     int group = -1;
-    for (int chunk = run_begin(blocks, blockIdx.y, runs); chunk < end; chunk += kChunk) {
+    for (int chunk = run_begin(blocks, run, runs); chunk < end; chunk += kChunk) {
         const int count = end - chunk < kChunk ? end - chunk : kChunk;
         __syncthreads();
         if (static_cast<int>(threadIdx.x) < count) lds_tile[threadIdx.x] = list.tiles[chunk + threadIdx.x];
@@ -783,8 +823,7 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
             lds_row[i] = i % 32 < tile.count ? list.row_of[tile.p0 + i % 32] : -1;
         }
         __syncthreads();
-        load(0);
-        for (int i = 0; i < count; ++i) {
+        const auto step = [&](Fetch &f, int i) {
             if (lds_tile[i].group != group) {
                 if (group >= 0) {
                     flush(group);
@@ -795,28 +834,35 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
             if (i) __syncthreads();   // the waves are done with the block before
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
+                float q[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    q[e] = f.u[0][r][e];
+#pragma unroll
+                    for (int c = 1; c < kParts<RT>; ++c) q[e] += f.u[c][r][e];
+                    if (lds_row[32 * i + 2 * up + e] < 0 || 16 * r + ur >= a.rank) q[e] = 0.f;
+                }
                 if constexpr (BF16) {
-                    float lo = u[r][0], hi = u[r][1];
 #pragma unroll
                     for (int third = 0; third < 3; ++third) {
-                        *reinterpret_cast<uint32_t *>(lds_u + third * kUThird + (16 * r + ur) * kUPitch + 4 * up) = pack2(lo, hi);
-                        lo = left_over(lo);
-                        hi = left_over(hi);
+                        *reinterpret_cast<uint32_t *>(lds_u + third * kUThird + (16 * r + ur) * kUPitch + 4 * up) = pack2(q[0], q[1]);
+                        q[0] = left_over(q[0]);
+                        q[1] = left_over(q[1]);
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        *reinterpret_cast<float *>(lds_u + (2 * up + e) * kUPitch + (16 * r + ur) * 4) = u[r][e];
+                        *reinterpret_cast<float *>(lds_u + (2 * up + e) * kUPitch + (16 * r + ur) * 4) = q[e];
                 }
             }
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
-                const int slot = kRowsPer * k + lr;
-                if (job.thr) v[k] = drop_piece<BF16>(d, v[k], static_cast<uint32_t>(lds_row[32 * i + slot]), n0 + lc);
-                *reinterpret_cast<u32x4 *>(lds_v + slot * kPitch + lc * kEs<BF16>) = v[k];
+                const int slot = kRowsPer * k + lr, row = lds_row[32 * i + slot];
+                if constexpr (DROP) f.v[k] = drop_piece<BF16>(d, f.v[k], static_cast<uint32_t>(row), n0 + lc);
+                *reinterpret_cast<u32x4 *>(lds_v + slot * kPitch + lc * kEs<BF16>) = in && row >= 0 ? f.v[k] : u32x4{0, 0, 0, 0};
             }
             __syncthreads();
-            if (i + 1 < count) load(i + 1);
+            if (i + 1 < count) load(f, i + 1);
             if constexpr (BF16) {
                 u32x4 vf[4];
                 const uint32_t l0 = lds_addr(lds_v) + static_cast<uint32_t>((8 * g + (t >> 2)) * kPitch + (wave * 64 + 4 * (t & 3)) * 2);
@@ -849,9 +895,35 @@ __global__ __launch_bounds__(256) void k_grad(TileList list, GradArgs a, DropArg
                     }
                 }
             }
-        }
+        };
+        load(ahead, 0);
+        for (int i = 0; i < count; ++i) step(ahead, i);
     }
     if (group >= 0) flush(group);
+}
+
+// The two launches of the backward pass.  In each, a gradient's blocks come first
+// (they are few and long), then those of the product that shares its rows:
+// du = B dy beside dB, both of which read dy; then dx beside dA.
+template <bool BF16, int M, int RT>
+__global__ __launch_bounds__(256) void k_back_dy(TileList blocks, GradArgs g, TileList tiles, ShrinkArgs s, DropArgs d) {
+    constexpr int kLds = kGradLds<BF16, RT> > kShrinkLds<M, RT> ? kGradLds<BF16, RT> : kShrinkLds<M, RT>;
+    __shared__ __align__(16) char lds[kLds];
+    const uint32_t index = block_index(), n = g.runs * g.slices;
+    if (index < n)
+        grad<BF16, RT, false>(blocks, g, d, index, lds);
+    else
+        shrink<BF16, M, RT, false>(tiles, s, d, index - n, lds);
+}
+template <bool BF16, int M, int RT, bool DROP>
+__global__ __launch_bounds__(256) void k_back_x(TileList blocks, GradArgs g, TileList tiles, ExpandArgs e, DropArgs d) {
+    constexpr int kLds = kGradLds<BF16, RT> > kExpandLds<BF16, M, RT> ? kGradLds<BF16, RT> : kExpandLds<BF16, M, RT>;
+    __shared__ __align__(16) char lds[kLds];
+    const uint32_t index = block_index(), n = g.runs * g.slices;
+    if (index < n)
+        grad<BF16, RT, DROP>(blocks, g, d, index, lds);
+    else if (e.out)   // (dx may not be wanted)
+        expand<BF16, M, RT, DROP>(tiles, e, d, index - n, lds);
 }
 
 struct ReduceJob {
@@ -906,49 +978,56 @@ __global__ __launch_bounds__(256) void k_zero(float *p, int64_t quads) {
 
 // ------------------------------------------------------------------- host --
 int rank_tiles(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Launch shapes, functions of the sizes alone.
 struct Shape {
     int rt, rp;
     int64_t places;
-    int h_shrink;                 // list height
-    int runs;                     // of k_grad
+    int runs;                     // of the gradients
 };
 
-// Rows per tile: 16 where an adapter has few rows on average (decoding), else as
-// many as share one read of its weights.
 Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     Shape s;
     s.rt = rank_tiles(rank);
     s.rp = 16 * s.rt;
     s.places = plan_places(rows, n);
-    const bool few = rows < static_cast<int64_t>(32) * n || rows <= 32;
-    s.h_shrink = few ? 0 : (s.rt == 2 || s.rt == 4) ? 2 : 1;
-    // runs of k_grad: four workgroups for each CU (all resident; two took 68 us, four 52 for 16,384 rows of 4096 +
-    // 4096 columns at rank 16, and with six the parts cost more than the occupancy gains)
-    const int64_t slices = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
+    // runs of the gradients: with both of them, four workgroups for each CU (two took 68 us, four 52 for 16,384 rows of
+    // 4096 + 4096 columns at rank 16, and with six the parts cost more than the occupancy gains)
+    const int64_t slices = ceil_div(n_in, kGradCols) + ceil_div(n_out, kGradCols);
     // a part costs what rank / 16 blocks do: runs of at least 1.5 times that many (2,047 rows at rank 64: runs of one
     // block took 21 us and their sum 12, runs of six 17 and 6)
-    const int64_t least = s.rt == 1 ? 1 : s.rt * 3 / 2, most = (plan_max_tiles(rows, n, 1) + least - 1) / least;
-    int64_t runs = 1024 / slices;
+    const int64_t least = s.rt == 1 ? 1 : s.rt * 3 / 2, most = ceil_div(plan_max_tiles(rows, n, 1), least);
+    const int64_t runs = 1024 / slices;
     s.runs = static_cast<int>(runs < 1 ? 1 : runs > most ? most : runs);
     return s;
 }
 
-// Ranges of the long axis in k_shrink: enough workgroups for two on each CU.
-int shrink_splits(const Shape &s, int64_t rows, int n, int width, int *per) {
-    const int64_t tiles = (rows >> (4 + s.h_shrink)) + (n < rows ? n : rows);
-    int64_t want = (2048 + tiles - 1) / tiles;
-    const int64_t most = (width + 511) / 512;
-    if (want > most) want = most;
-    if (want > 8) want = 8;
-    if (want < 1) want = 1;
-    *per = static_cast<int>(((width + want - 1) / want + 255) / 256 * 256);
-    return (width + *per - 1) / *per;
+// Tiles of the shrinking product (16 << h rows) and ranges of its long axis: as
+// many workgroups as `groups`, if ranges of a kilobyte and tiles of 16 rows give
+// them.
+struct ShrinkShape {
+    int h, splits, per;
+};
+ShrinkShape shrink_shape(int64_t rows, int n, int width, int es, int groups, int most_splits) {
+    const int64_t wide = ceil_div(static_cast<int64_t>(width) * es, 1024), most = wide < most_splits ? wide : most_splits;
+    ShrinkShape s;
+    s.h = (rows >> 5) * most < 256 ? 0 : 1;
+    const int64_t tiles = (rows >> (4 + s.h)) + (n < rows ? n : rows);
+    int64_t want = ceil_div(groups, tiles);
+    want = want > most ? most : want;
+    const int step = 512 / es;   // the four waves' pieces
+    s.per = static_cast<int>(ceil_div(ceil_div(width, want), step) * step);
+    s.splits = static_cast<int>(ceil_div(width, s.per));
+    return s;
 }
+// The forward pass hides the drawing of its dropout behind more workgroups (16,384 x 4096 at rank 16: 39 us with 512,
+// 32 with 2048); without it, and in the backward pass, fewer parts are better for those that add them.
+constexpr int kForwardGroups = 2048, kGroups = 512;
+constexpr int kForwardSplits = 8;
 
 struct WsLayout {
-    size_t part, du, part_a, part_b, bytes;
+    size_t part, part_a, part_b, bytes;
 };
 WsLayout ws_layout(const Shape &s, int64_t rows, int n_in, int n_out, int n) {
     WsLayout l;
@@ -958,19 +1037,22 @@ WsLayout ws_layout(const Shape &s, int64_t rows, int n_in, int n_out, int n) {
         at += align256(b);
         return here;
     };
-    int per;
-    const int sf = shrink_splits(s, rows, n, n_in, &per), sb = shrink_splits(s, rows, n, n_out, &per);
-    const size_t u = static_cast<size_t>(s.places) * s.rp;
+    int splits = 1;
+    for (int es = 2; es <= 4; es += 2) {
+        const int f = shrink_shape(rows, n, n_in, es, kForwardGroups, kForwardSplits).splits,
+                  b = shrink_shape(rows, n, n_out, es, kGroups, parts_of(s.rt)).splits;
+        splits = f > splits ? f : splits;
+        splits = b > splits ? b : splits;
+    }
     const size_t parts = static_cast<size_t>(s.runs) + n;
-    l.part = take(u * 4 * (sf > sb ? sf : sb));
-    l.du = take(u * 4);
+    l.part = take(static_cast<size_t>(s.places) * s.rp * 4 * splits);
     l.part_a = take(parts * s.rp * n_in * 4);
     l.part_b = take(parts * s.rp * n_out * 4);
     l.bytes = at;
     return l;
 }
 
-template <bool BF16, bool DROP, typename F>
+template <typename F>
 void with_rank(int rt, F f) {
     switch (rt) {
         case 1: f(std::integral_constant<int, 1>{}); break;
@@ -979,40 +1061,15 @@ void with_rank(int rt, F f) {
         default: f(std::integral_constant<int, 8>{}); break;
     }
 }
-
-template <bool BF16, bool DROP>
-void run_shrink(const Shape &s, const PlanView &pv, const void *v, int64_t ld, int width, const void *W, int rank,
-                float *part, int splits, int per, const DropArgs &d, hipStream_t st) {
-    const TileList list = tile_list(pv, s.h_shrink);
-    const dim3 grid = tile_grid(splits, plan_max_tiles(pv.rows, pv.n, s.h_shrink));
-    with_rank<BF16, DROP>(s.rt, [&](auto rt) {
-        constexpr int RT = decltype(rt)::value, M = RT == 2 || RT == 4 ? 4 : 2;
-        const auto go = [&](auto kernel) {
-            kernel<<<grid, 256, 0, st>>>(list, static_cast<const char *>(v), ld, width, static_cast<const char *>(W), rank,
-                                         part, s.places, per, d);
-        };
-        s.h_shrink == 0 ? go(k_shrink<BF16, 1, RT, DROP>) : go(k_shrink<BF16, M, RT, DROP>);
-    });
+template <typename F>
+void with_tile(int h, F f) {
+    if (h == 0)
+        f(std::integral_constant<int, 1>{});
+    else
+        f(std::integral_constant<int, 2>{});
 }
-
-template <bool BF16, bool DROP>
-void run_expand(const Shape &s, const PlanView &pv, const ExpandArgs &a, const DropArgs &d, hipStream_t st) {
-    with_rank<BF16, DROP>(s.rt, [&](auto rt) {
-        constexpr int RT = decltype(rt)::value, kSlice = 4 * kCols<BF16, RT>;
-        // the tallest tiles that leave two workgroups for each CU (64 rows, 32 at rank 128, whose operands fill LDS)
-        const int64_t slices = (a.width + kSlice - 1) / kSlice;
-        int h = RT == 8 ? 1 : 2;
-        while (h > 0 && (static_cast<int64_t>(pv.rows) >> (4 + h)) * slices < 512) --h;
-        const TileList list = tile_list(pv, h);
-        const dim3 grid = tile_grid(slices, plan_max_tiles(pv.rows, pv.n, h));
-        if (h == 0)
-            k_expand<BF16, 1, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
-        else if (RT == 8 || h == 1)
-            k_expand<BF16, 2, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
-        else
-            k_expand<BF16, RT == 8 ? 2 : 4, RT, DROP><<<grid, 256, 0, st>>>(list, a, d);
-    });
-}
+// Tiles of the expanding product: 32 rows, or 16 where those leave CUs without work.
+int expand_height(int64_t rows, int slices) { return (rows >> 5) * slices < 512 ? 0 : 1; }
 
 }  // namespace
 
@@ -1040,19 +1097,30 @@ hipError_t launch_adapter_forward(const AdapterDims &m, bool bf16, const void *p
     const Shape s = shape_of(m.rows, m.n_in, m.n_out, m.rank, m.n);
     const WsLayout l = ws_layout(s, m.rows, m.n_in, m.n_out, m.n);
     float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
-    int per;
-    const int splits = shrink_splits(s, m.rows, m.n, m.n_in, &per);
-    const ExpandArgs e = {part, splits, s.places, scale, static_cast<const char *>(B), m.rank, m.n_out,
-                          static_cast<const char *>(base), ld_b, static_cast<char *>(y), ld_y, u};
-    const auto go = [&](auto b) {
+    const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_in, bf16 ? 2 : 4, d.thr ? kForwardGroups : kGroups, kForwardSplits);
+    const ShrinkArgs sa = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<const char *>(A), m.rank, part, s.places,
+                           h.splits, h.per};
+    ExpandArgs e = {part, h.splits, s.places, scale, static_cast<const char *>(B), m.rank, m.n_out,
+                    static_cast<const char *>(base), ld_b, static_cast<char *>(y), ld_y, u, 0};
+    const auto go = [&](auto b, auto rt) {
         constexpr bool BF16 = decltype(b)::value;
-        if (d.thr)
-            run_shrink<BF16, true>(s, pv, x, ld_x, m.n_in, A, m.rank, part, splits, per, d, st);
-        else
-            run_shrink<BF16, false>(s, pv, x, ld_x, m.n_in, A, m.rank, part, splits, per, d, st);
-        run_expand<BF16, false>(s, pv, e, d, st);
+        constexpr int RT = decltype(rt)::value;
+        with_tile(h.h, [&](auto mt) {
+            constexpr int M = decltype(mt)::value;
+            const dim3 grid = block_grid(plan_max_tiles(m.rows, m.n, h.h) * h.splits);
+            if (d.thr)
+                k_shrink<BF16, M, RT, true><<<grid, 256, 0, st>>>(tile_list(pv, h.h), sa, d);
+            else
+                k_shrink<BF16, M, RT, false><<<grid, 256, 0, st>>>(tile_list(pv, h.h), sa, d);
+        });
+        e.slices = static_cast<int>(ceil_div(m.n_out, kSliceCols<BF16, RT>));
+        const int he = expand_height(m.rows, e.slices);
+        with_tile(he, [&](auto mt) {
+            k_expand<BF16, decltype(mt)::value, RT, false>
+                <<<block_grid(plan_max_tiles(m.rows, m.n, he) * e.slices), 256, 0, st>>>(tile_list(pv, he), e, d);
+        });
     };
-    bf16 ? go(std::true_type{}) : go(std::false_type{});
+    with_rank(s.rt, [&](auto rt) { bf16 ? go(std::true_type{}, rt) : go(std::false_type{}, rt); });
     return hipGetLastError();
 }
 
@@ -1074,44 +1142,48 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
     const Shape s = shape_of(m.rows, m.n_in, m.n_out, m.rank, m.n);
     const WsLayout l = ws_layout(s, m.rows, m.n_in, m.n_out, m.n);
     char *w = static_cast<char *>(ws);
-    float *part = reinterpret_cast<float *>(w + l.part), *du = reinterpret_cast<float *>(w + l.du);
-    int per;
-    const int splits = shrink_splits(s, m.rows, m.n, m.n_out, &per);
-    const auto go = [&](auto b) {
+    float *part = reinterpret_cast<float *>(w + l.part);
+    const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_out, bf16 ? 2 : 4, kGroups, parts_of(s.rt));
+    const ShrinkArgs sa = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<const char *>(B), m.rank, part, s.places,
+                           h.splits, h.per};
+    const GradArgs gb = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<int>(ceil_div(m.n_out, kGradCols)), u, 0,
+                         s.places, m.rank, reinterpret_cast<float *>(w + l.part_b), s.runs};
+    const GradArgs ga = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<int>(ceil_div(m.n_in, kGradCols)), part,
+                         h.splits, s.places, m.rank, reinterpret_cast<float *>(w + l.part_a), s.runs};
+    ExpandArgs e = {part, h.splits, s.places, scale, static_cast<const char *>(A), m.rank, m.n_in,
+                    static_cast<const char *>(base), ld_b, static_cast<char *>(dx), ld_dx, nullptr, 0};
+    const TileList blocks = tile_list(pv, 1);
+    const auto go = [&](auto b, auto rt) {
         constexpr bool BF16 = decltype(b)::value;
-        run_shrink<BF16, false>(s, pv, dy, ld_dy, m.n_out, B, m.rank, part, splits, per, d, st);
-        k_join<<<tile_grid(1, plan_max_tiles(m.rows, m.n, 2)), 256, 0, st>>>(tile_list(pv, 2), part, splits, s.places, s.rp,
-                                                                            scale, du);
-        GradArgs ga = {};
-        ga.rank = m.rank;
-        ga.job[0] = {static_cast<const char *>(dy), ld_dy, m.n_out, (m.n_out + kGradCols - 1) / kGradCols, u, 1,
-                     reinterpret_cast<float *>(w + l.part_b), 0};
-        ga.job[1] = {static_cast<const char *>(x), ld_x, m.n_in, (m.n_in + kGradCols - 1) / kGradCols, du, 0,
-                     reinterpret_cast<float *>(w + l.part_a), d.thr};
-        const dim3 grid(static_cast<unsigned>(ga.job[0].slices + ga.job[1].slices), static_cast<unsigned>(s.runs));
-        with_rank<BF16, false>(s.rt, [&](auto rt) {
-            k_grad<BF16, decltype(rt)::value><<<grid, 256, 0, st>>>(tile_list(pv, 1), ga, d);
+        constexpr int RT = decltype(rt)::value;
+        with_tile(h.h, [&](auto mt) {
+            const int64_t n = static_cast<int64_t>(gb.runs) * gb.slices + plan_max_tiles(m.rows, m.n, h.h) * h.splits;
+            k_back_dy<BF16, decltype(mt)::value, RT><<<block_grid(n), 256, 0, st>>>(blocks, gb, tile_list(pv, h.h), sa, d);
         });
-        ReduceArgs r = {};
-        r.job[0] = {ga.job[0].part, dB, scale, 1.f, m.n_out, (m.n_out + 1023) / 1024};
-        r.job[1] = {ga.job[1].part, dA, nullptr, d.scale, m.n_in, (m.n_in + 1023) / 1024};
-        r.head = pv.head;
-        r.first = pv.first[1];
-        r.runs = s.runs;
-        r.rows = pv.rows;
-        r.n = m.n;
-        r.rank = m.rank;
-        r.rp = s.rp;
-        r.accumulate = accumulate;
-        k_reduce<<<dim3(static_cast<unsigned>(m.n * m.rank), static_cast<unsigned>(r.job[0].slices + r.job[1].slices)), 256, 0,
-                   st>>>(r);
-        if (dx) {
-            const ExpandArgs e = {du, 1, s.places, nullptr, static_cast<const char *>(A), m.rank, m.n_in,
-                                  static_cast<const char *>(base), ld_b, static_cast<char *>(dx), ld_dx, nullptr};
-            d.thr ? run_expand<BF16, true>(s, pv, e, d, st) : run_expand<BF16, false>(s, pv, e, d, st);
-        }
+        e.slices = static_cast<int>(ceil_div(m.n_in, kSliceCols<BF16, RT>));
+        const int he = expand_height(m.rows, e.slices);
+        with_tile(he, [&](auto mt) {
+            constexpr int M = decltype(mt)::value;
+            const int64_t n = static_cast<int64_t>(ga.runs) * ga.slices + (dx ? plan_max_tiles(m.rows, m.n, he) * e.slices : 0);
+            if (d.thr)
+                k_back_x<BF16, M, RT, true><<<block_grid(n), 256, 0, st>>>(blocks, ga, tile_list(pv, he), e, d);
+            else
+                k_back_x<BF16, M, RT, false><<<block_grid(n), 256, 0, st>>>(blocks, ga, tile_list(pv, he), e, d);
+        });
     };
-    bf16 ? go(std::true_type{}) : go(std::false_type{});
+    with_rank(s.rt, [&](auto rt) { bf16 ? go(std::true_type{}, rt) : go(std::false_type{}, rt); });
+    ReduceArgs r = {};
+    r.job[0] = {gb.part, dB, scale, 1.f, m.n_out, static_cast<int>(ceil_div(m.n_out, 1024))};
+    r.job[1] = {ga.part, dA, scale, d.scale, m.n_in, static_cast<int>(ceil_div(m.n_in, 1024))};
+    r.head = pv.head;
+    r.first = pv.first[1];
+    r.runs = s.runs;
+    r.rows = pv.rows;
+    r.n = m.n;
+    r.rank = m.rank;
+    r.rp = s.rp;
+    r.accumulate = accumulate;
+    k_reduce<<<dim3(static_cast<unsigned>(m.n * m.rank), static_cast<unsigned>(r.job[0].slices + r.job[1].slices)), 256, 0, st>>>(r);
     return hipGetLastError();
 }
 
