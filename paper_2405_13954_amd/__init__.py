@@ -160,20 +160,25 @@ def lib():
 
 
 # ------------------------------------------------------------------ helpers --
+_torch_module = None
+_dtype_codes = {}
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _dtype_codes.update({torch.bfloat16: BF16, torch.float32: F32, torch.float64: F64})
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
-    torch = _torch()
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.float64:
-        return F64
-    raise TypeError(f"unsupported dtype {t.dtype} (bfloat16, float32 or float64)")
+    _torch()
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype} (bfloat16, float32 or float64)")
+    return code
 
 
 def _ptr(t):
