@@ -1,0 +1,116 @@
+"""Adapters at sizes whose launches take the kernels' other forms (taller tiles, several ranges of the long axis, runs
+that pass from one adapter to the next), against float64 products on the GPU, with the bounds of the small tests; and
+the edges of the plan's and the workspace's memory."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -23
+
+
+def _inputs(rows, n_in, n_out, rank, n, dtype, p, seed=0):
+    import torch
+    import paper_2405_13954_amd as P
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    mk = lambda std, *s: (torch.randn(s, generator=g, device="cuda") * std).to(dt)  # noqa: E731
+    c = dict(x=mk(1.0, rows, n_in), dy=mk(0.1, rows, n_out), a=mk(n_in ** -0.5, n, rank, n_in),
+             b=mk(rank ** -0.5, n, rank, n_out), base=mk(1.0, rows, n_out), back=mk(0.1, rows, n_in),
+             scale=torch.rand(n, generator=g, device="cuda") + 0.5)
+    # requests of ragged lengths in no order, a tenth of them without an adapter
+    cuts = np.sort(np.random.default_rng(seed).choice(np.arange(1, rows), 37, replace=False))
+    ids = torch.zeros(rows, dtype=torch.int32)
+    for i, (lo, hi) in enumerate(zip([0, *cuts], [*cuts, rows])):
+        ids[lo:hi] = -1 if i % 10 == 9 else (i * 7) % n
+    c["ids"] = ids.cuda()
+    c["kw"] = dict(p=p, seed=5, offset=6)
+    c["f"] = torch.ones(rows, n_in, device="cuda", dtype=torch.double)
+    if p:
+        one = torch.ones(rows, n_in, device="cuda")
+        P.logra_dropout(one, one, p, 5, 6)
+        c["f"] = one.double()
+    return c
+
+
+def _within(got, want, bound, what):
+    over = ((got.double() - want).abs() - bound).max()
+    assert float(over) <= 0.0, f"{what}: {float(over):.3e} beyond the bound"
+
+
+SHAPES = [(8300, 264, 520, 9, 3), (8300, 520, 264, 20, 5), (8300, 264, 520, 40, 2), (8300, 136, 520, 100, 2),
+          (17000, 264, 264, 16, 6), (2500, 4096, 136, 16, 4), (900, 136, 4096, 24, 2)]
+
+
+@pytest.mark.parametrize("p", [0.0, 0.1])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward_and_backward(shape, dtype, p):
+    import torch
+    import paper_2405_13954_amd as P
+    rows, n_in, n_out, rank, n = shape
+    print("[adapters]", shape, dtype, p, flush=True)
+    c = _inputs(*shape, dtype, p)
+    plan = P.logra_adapter_plan(c["ids"], n)
+    y, u = torch.empty_like(c["base"]), torch.empty(rows, rank, device="cuda")
+    P.logra_adapter_forward(c["x"], c["a"], c["b"], plan, y, base=c["base"], scale=c["scale"], u=u, **c["kw"])
+    da, db, dx = (torch.empty(t.shape, device="cuda", dtype=d) for t, d in
+                  ((c["a"], torch.float32), (c["b"], torch.float32), (c["back"], c["back"].dtype)))
+    P.logra_adapter_backward(c["x"], c["dy"], c["a"], c["b"], plan, u, da, db, dx=dx, base=c["back"], scale=c["scale"], **c["kw"])
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    operand = 2.0 ** -16 if dtype == "bf16" else 0.0
+    x, dy, base, back = c["x"].double() * c["f"], c["dy"].double(), c["base"].double(), c["back"].double()
+    u64, ua = torch.zeros(rows, rank, device="cuda", dtype=torch.double), torch.zeros(rows, rank, device="cuda", dtype=torch.double)
+    y64, ya, dx64, dxa = base.clone(), base.abs(), torch.zeros_like(back), torch.zeros_like(back)
+    for i in range(n):
+        at = torch.nonzero(c["ids"] == i)[:, 0]
+        A, B, s = c["a"][i].double(), c["b"][i].double(), float(c["scale"][i])
+        u64[at], ua[at] = x[at] @ A.T, x[at].abs() @ A.abs().T
+        y64[at] += s * (u64[at] @ B)
+        ya[at] += s * (ua[at] @ B.abs())
+        du, dua = s * (dy[at] @ B.T), s * (dy[at].abs() @ B.abs().T)
+        dx64[at], dxa[at] = du @ A, dua @ A.abs()
+        count = len(at)
+        _within(da[i], du.T @ x[at], (count + n_out + 16) * EPS * (dua.T @ x[at].abs()), f"dA of {i}")
+        ui = u[at].double()
+        _within(db[i], s * (ui.T @ dy[at]), (count + n_in + 16) * EPS * s * (ui.abs().T @ dy[at].abs()), f"dB of {i}")
+    _within(u, u64, (n_in + 8) * EPS * ua, "u")
+    _within(y, y64, ((n_in + rank + 8) * EPS + operand) * ya + half * y64.abs(), "y")
+    dx64, dxa = back + dx64 * c["f"], back.abs() + dxa * c["f"]
+    _within(dx, dx64, ((n_out + rank + 8) * EPS + operand) * dxa + half * dx64.abs(), "dx")
+
+
+@pytest.mark.parametrize("shape", [(1, 8, 8, 1, 1), (3000, 264, 136, 16, 1023), (5000, 512, 520, 64, 7), (300, 64, 4096, 100, 40),
+                                   (17000, 64, 64, 8, 2)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_memory_of_plan_and_workspace(shape, dtype):
+    # plan and workspace are exactly as large as asked for, inside a larger buffer whose other bytes must stay
+    import torch
+    import paper_2405_13954_amd as P
+    rows, n_in, n_out, rank, n = shape
+    print("[memory]", shape, dtype, flush=True)
+
+    def guarded(size):
+        full = torch.full((size + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+        return full, full[4096:4096 + size]
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda").to(dt)  # noqa: E731
+    full_plan, plan = guarded(P.logra_adapter_plan_size(rows, n))
+    full_ws, ws = guarded(P.logra_adapter_ws_size(rows, n_in, n_out, rank, n))
+    ids = torch.randint(-1, n, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    P.logra_adapter_plan(ids, n, plan=plan)
+    x, a, b, y, u = mk(rows, n_in), mk(n, rank, n_in), mk(n, rank, n_out), mk(rows, n_out), torch.empty(rows, rank, device="cuda")
+    full_da, da = guarded(n * rank * n_in * 4)
+    full_db, db = guarded(n * rank * n_out * 4)
+    da, db = da.view(torch.float32).view(n, rank, n_in), db.view(torch.float32).view(n, rank, n_out)
+    for p in (0.0, 0.3):
+        P.logra_adapter_forward(x, a, b, plan, y, base=y, u=u, p=p, seed=1, ws=ws)
+        P.logra_adapter_backward(x, y, a, b, plan, u, da, db, dx=torch.empty_like(x), p=p, seed=1, ws=ws)
+        P.logra_adapter_backward(x, y, a, b, plan, u, da, db, p=p, seed=1, ws=ws)
+    torch.cuda.synchronize()
+    for full, what in ((full_plan, "plan"), (full_ws, "workspace"), (full_da, "dA"), (full_db, "dB")):
+        assert bool((full[:4096] == 0xA5).all()) and bool((full[-4096:] == 0xA5).all()), f"a store outside the {what}"
+    assert bool(torch.isfinite(da).all()) and bool(torch.isfinite(db).all())
