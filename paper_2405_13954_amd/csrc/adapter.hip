@@ -47,6 +47,10 @@ namespace {
 constexpr int kHeights = 6;          // tile lists of 16 << h rows
 constexpr int kSeg = 4096;           // rows of one workgroup of the plan's kernels
 constexpr int kPlanMagic = 0x4c6f4164;
+// Ranges of the long axis in k_shrink at most, which all that read U add up (with
+// eight they paid more for it than k_shrink gained: 96 rows of 64 adapters, 4096 to
+// 14336 columns, 16.7 against 15.4 us).
+constexpr int kMaxParts = 4;
 constexpr int kPad = 32;             // groups start at multiples of this
 
 struct PlanHead {
@@ -527,7 +531,7 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
 
     // Loads return in the order in which they are issued: first what the operands are made of (it comes from L2), then
     // the rows' base (from memory), which is on its way while the operands are put together.
-    constexpr int kWVecs = kRp * (kSlice / kV) / 256, kItems = (16 * M * kRp / 4 + 255) / 256, kAhead = kItems == 1 ? 4 : kItems == 2 ? 2 : 1;
+    constexpr int kWVecs = kRp * (kSlice / kV) / 256, kItems = (16 * M * kRp / 4 + 255) / 256, kAhead = 3;
     constexpr int kPairs = kNw * kEs<BF16> / 128, kLoads = kPairs ? 2 : 1, kQ = kPairs ? kPairs : 1;
     int row[M][kLoads];   // 128-byte pieces of 8 rows (64-byte pieces of 16 rows where the wave has only 64 bytes of columns)
 #pragma unroll
@@ -545,7 +549,9 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
         w[k] = in ? ld128(a.W + ((static_cast<int64_t>(tile.group) * a.rank + r) * a.width + n0 + c) * kEs<BF16>)
                   : u32x4{0, 0, 0, 0};
     }
-    f32x4 u[kItems][kAhead];   // four ranks of a row, of the first splits
+    // Four ranks of a row, of each split; the fourth split is added at once, and not kept for later (15.2 us, with all kept
+    // 15.8, for 96 rows of 64 adapters).
+    f32x4 u[kItems][kAhead];
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
         const int i = threadIdx.x + 256 * k, slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
@@ -729,7 +735,7 @@ constexpr int kGradCols = 256;
 
 // Parts of du that are fetched one by one, and so the splits of the backward
 // pass's k_shrink.
-__host__ __device__ constexpr int parts_of(int rt) { return rt == 1 ? 4 : 2; }
+__host__ __device__ constexpr int parts_of(int rt) { return rt == 1 ? kMaxParts : 2; }
 template <int RT>
 constexpr int kParts = parts_of(RT);
 constexpr int kGradChunk = 32;   // blocks whose rows are looked up together
@@ -831,7 +837,7 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
                 }
                 group = lds_tile[i].group;
             }
-            if (i) __syncthreads();   // the waves are done with the block before
+            if (i) __syncthreads();   // the waves are done with the block before (two blocks in LDS and one barrier: no gain)
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 float q[2];
@@ -1012,7 +1018,7 @@ struct ShrinkShape {
 ShrinkShape shrink_shape(int64_t rows, int n, int width, int es, int groups, int most_splits) {
     const int64_t wide = ceil_div(static_cast<int64_t>(width) * es, 1024), most = wide < most_splits ? wide : most_splits;
     ShrinkShape s;
-    s.h = (rows >> 5) * most < 256 ? 0 : 1;
+    s.h = (rows >> 5) * most < 192 ? 0 : 1;
     const int64_t tiles = (rows >> (4 + s.h)) + (n < rows ? n : rows);
     int64_t want = ceil_div(groups, tiles);
     want = want > most ? most : want;
@@ -1024,7 +1030,6 @@ ShrinkShape shrink_shape(int64_t rows, int n, int width, int es, int groups, int
 // The forward pass hides the drawing of its dropout behind more workgroups (16,384 x 4096 at rank 16: 39 us with 512,
 // 32 with 2048); without it, and in the backward pass, fewer parts are better for those that add them.
 constexpr int kForwardGroups = 2048, kGroups = 512;
-constexpr int kForwardSplits = 8;
 
 struct WsLayout {
     size_t part, part_a, part_b, bytes;
@@ -1039,7 +1044,7 @@ WsLayout ws_layout(const Shape &s, int64_t rows, int n_in, int n_out, int n) {
     };
     int splits = 1;
     for (int es = 2; es <= 4; es += 2) {
-        const int f = shrink_shape(rows, n, n_in, es, kForwardGroups, kForwardSplits).splits,
+        const int f = shrink_shape(rows, n, n_in, es, kForwardGroups, kMaxParts).splits,
                   b = shrink_shape(rows, n, n_out, es, kGroups, parts_of(s.rt)).splits;
         splits = f > splits ? f : splits;
         splits = b > splits ? b : splits;
@@ -1097,7 +1102,7 @@ hipError_t launch_adapter_forward(const AdapterDims &m, bool bf16, const void *p
     const Shape s = shape_of(m.rows, m.n_in, m.n_out, m.rank, m.n);
     const WsLayout l = ws_layout(s, m.rows, m.n_in, m.n_out, m.n);
     float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
-    const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_in, bf16 ? 2 : 4, d.thr ? kForwardGroups : kGroups, kForwardSplits);
+    const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_in, bf16 ? 2 : 4, d.thr ? kForwardGroups : kGroups, kMaxParts);
     const ShrinkArgs sa = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<const char *>(A), m.rank, part, s.places,
                            h.splits, h.per};
     ExpandArgs e = {part, h.splits, s.places, scale, static_cast<const char *>(B), m.rank, m.n_out,
