@@ -530,6 +530,8 @@ int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype
  * Sums are fp32, in an order that depends on the sizes and the rows' order
  * alone: reruns are bitwise identical.  The rounding of u and du to matrix
  * operands leaves 16 significant bits in y and dx, and all 24 in dA and dB.
+ * A row whose u or du is infinite may get NaN where the formulas give an
+ * infinity (its operands are differences); other rows' y and dx are unaffected.
  *
  * ws: logra_adapter_ws_size bytes for either call (contents on entry are
  * ignored; calls that overlap need their own).  Limits: n_in, n_out multiples of

@@ -9,42 +9,47 @@
 // contiguous as the projections P_in and P_out of this library are.  So the
 // forward and the backward pass are made of the same three products:
 //
-//   k_shrink   U[t][r]  = sum_j W_a[r][j] v_t[j]            (x with A, dy with B)
-//   k_expand   out_t[j] = base_t[j] + sum_r U[t][r] W_a[r][j]   (B, then A)
-//   k_grad     dW_a[r][j] = sum_t U[t][r] v_t[j]            (dy with u, x with du)
+//   shrink   U[t][r]  = sum_j W_a[r][j] v_t[j]                  (x with A, dy with B)
+//   expand   out_t[j] = base_t[j] + sum_r U[t][r] W_a[r][j]     (B, then A)
+//   grad     dW_a[r][j] = sum_t U[t][r] v_t[j]                  (dy with u, x with du)
 //
-// All are bound by memory (2 rank multiply-adds for each element of x or y):
-// the design keeps every element of x, dy, base, y read or written once by
-// each product, and the weights in L2.
+// All are bound by memory (2 rank multiply-adds for each element of x or y): the
+// design has each product read or write every element of x, dy, base and y once,
+// and keeps the weights in L2.  Few rows are bound by latency: each product is
+// one launch, shared by the two that can run together.
 //
 //  0. k_plan_*: groups the rows of a batch by adapter, stably (so that sums run
 //     in row order, and reruns give the same bits).  Each group starts at a
-//     multiple of 32 in the order, and lists of its tiles of 16, 32, .. 512 rows
-//     let a workgroup find its rows with one load.  Kernels that get memory which
-//     is no plan for their sizes do nothing.
-//  1. k_shrink: a workgroup owns a tile of 16 M rows and a range of the long
+//     multiple of 32 in the order, and lists of its tiles of 16 and 32 rows let
+//     a workgroup find its rows with one load.  Kernels that get memory which is
+//     no plan for their sizes do nothing.
+//  1. shrink: a workgroup owns a tile of 16 or 32 rows and a range of the long
 //     axis, its four waves taking 128-byte pieces of it in turn; the waves' sums
 //     are added through LDS.  Few rows: the axis is split over workgroups, whose
-//     partial sums the next kernel adds in order.
-//  2. k_expand: a workgroup owns 16 M rows and a slice of columns; W's slice is
-//     put in LDS once, U comes as MFMA operands straight from memory.  A bf16 W
-//     takes U as two bf16 halves (about 16 significant bits, so that U's rounding
-//     stays far below that of the output); rank 16 then fills the 32-deep
-//     contraction of one MFMA exactly.  fp32 uses fp32 MFMAs.
-//  3. k_prep (backward): sums the partial du, applies s_a, and for bf16 lays u and
-//     du out by rank as three bf16 thirds (24 significant bits: the gradients are
-//     fp32, so nothing of u and du may be lost), the operands of k_grad.
-//  4. k_grad: a workgroup owns a chunk of an adapter's rows and 256 columns; 32
-//     rows at a time go through LDS, where transposed reads (bf16:
-//     ds_read_b64_tr_b16) turn them into operands whose contraction runs over
-//     rows.  k_reduce adds the chunks' sums in order.
+//     parts those that read U add in order.  16,384 x 4096 bf16 at rank 16: 24 us
+//     (5.6 TB/s), 31 with the dropout of x drawn on the way.
+//  2. expand: a workgroup owns 16 or 32 rows and a slice of columns; W's slice is
+//     put in LDS once, and U as MFMA operands.  A bf16 W takes U as two bf16
+//     halves (16 significant bits, so that U's rounding stays far below that of
+//     the output); rank 16 then fills the 32-deep contraction of one MFMA exactly.
+//     fp32 uses fp32 MFMAs.  16,384 x 4096 bf16 at rank 16: 57 us for 268 MB
+//     (4.7 TB/s; a copy in the same pieces takes 48).
+//  3. grad: a workgroup owns a run of an order's blocks of 32 rows and 256
+//     columns; a block goes through LDS, where transposed reads (bf16:
+//     ds_read_b64_tr_b16) turn it into operands whose contraction runs over
+//     rows.  A bf16 v takes U as three bf16 thirds (24 significant bits: the
+//     gradients are fp32, so nothing of u and du may be lost).  k_reduce adds the
+//     runs' sums in order.
+//  Forward: k_shrink, k_expand.  Backward: k_back_dy (du and dB, both of which
+//  read dy), k_back_x (dx and dA), k_reduce: 16,384 rows, 4096 + 4096 columns,
+//  rank 16: 46 + 80 + 7 us for the 537 MB that the pass cannot do without.
 #include "counter_rng.h"
 #include "internal.h"
 
 namespace logra {
 namespace {
 
-constexpr int kHeights = 6;          // tile lists of 16 << h rows
+constexpr int kHeights = 2;          // tile lists of 16 << h rows
 constexpr int kSeg = 4096;           // rows of one workgroup of the plan's kernels
 constexpr int kPlanMagic = 0x4c6f4164;
 // Ranges of the long axis in k_shrink at most, which all that read U add up (with
@@ -59,7 +64,7 @@ struct PlanHead {
     int tiles_all[kHeights];         // and of the rows without one, which come last
 };
 struct Tile {
-    int group, p0, count, index;     // adapter, first place in the order, rows, number within the group
+    int group, p0, count, pad;       // adapter, first place in the order, rows; 16 bytes, one load
 };
 
 // The plan's memory: head, row of each place (-1: a pad), tile lists, each
@@ -95,7 +100,8 @@ PlanLayout plan_layout(int64_t rows, int n) {
         return here;
     };
     l.row_of = take(static_cast<size_t>(plan_places(rows, n)) * 4);
-    for (int h = 0; h < kHeights; ++h) l.tiles[h] = take(static_cast<size_t>(plan_max_tiles(rows, n, h)) * sizeof(Tile));
+    for (int h = 0; h < kHeights; ++h)
+        l.tiles[h] = take(static_cast<size_t>(plan_max_tiles(rows, n, h)) * sizeof(Tile));
     for (int h = 0; h < kHeights; ++h) l.first[h] = take(static_cast<size_t>(n + 2) * 4);
     l.start = take(static_cast<size_t>(n + 2) * 4);
     l.hist = take(static_cast<size_t>((rows + kSeg - 1) / kSeg) * (n + 1) * 4);
@@ -222,7 +228,7 @@ __global__ __launch_bounds__(1024) void k_plan_scan(PlanView v, int segs) {
                     hi = mid;
             }
             const int i = t - lds_first[lo], left = lds_count[lo] - i * height;
-            v.tiles[h][t] = {lo, lds_start[lo] + i * height, left < height ? left : height, i};
+            v.tiles[h][t] = {lo, lds_start[lo] + i * height, left < height ? left : height, 0};
         }
         __syncthreads();
     }
@@ -238,7 +244,8 @@ __global__ __launch_bounds__(256) void k_plan_scatter(const int *row_adapter, Pl
     __syncthreads();
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kSeg + wave * (kSeg / 4);
     for (int i = 0; i < kSeg / 4; i += 64)
-        if (at + i + lane < v.rows) atomicAdd(&next[wave][group_of(row_adapter, static_cast<int>(at + i + lane), v.n)], 1);
+        if (at + i + lane < v.rows)
+            atomicAdd(&next[wave][group_of(row_adapter, static_cast<int>(at + i + lane), v.n)], 1);
     __syncthreads();
     for (int g = threadIdx.x; g < groups; g += 256) {
         int p = v.start[g] + v.hist[static_cast<int64_t>(blockIdx.x) * groups + g];
@@ -302,6 +309,16 @@ inline dim3 block_grid(int64_t blocks) {
     return dim3(static_cast<unsigned>(x), static_cast<unsigned>((blocks + x - 1) / x));
 }
 
+__device__ __forceinline__ u32x4 zeros() { return u32x4{0, 0, 0, 0}; }
+__device__ __forceinline__ f32x4 zeros4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+__device__ __forceinline__ f32x4 ldf4(const void *p) { return *reinterpret_cast<const f32x4 *>(p); }
+__device__ __forceinline__ float ldf(const void *p) { return *reinterpret_cast<const float *>(p); }
+__device__ __forceinline__ void stf4(void *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+__device__ __forceinline__ void st128(void *p, u32x4 v) { *reinterpret_cast<u32x4 *>(p) = v; }
+__device__ __forceinline__ void st128_nt(void *p, u32x4 v) {
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+}
+
 // ----------------------------------------------------------------- shrink --
 template <bool BF16>
 constexpr int kEs = BF16 ? 2 : 4;
@@ -341,7 +358,8 @@ constexpr int kShrinkLds = 4 * 16 * M * 16 * RT * 4;
 // Block `index`: tile and range of the long axis; part = the sum over the range
 // of W_a[r][j] drop(v_t[j]).
 template <bool BF16, int M, int RT, bool DROP>
-__device__ __forceinline__ void shrink(const TileList &list, const ShrinkArgs &a, const DropArgs &d, uint32_t index, char *lds) {
+__device__ __forceinline__ void shrink(const TileList &list, const ShrinkArgs &a, const DropArgs &d, uint32_t index,
+                                       char *lds) {
     constexpr int kRp = 16 * RT, kUnit = 8 * kVec<BF16>;   // 128 bytes of a row
     float(*red)[16 * M][kRp] = reinterpret_cast<float(*)[16 * M][kRp]>(lds);
     const int at = index / a.splits, split = index - at * a.splits;
@@ -375,7 +393,7 @@ __device__ __forceinline__ void shrink(const TileList &list, const ShrinkArgs &a
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) acc[m][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < RT; ++r) acc[m][r] = zeros4();
 
     struct Piece {
         u32x4 x[2][M], w[2][RT];
@@ -385,11 +403,12 @@ __device__ __forceinline__ void shrink(const TileList &list, const ShrinkArgs &a
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t off = static_cast<int64_t>(j) * kEs<BF16>;
-            const bool in_x = whole || j + pair_col() * kVec<BF16> < end, in_w = whole || j + (4 * h + g) * kVec<BF16> < end;
+            const bool in_x = whole || j + pair_col() * kVec<BF16> < end;
+            const bool in_w = whole || j + (4 * h + g) * kVec<BF16> < end;
 #pragma unroll
-            for (int m = 0; m < M; ++m) p.x[h][m] = in_x ? ld128_nt(vp[m][h] + off) : u32x4{0, 0, 0, 0};
+            for (int m = 0; m < M; ++m) p.x[h][m] = in_x ? ld128_nt(vp[m][h] + off) : zeros();
 #pragma unroll
-            for (int r = 0; r < RT; ++r) p.w[h][r] = in_w ? ld128(wp[r] + off + 64 * h) : u32x4{0, 0, 0, 0};
+            for (int r = 0; r < RT; ++r) p.w[h][r] = in_w ? ld128(wp[r] + off + 64 * h) : zeros();
         }
     };
     const auto multiply = [&](Piece &p, int j) {
@@ -398,7 +417,8 @@ __device__ __forceinline__ void shrink(const TileList &list, const ShrinkArgs &a
             if constexpr (DROP) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    p.x[h][m] = drop_piece<BF16>(d, p.x[h][m], static_cast<uint32_t>(row[m][h]), j + pair_col() * kVec<BF16>);
+                    p.x[h][m] = drop_piece<BF16>(d, p.x[h][m], static_cast<uint32_t>(row[m][h]),
+                                                 j + pair_col() * kVec<BF16>);
             }
             swap8(p.x[0][m], p.x[1][m]);
         }
@@ -433,19 +453,19 @@ __device__ __forceinline__ void shrink(const TileList &list, const ShrinkArgs &a
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4 *>(&red[wave][16 * m + t][16 * r + 4 * g]) = acc[m][r];
+        for (int r = 0; r < RT; ++r) stf4(&red[wave][16 * m + t][16 * r + 4 * g], acc[m][r]);
     __syncthreads();
     const float f = DROP ? d.scale : 1.f;
     float *out = a.part + (static_cast<int64_t>(split) * a.places + tile.p0) * kRp;
     for (int i = threadIdx.x; i < 16 * M * kRp / 4; i += 256) {
         const int slot = i / (kRp / 4), r = i % (kRp / 4) * 4;
         if (slot >= tile.count) break;
-        f32x4 s = *reinterpret_cast<f32x4 *>(&red[0][slot][r]);
+        f32x4 s = ldf4(&red[0][slot][r]);
 #pragma unroll
-        for (int w = 1; w < 4; ++w) s += *reinterpret_cast<f32x4 *>(&red[w][slot][r]);
+        for (int w = 1; w < 4; ++w) s += ldf4(&red[w][slot][r]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] = r + e < rank ? s[e] * f : 0.f;
-        *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(slot) * kRp + r) = s;
+        stf4(out + static_cast<int64_t>(slot) * kRp + r, s);
     }
 }
 
@@ -504,7 +524,8 @@ constexpr int kExpandLds = 16 * RT * kWPitch<BF16, RT> + 16 * M * kURow<RT>;
 
 // Block `index`: tile of 16 M rows and slice of four waves' columns.
 template <bool BF16, int M, int RT, bool DROP>
-__device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a, const DropArgs &d, uint32_t index, char *lds) {
+__device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a, const DropArgs &d, uint32_t index,
+                                       char *lds) {
     constexpr int kRp = 16 * RT, kNw = kCols<BF16, RT>, kSlice = kSliceCols<BF16, RT>, kPitch = kWPitch<BF16, RT>;
     constexpr int kV = kVec<BF16>, kUPitch = kURow<RT>;
     char *lds_w = lds, *lds_u = lds + kRp * kPitch;
@@ -523,8 +544,8 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
             const int64_t row = list.row_of[tile.p0 + i / (kSlice / kV)];
             const int col = n0 + i % (kSlice / kV) * kV;
             if (col >= a.width) continue;
-            const u32x4 b = a.base ? ld128_nt(a.base + (row * a.ld_b + col) * kEs<BF16>) : u32x4{0, 0, 0, 0};
-            __builtin_nontemporal_store(b, reinterpret_cast<u32x4 *>(a.out + (row * a.ld_o + col) * kEs<BF16>));
+            const u32x4 b = a.base ? ld128_nt(a.base + (row * a.ld_b + col) * kEs<BF16>) : zeros();
+            st128_nt(a.out + (row * a.ld_o + col) * kEs<BF16>, b);
         }
         return;
     }
@@ -533,7 +554,8 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
     // the rows' base (from memory), which is on its way while the operands are put together.
     constexpr int kWVecs = kRp * (kSlice / kV) / 256, kItems = (16 * M * kRp / 4 + 255) / 256, kAhead = 3;
     constexpr int kPairs = kNw * kEs<BF16> / 128, kLoads = kPairs ? 2 : 1, kQ = kPairs ? kPairs : 1;
-    int row[M][kLoads];   // 128-byte pieces of 8 rows (64-byte pieces of 16 rows where the wave has only 64 bytes of columns)
+    // 128-byte pieces of 8 rows (64-byte pieces of 16 rows where the wave has only 64 bytes of columns)
+    int row[M][kLoads];
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
@@ -547,10 +569,10 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
         const int i = threadIdx.x + 256 * k, r = i / (kSlice / kV), c = i % (kSlice / kV) * kV;
         const bool in = r < a.rank && n0 + c < a.width;
         w[k] = in ? ld128(a.W + ((static_cast<int64_t>(tile.group) * a.rank + r) * a.width + n0 + c) * kEs<BF16>)
-                  : u32x4{0, 0, 0, 0};
+                  : zeros();
     }
-    // Four ranks of a row, of each split; the fourth split is added at once, and not kept for later (15.2 us, with all kept
-    // 15.8, for 96 rows of 64 adapters).
+    // Four ranks of a row, of each split; the fourth split is added at once, and not kept for later (15.2 us, with all
+    // kept 15.8, for 96 rows of 64 adapters).
     f32x4 u[kItems][kAhead];
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
@@ -558,10 +580,10 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
         const float *up = a.part + (static_cast<int64_t>(tile.p0) + slot) * kRp + r;
 #pragma unroll
         for (int c = 0; c < kAhead; ++c)
-            u[k][c] = slot < tile.count && c < a.splits ? *reinterpret_cast<const f32x4 *>(up + c * a.places * kRp)
-                                                        : f32x4{0.f, 0.f, 0.f, 0.f};
+            u[k][c] = slot < tile.count && c < a.splits ? ldf4(up + c * a.places * kRp)
+                                                        : zeros4();
         for (int c = kAhead; c < a.splits; ++c)
-            if (slot < tile.count) u[k][0] += *reinterpret_cast<const f32x4 *>(up + c * a.places * kRp);
+            if (slot < tile.count) u[k][0] += ldf4(up + c * a.places * kRp);
     }
     const float s = a.scale ? a.scale[tile.group] : 1.f;
     const int w0 = n0 + wave * kNw, col0 = w0 + (kPairs ? pair_col() : g) * kV;
@@ -575,13 +597,13 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
                 const int col = col0 + 8 * q * kV;
                 base[m][q][h] = a.base && row[m][h] >= 0 && col < a.width
                                     ? ld128_nt(a.base + (row[m][h] * a.ld_b + col) * kEs<BF16>)
-                                    : u32x4{0, 0, 0, 0};
+                                    : zeros();
             }
 
 #pragma unroll
     for (int k = 0; k < kWVecs; ++k) {
         const int i = threadIdx.x + 256 * k, r = i / (kSlice / kV), c = i % (kSlice / kV) * kV;
-        *reinterpret_cast<u32x4 *>(lds_w + r * kPitch + c * kEs<BF16>) = w[k];
+        st128(lds_w + r * kPitch + c * kEs<BF16>, w[k]);
     }
     // U: the splits' sums, scaled, as operands
 #pragma unroll
@@ -605,7 +627,7 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
             o[kRp / 2] = pack2(left_over(v[0]), left_over(v[1]));
             o[kRp / 2 + 1] = pack2(left_over(v[2]), left_over(v[3]));
         } else {
-            *reinterpret_cast<f32x4 *>(lds_u + slot * kUPitch + 4 * r) = v;
+            stf4(lds_u + slot * kUPitch + 4 * r, v);
         }
     }
     __syncthreads();
@@ -633,7 +655,7 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
         if (16 * m >= tile.count) break;
         f32x4 acc[kBlocks];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int b = 0; b < kBlocks; ++b) acc[b] = zeros4();
         const char *lu = lds_u + (16 * m + t) * kUPitch;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -642,13 +664,13 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) acc[b] = mfma16_bf16(as_bf16x8(wf[b][r]), as_bf16x8(uf), acc[b]);
             } else {
-                const f32x4 uf = *reinterpret_cast<const f32x4 *>(lu + (16 * r + 4 * g) * 4);
+                const f32x4 uf = ldf4(lu + (16 * r + 4 * g) * 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const char *lw = lds_w + (16 * r + 4 * g + e) * kPitch + (wave * kNw + t) * 4;
 #pragma unroll
                     for (int b = 0; b < kBlocks; ++b)
-                        acc[b] = mfma16_f32(*reinterpret_cast<const float *>(lw + 64 * b), uf[e], acc[b]);
+                        acc[b] = mfma16_f32(ldf(lw + 64 * b), uf[e], acc[b]);
                 }
             }
         }
@@ -675,7 +697,8 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
             if constexpr (BF16) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    o[e] = pack2(y[2 * e] + __uint_as_float(b[e] << 16), y[2 * e + 1] + __uint_as_float(b[e] & 0xFFFF0000u));
+                    o[e] = pack2(y[2 * e] + __uint_as_float(b[e] << 16),
+                                 y[2 * e + 1] + __uint_as_float(b[e] & 0xFFFF0000u));
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(y[e] + __uint_as_float(b[e]));
@@ -697,7 +720,7 @@ __device__ __forceinline__ void expand(const TileList &list, const ExpandArgs &a
 #pragma unroll
             for (int h = 0; h < kLoads; ++h)
                 if (row[m][h] >= 0 && col < a.width)
-                    __builtin_nontemporal_store(o[h], reinterpret_cast<u32x4 *>(a.out + (row[m][h] * a.ld_o + col) * kEs<BF16>));
+                    st128_nt(a.out + (row[m][h] * a.ld_o + col) * kEs<BF16>, o[h]);
         }
     }
 }
@@ -717,7 +740,9 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
 // empty: there are at most as many as blocks.
 constexpr uint32_t kMaxRuns = 1024;   // with the 2^19 + 1023 blocks at most, products fit 32 bits
 __device__ __forceinline__ uint32_t run_begin(uint32_t blocks, uint32_t i, uint32_t n) { return blocks * i / n; }
-__device__ __forceinline__ uint32_t run_of(uint32_t blocks, uint32_t j, uint32_t n) { return ((j + 1) * n - 1) / blocks; }
+__device__ __forceinline__ uint32_t run_of(uint32_t blocks, uint32_t j, uint32_t n) {
+    return ((j + 1) * n - 1) / blocks;
+}
 
 struct GradArgs {
     const char *v;            // rows x or dy
@@ -748,7 +773,8 @@ constexpr int kGradLds = 32 * kVPitch<BF16> + kULds<BF16, RT> + kGradChunk * (32
 
 // Block `index`: run and slice of kGradCols columns of v.
 template <bool BF16, int RT, bool DROP>
-__device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, const DropArgs &d, uint32_t index, char *lds) {
+__device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, const DropArgs &d, uint32_t index,
+                                     char *lds) {
     constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kVPitch<BF16>;
     constexpr int kLoads = 32 * (kGradCols / kV) / 256;      // 16-byte loads of a thread for 32 rows
     constexpr int kRowsPer = 32 / kLoads;                    // rows that the workgroup loads at once
@@ -767,8 +793,9 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
     const int lr = threadIdx.x / (kGradCols / kV), lc = threadIdx.x % (kGradCols / kV) * kV;
     const bool in = n0 + lc < a.width;
     const int ur = threadIdx.x & 15, up = threadIdx.x >> 4;   // rank within 16 and pair of places that the thread loads
-    // The next block is on its way while one is multiplied (two ahead measured the same).  Every lane loads: for a pad, and beyond the rank or the width, something
-    // of the block's first row or the first column, which is put aside when it is used.
+    // The next block is on its way while one is multiplied (two ahead measured the same).  Every lane loads: for a pad,
+    // and beyond the rank or the width, something of the block's first row or the first column, which is put aside when
+    // it is used.
     struct Fetch {
         float u[kParts<RT>][RT][2];
         u32x4 v[kLoads];
@@ -780,7 +807,8 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
         for (int e = 0; e < 2; ++e) {
             const int row = lds_row[32 * i + 2 * up + e];
             const int64_t place = static_cast<int64_t>(lds_tile[i].p0) + (row < 0 ? 0 : 2 * up + e);
-            const float *q = a.splits ? a.U + place * kRp + ur : a.U + static_cast<int64_t>(row < 0 ? first : row) * a.rank;
+            const float *q = a.splits ? a.U + place * kRp + ur
+                                      : a.U + static_cast<int64_t>(row < 0 ? first : row) * a.rank;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const int k = 16 * r + ur, known = k < a.rank ? k : 0;
@@ -803,7 +831,7 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) acc[b][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < RT; ++r) acc[b][r] = zeros4();
     };
     // lane holds columns 4 g .. + 3 of block b for rank 16 r + t
     const auto flush = [&](int group) {
@@ -814,7 +842,7 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
             if (col >= a.width) continue;
 #pragma unroll
             for (int r = 0; r < RT; ++r)
-                *reinterpret_cast<f32x4 *>(out + static_cast<int64_t>(16 * r + t) * a.width + col) = acc[b][r];
+                stf4(out + static_cast<int64_t>(16 * r + t) * a.width + col, acc[b][r]);
         }
     };
     clear();
@@ -837,7 +865,7 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
                 }
                 group = lds_tile[i].group;
             }
-            if (i) __syncthreads();   // the waves are done with the block before (two blocks in LDS and one barrier: no gain)
+            if (i) __syncthreads();   // the waves are done with the block before (two in LDS and one barrier: no gain)
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 float q[2];
@@ -851,7 +879,8 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
                 if constexpr (BF16) {
 #pragma unroll
                     for (int third = 0; third < 3; ++third) {
-                        *reinterpret_cast<uint32_t *>(lds_u + third * kUThird + (16 * r + ur) * kUPitch + 4 * up) = pack2(q[0], q[1]);
+                        char *to = lds_u + third * kUThird + (16 * r + ur) * kUPitch + 4 * up;
+                        *reinterpret_cast<uint32_t *>(to) = pack2(q[0], q[1]);
                         q[0] = left_over(q[0]);
                         q[1] = left_over(q[1]);
                     }
@@ -865,13 +894,14 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
             for (int k = 0; k < kLoads; ++k) {
                 const int slot = kRowsPer * k + lr, row = lds_row[32 * i + slot];
                 if constexpr (DROP) f.v[k] = drop_piece<BF16>(d, f.v[k], static_cast<uint32_t>(row), n0 + lc);
-                *reinterpret_cast<u32x4 *>(lds_v + slot * kPitch + lc * kEs<BF16>) = in && row >= 0 ? f.v[k] : u32x4{0, 0, 0, 0};
+                st128(lds_v + slot * kPitch + lc * kEs<BF16>, in && row >= 0 ? f.v[k] : zeros());
             }
             __syncthreads();
             if (i + 1 < count) load(f, i + 1);
             if constexpr (BF16) {
                 u32x4 vf[4];
-                const uint32_t l0 = lds_addr(lds_v) + static_cast<uint32_t>((8 * g + (t >> 2)) * kPitch + (wave * 64 + 4 * (t & 3)) * 2);
+                const uint32_t l0 = lds_addr(lds_v) + static_cast<uint32_t>((8 * g + (t >> 2)) * kPitch +
+                                                                            (wave * 64 + 4 * (t & 3)) * 2);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     const s16x4 v8[2] = {read_tr(l0 + 32 * b), read_tr(l0 + 32 * b + 4 * kPitch)};
@@ -892,10 +922,10 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
                     float uf[RT];
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
-                        uf[r] = *reinterpret_cast<const float *>(lds_u + (4 * k + g) * kUPitch + (16 * r + t) * 4);
+                        uf[r] = ldf(lds_u + (4 * k + g) * kUPitch + (16 * r + t) * 4);
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
-                        const float vf = *reinterpret_cast<const float *>(lds_v + (4 * k + g) * kPitch + (wave * 64 + 16 * b + t) * 4);
+                        const float vf = ldf(lds_v + (4 * k + g) * kPitch + (wave * 64 + 16 * b + t) * 4);
 #pragma unroll
                         for (int r = 0; r < RT; ++r) acc[b][r] = mfma16_f32(vf, uf[r], acc[b][r]);
                     }
@@ -912,7 +942,8 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
 // (they are few and long), then those of the product that shares its rows:
 // du = B dy beside dB, both of which read dy; then dx beside dA.
 template <bool BF16, int M, int RT>
-__global__ __launch_bounds__(256) void k_back_dy(TileList blocks, GradArgs g, TileList tiles, ShrinkArgs s, DropArgs d) {
+__global__ __launch_bounds__(256) void k_back_dy(TileList blocks, GradArgs g, TileList tiles, ShrinkArgs s,
+                                                 DropArgs d) {
     constexpr int kLds = kGradLds<BF16, RT> > kShrinkLds<M, RT> ? kGradLds<BF16, RT> : kShrinkLds<M, RT>;
     __shared__ __align__(16) char lds[kLds];
     const uint32_t index = block_index(), n = g.runs * g.slices;
@@ -956,7 +987,7 @@ __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
     if (col >= job.width) return;
     const int ad = blockIdx.x / a.rank, r = blockIdx.x % a.rank;
     const uint32_t j0 = a.first[ad], j1 = a.first[ad + 1], blocks = a.first[a.n];
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    f32x4 s = zeros4();
     if (j1 > j0) {
         const uint32_t runs = blocks < static_cast<uint32_t>(a.runs) ? blocks : a.runs;
         const int i0 = run_of(blocks, j0, runs), i1 = run_of(blocks, j1 - 1, runs);
@@ -965,7 +996,7 @@ __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
         for (int i = i0; i <= i1; i += 8) {   // eight loads on their way, added in order
             f32x4 v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = i + k <= i1 ? *reinterpret_cast<const f32x4 *>(p + k * step) : f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < 8; ++k) v[k] = i + k <= i1 ? ldf4(p + k * step) : zeros4();
 #pragma unroll
             for (int k = 0; k < 8; ++k) s += v[k];
             p += 8 * step;
@@ -973,13 +1004,13 @@ __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
     }
     s *= job.f * (job.scale ? job.scale[ad] : 1.f);
     float *out = job.dW + static_cast<int64_t>(blockIdx.x) * job.width + col;
-    if (a.accumulate) s += *reinterpret_cast<const f32x4 *>(out);
-    *reinterpret_cast<f32x4 *>(out) = s;
+    if (a.accumulate) s += ldf4(out);
+    stf4(out, s);
 }
 
 __global__ __launch_bounds__(256) void k_zero(float *p, int64_t quads) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i < quads) reinterpret_cast<f32x4 *>(p)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (i < quads) reinterpret_cast<f32x4 *>(p)[i] = zeros4();
 }
 
 // ------------------------------------------------------------------- host --
@@ -1016,7 +1047,8 @@ struct ShrinkShape {
     int h, splits, per;
 };
 ShrinkShape shrink_shape(int64_t rows, int n, int width, int es, int groups, int most_splits) {
-    const int64_t wide = ceil_div(static_cast<int64_t>(width) * es, 1024), most = wide < most_splits ? wide : most_splits;
+    const int64_t wide = ceil_div(static_cast<int64_t>(width) * es, 1024);
+    const int64_t most = wide < most_splits ? wide : most_splits;
     ShrinkShape s;
     s.h = (rows >> 5) * most < 192 ? 0 : 1;
     const int64_t tiles = (rows >> (4 + s.h)) + (n < rows ? n : rows);
@@ -1103,8 +1135,8 @@ hipError_t launch_adapter_forward(const AdapterDims &m, bool bf16, const void *p
     const WsLayout l = ws_layout(s, m.rows, m.n_in, m.n_out, m.n);
     float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
     const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_in, bf16 ? 2 : 4, d.thr ? kForwardGroups : kGroups, kMaxParts);
-    const ShrinkArgs sa = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<const char *>(A), m.rank, part, s.places,
-                           h.splits, h.per};
+    const ShrinkArgs sa = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<const char *>(A), m.rank, part,
+                           s.places, h.splits, h.per};
     ExpandArgs e = {part, h.splits, s.places, scale, static_cast<const char *>(B), m.rank, m.n_out,
                     static_cast<const char *>(base), ld_b, static_cast<char *>(y), ld_y, u, 0};
     const auto go = [&](auto b, auto rt) {
@@ -1137,7 +1169,8 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
     const DropArgs d = drop_args(drop_p, seed, offset);
     if (m.rows == 0) {   // sums over nothing
         if (!accumulate) {
-            const int64_t na = static_cast<int64_t>(m.n) * m.rank * m.n_in / 4, nb = static_cast<int64_t>(m.n) * m.rank * m.n_out / 4;
+            const int64_t na = static_cast<int64_t>(m.n) * m.rank * m.n_in / 4;
+            const int64_t nb = static_cast<int64_t>(m.n) * m.rank * m.n_out / 4;
             k_zero<<<static_cast<unsigned>((na + 255) / 256), 256, 0, st>>>(dA, na);
             k_zero<<<static_cast<unsigned>((nb + 255) / 256), 256, 0, st>>>(dB, nb);
         }
@@ -1149,12 +1182,12 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
     char *w = static_cast<char *>(ws);
     float *part = reinterpret_cast<float *>(w + l.part);
     const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_out, bf16 ? 2 : 4, kGroups, parts_of(s.rt));
-    const ShrinkArgs sa = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<const char *>(B), m.rank, part, s.places,
-                           h.splits, h.per};
-    const GradArgs gb = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<int>(ceil_div(m.n_out, kGradCols)), u, 0,
-                         s.places, m.rank, reinterpret_cast<float *>(w + l.part_b), s.runs};
-    const GradArgs ga = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<int>(ceil_div(m.n_in, kGradCols)), part,
-                         h.splits, s.places, m.rank, reinterpret_cast<float *>(w + l.part_a), s.runs};
+    const ShrinkArgs sa = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<const char *>(B), m.rank, part,
+                           s.places, h.splits, h.per};
+    const GradArgs gb = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<int>(ceil_div(m.n_out, kGradCols)),
+                         u, 0, s.places, m.rank, reinterpret_cast<float *>(w + l.part_b), s.runs};
+    const GradArgs ga = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<int>(ceil_div(m.n_in, kGradCols)),
+                         part, h.splits, s.places, m.rank, reinterpret_cast<float *>(w + l.part_a), s.runs};
     ExpandArgs e = {part, h.splits, s.places, scale, static_cast<const char *>(A), m.rank, m.n_in,
                     static_cast<const char *>(base), ld_b, static_cast<char *>(dx), ld_dx, nullptr, 0};
     const TileList blocks = tile_list(pv, 1);
@@ -1163,13 +1196,15 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
         constexpr int RT = decltype(rt)::value;
         with_tile(h.h, [&](auto mt) {
             const int64_t n = static_cast<int64_t>(gb.runs) * gb.slices + plan_max_tiles(m.rows, m.n, h.h) * h.splits;
-            k_back_dy<BF16, decltype(mt)::value, RT><<<block_grid(n), 256, 0, st>>>(blocks, gb, tile_list(pv, h.h), sa, d);
+            k_back_dy<BF16, decltype(mt)::value, RT>
+                <<<block_grid(n), 256, 0, st>>>(blocks, gb, tile_list(pv, h.h), sa, d);
         });
         e.slices = static_cast<int>(ceil_div(m.n_in, kSliceCols<BF16, RT>));
         const int he = expand_height(m.rows, e.slices);
         with_tile(he, [&](auto mt) {
             constexpr int M = decltype(mt)::value;
-            const int64_t n = static_cast<int64_t>(ga.runs) * ga.slices + (dx ? plan_max_tiles(m.rows, m.n, he) * e.slices : 0);
+            const int64_t n = static_cast<int64_t>(ga.runs) * ga.slices +
+                              (dx ? plan_max_tiles(m.rows, m.n, he) * e.slices : 0);
             if (d.thr)
                 k_back_x<BF16, M, RT, true><<<block_grid(n), 256, 0, st>>>(blocks, ga, tile_list(pv, he), e, d);
             else
@@ -1188,7 +1223,8 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
     r.rank = m.rank;
     r.rp = s.rp;
     r.accumulate = accumulate;
-    k_reduce<<<dim3(static_cast<unsigned>(m.n * m.rank), static_cast<unsigned>(r.job[0].slices + r.job[1].slices)), 256, 0, st>>>(r);
+    const dim3 grid(static_cast<unsigned>(m.n * m.rank), static_cast<unsigned>(r.job[0].slices + r.job[1].slices));
+    k_reduce<<<grid, 256, 0, st>>>(r);
     return hipGetLastError();
 }
 

@@ -159,24 +159,6 @@ hipError_t launch_topk_filtered(const float *s, int64_t ld_s, int Q, int64_t N, 
                                 float *val, int64_t *idx, const int *cnt, const float *cval,
                                 const int *cidx, int cap, hipStream_t st);
 
-// Workgroups of `threads` threads of kernel K that the current device holds at once.
-template <auto K>
-int resident_groups(int threads) {
-    static int cache[64] = {0};
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 1024;
-    if (cache[dev] == 0) {
-        int cus = 0, per_cu = 0;
-        if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) cus = 256;
-        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, reinterpret_cast<const void *>(K), threads, 0) !=
-                hipSuccess ||
-            per_cu <= 0)
-            per_cu = 1;
-        cache[dev] = cus * per_cu;
-    }
-    return cache[dev];
-}
-
 // Dropout, adapters and the token loss (adapter.hip, dropout.hip, loss.hip).
 struct DropArgs;                         // counter_rng.h
 constexpr int kMaxAdapters = 1023;       // with the rows that have none, 1024 groups: one thread each
