@@ -149,14 +149,30 @@ __device__ __forceinline__ int group_of(const int *row_adapter, int row, int n) 
     return a >= 0 && a < n ? a : n;
 }
 
-__global__ __launch_bounds__(256) void k_plan_hist(const int *row_adapter, PlanView v) {
+// The groups of a thread's rows, `step` apart (all loads together); -1 beyond
+// the last row.
+template <int N>
+__device__ __forceinline__ void groups_of(const int *row_adapter, const PlanView &v, int64_t at, int step,
+                                          int (&group)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int64_t row = at + static_cast<int64_t>(k) * step;
+        group[k] = row < v.rows ? group_of(row_adapter, static_cast<int>(row), v.n) : -1;
+    }
+}
+
+__global__ __launch_bounds__(1024) void k_plan_hist(const int *row_adapter, PlanView v) {
     __shared__ int cnt[1024];
-    for (int g = threadIdx.x; g <= v.n; g += 256) cnt[g] = 0;
+    const int g = threadIdx.x;
+    int group[kSeg / 1024];
+    groups_of(row_adapter, v, static_cast<int64_t>(blockIdx.x) * kSeg + threadIdx.x, 1024, group);
+    cnt[g] = 0;
     __syncthreads();
-    const int at = blockIdx.x * kSeg, end = v.rows - at < kSeg ? v.rows : at + kSeg;
-    for (int i = at + threadIdx.x; i < end; i += 256) atomicAdd(&cnt[group_of(row_adapter, i, v.n)], 1);
+#pragma unroll
+    for (int k = 0; k < kSeg / 1024; ++k)
+        if (group[k] >= 0) atomicAdd(&cnt[group[k]], 1);
     __syncthreads();
-    for (int g = threadIdx.x; g <= v.n; g += 256) v.hist[static_cast<int64_t>(blockIdx.x) * (v.n + 1) + g] = cnt[g];
+    if (g <= v.n) v.hist[static_cast<int64_t>(blockIdx.x) * (v.n + 1) + g] = cnt[g];
 }
 
 // Exclusive sum over the workgroup's 1024 threads; `total` gets the whole sum.
@@ -234,44 +250,59 @@ __global__ __launch_bounds__(1024) void k_plan_scan(PlanView v, int segs) {
     }
 }
 
-// Places of the rows: each of the four waves takes 1024 consecutive rows, 64 at
-// a time; lanes of one group are ranked by their lane numbers, so a group's rows
-// keep their order.
-__global__ __launch_bounds__(256) void k_plan_scatter(const int *row_adapter, PlanView v) {
-    __shared__ int next[4][1024];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, groups = v.n + 1;
-    for (int i = threadIdx.x; i < 4 * 1024; i += 256) next[i >> 10][i & 1023] = 0;
+// The wave's lanes with a row of the same group: two groups differ in a bit.
+__device__ __forceinline__ uint64_t lanes_alike(int group, uint64_t live, int n) {
+    uint64_t same = live;
+    for (int bit = 1; bit <= n; bit <<= 1) {
+        const uint64_t set = __ballot((group & bit) != 0);
+        same &= group & bit ? set : ~set;
+    }
+    return same;
+}
+
+// Places of the rows: each of the 16 waves takes 256 consecutive rows, 64 at a
+// time; lanes of one group are ranked by their lane numbers, so a group's rows
+// keep their order.  Bound by latency (96 rows of 64 adapters 3.5 us; with a turn
+// for each group of the 64 rows, 18).
+__global__ __launch_bounds__(1024) void k_plan_scatter(const int *row_adapter, PlanView v) {
+    constexpr int kIter = kSeg / 1024;
+    __shared__ int next[16][1024];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = threadIdx.x;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kSeg + wave * (kSeg / 16) + lane;
+    int group[kIter];
+    uint64_t same[kIter] = {};
+    groups_of(row_adapter, v, at, 64, group);
+    const int before = g <= v.n ? v.start[g] + v.hist[static_cast<int64_t>(blockIdx.x) * (v.n + 1) + g] : 0;
+    if (g <= v.n)
+        for (int w = 0; w < 16; ++w) next[w][g] = 0;
     __syncthreads();
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * kSeg + wave * (kSeg / 4);
-    for (int i = 0; i < kSeg / 4; i += 64)
-        if (at + i + lane < v.rows)
-            atomicAdd(&next[wave][group_of(row_adapter, static_cast<int>(at + i + lane), v.n)], 1);
+#pragma unroll
+    for (int k = 0; k < kIter; ++k) {
+        const uint64_t live = __ballot(group[k] >= 0);
+        if (!live) break;
+        same[k] = lanes_alike(group[k], live, v.n);
+        if (group[k] >= 0) atomicAdd(&next[wave][group[k]], 1);
+    }
     __syncthreads();
-    for (int g = threadIdx.x; g < groups; g += 256) {
-        int p = v.start[g] + v.hist[static_cast<int64_t>(blockIdx.x) * groups + g];
-        for (int w = 0; w < 4; ++w) {
+    if (g <= v.n) {
+        int p = before;
+        for (int w = 0; w < 16; ++w) {
             const int c = next[w][g];
             next[w][g] = p;
             p += c;
         }
     }
     __syncthreads();
-    for (int i = 0; i < kSeg / 4; i += 64) {
-        const int64_t row = at + i + lane;
-        const bool live = row < v.rows;
-        const int g = live ? group_of(row_adapter, static_cast<int>(row), v.n) : -1;
-        uint64_t left = __ballot(live);
-        while (left) {   // one group of these 64 rows at a time
-            const int gl = __shfl(g, __ffsll(static_cast<unsigned long long>(left)) - 1);
-            const uint64_t same = __ballot(g == gl);
-            volatile int *slot = &next[wave][gl];
-            const int p = *slot;
-            __builtin_amdgcn_wave_barrier();
-            if (g == gl) v.row_of[p + __popcll(same & ((uint64_t{1} << lane) - 1))] = static_cast<int>(row);
-            if (lane == 0) *slot = p + __popcll(same);
-            __builtin_amdgcn_wave_barrier();
-            left &= ~same;
+#pragma unroll
+    for (int k = 0; k < kIter; ++k) {
+        volatile int *slot = &next[wave][group[k] < 0 ? 0 : group[k]];
+        const int p = *slot, rank = __popcll(same[k] & ((uint64_t{1} << lane) - 1));
+        __builtin_amdgcn_wave_barrier();   // every lane has read its group's place
+        if (group[k] >= 0) {
+            v.row_of[p + rank] = static_cast<int>(at + 64 * k);
+            if (rank == 0) *slot = p + __popcll(same[k]);
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -1115,9 +1146,9 @@ size_t adapter_plan_bytes(int64_t rows, int n) { return plan_layout(rows, n).byt
 hipError_t launch_adapter_plan(const int *row_adapter, int64_t rows, int n, void *plan, hipStream_t s) {
     const PlanView v = plan_view(plan, rows, n);
     const int segs = static_cast<int>((rows + kSeg - 1) / kSeg);
-    k_plan_hist<<<segs, 256, 0, s>>>(row_adapter, v);
+    k_plan_hist<<<segs, 1024, 0, s>>>(row_adapter, v);
     k_plan_scan<<<1, 1024, 0, s>>>(v, segs);
-    k_plan_scatter<<<segs, 256, 0, s>>>(row_adapter, v);
+    k_plan_scatter<<<segs, 1024, 0, s>>>(row_adapter, v);
     return hipGetLastError();
 }
 
