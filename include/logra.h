@@ -533,8 +533,9 @@ int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype
  * A row whose u or du is infinite may get NaN where the formulas give an
  * infinity (its operands are differences); other rows' y and dx are unaffected.
  *
- * ws: logra_adapter_ws_size bytes for either call (contents on entry are
- * ignored; calls that overlap need their own).  Limits: n_in, n_out multiples of
+ * ws: logra_adapter_ws_size bytes for either call, logra_adapter_forward_ws_size
+ * for the forward call alone (serving needs no room for gradients; contents on
+ * entry are ignored; calls that overlap need their own).  Limits: n_in, n_out multiples of
  * 8 (bf16) or 4 (fp32), 1 <= rank <= LOGRA_MAX_ADAPTER_RANK.  rows = 0: y, u, dx
  * have no rows; dA and dB are cleared unless accumulate.  A plan made for other
  * rows or n_adapters is recognised on the device: nothing is written then.
@@ -543,6 +544,7 @@ size_t logra_adapter_plan_size(int64_t rows, int n_adapters);
 int logra_adapter_plan(const int32_t *row_adapter, int64_t rows, int n_adapters, void *plan, size_t plan_bytes,
                        void *stream);
 size_t logra_adapter_ws_size(int64_t rows, int n_in, int n_out, int rank, int n_adapters);
+size_t logra_adapter_forward_ws_size(int64_t rows, int n_in, int n_out, int rank, int n_adapters);
 int logra_adapter_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, int n_in, int n_out, int rank,
                           int n_adapters, const void *plan, size_t plan_bytes, const void *A, const void *B,
                           const float *scale, const void *base, int64_t ld_base, void *y, int64_t ld_y, float *u,

@@ -22,8 +22,8 @@ __all__ = [
     "logra_cov_accumulate_f64",
     "logra_precondition_ws_size", "logra_precondition", "logra_precondition_blocks", "logra_precondition_f64",
     "logra_influence_ws_size", "logra_influence_scores",
-    "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size", "logra_adapter_forward",
-    "logra_adapter_backward", "logra_dropout", "logra_token_loss",
+    "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size",
+    "logra_adapter_forward_ws_size", "logra_adapter_forward", "logra_adapter_backward", "logra_dropout", "logra_token_loss",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -48,8 +48,8 @@ EXPORTED = (
     "logra_influence_stream_ws_size", "logra_influence_stream", "logra_offload_rows",
     "logra_store_read_rows", "logra_store_write_rows", "logra_influence_stream_file_ws_size",
     "logra_influence_stream_file", "logra_offload_rows_file",
-    "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size", "logra_adapter_forward",
-    "logra_adapter_backward", "logra_dropout", "logra_token_loss",
+    "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size",
+    "logra_adapter_forward_ws_size", "logra_adapter_forward", "logra_adapter_backward", "logra_dropout", "logra_token_loss",
 )
 
 
@@ -137,8 +137,9 @@ def lib():
         L.logra_adapter_plan_size.argtypes = [i64, i32]
         L.logra_adapter_plan_size.restype = sz
         L.logra_adapter_plan.argtypes = [vp, i64, i32, vp, sz, vp]
-        L.logra_adapter_ws_size.argtypes = [i64, i32, i32, i32, i32]
-        L.logra_adapter_ws_size.restype = sz
+        for name in ("logra_adapter_ws_size", "logra_adapter_forward_ws_size"):
+            getattr(L, name).argtypes = [i64, i32, i32, i32, i32]
+            getattr(L, name).restype = sz
         L.logra_adapter_forward.argtypes = [vp, i64, i32, i64, i32, i32, i32, i32, vp, sz, vp, vp, vp, vp, i64, vp, i64,
                                             vp, f64, u64, u64, vp, sz, vp]
         L.logra_adapter_backward.argtypes = [vp, i64, vp, i64, i32, i64, i32, i32, i32, i32, vp, sz, vp, vp, vp, vp, vp,
@@ -572,7 +573,7 @@ def logra_adapter_plan(row_adapter, n_adapters: int, plan=None, stream=None):
         raise TypeError("row_adapter must be a contiguous 1-D int32 tensor")
     rows = row_adapter.shape[0]
     if plan is None:
-        plan = torch.empty(logra_adapter_plan_size(rows, n_adapters), dtype=torch.uint8, device=row_adapter.device)
+        plan = _scratch(logra_adapter_plan_size(rows, n_adapters), row_adapter.device, stream)
     _check(lib().logra_adapter_plan(row_adapter.data_ptr(), rows, n_adapters, plan.data_ptr(), plan.numel(),
                                     _stream(stream)))
     return plan
@@ -580,6 +581,22 @@ def logra_adapter_plan(row_adapter, n_adapters: int, plan=None, stream=None):
 
 def logra_adapter_ws_size(rows, n_in, n_out, rank, n_adapters) -> int:
     return int(lib().logra_adapter_ws_size(rows, n_in, n_out, rank, n_adapters))
+
+
+def logra_adapter_forward_ws_size(rows, n_in, n_out, rank, n_adapters) -> int:
+    return int(lib().logra_adapter_forward_ws_size(rows, n_in, n_out, rank, n_adapters))
+
+
+def _scratch(nbytes: int, device, stream):
+    """Bytes for work on `stream`, out of that stream's memory: whatever held them before, and whatever gets them
+    afterwards, is ordered with this work."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def _matrix(t, rows: int, width: int, dtype, name: str):
@@ -617,7 +634,8 @@ def logra_adapter_forward(x, a, b, plan, y, base=None, scale=None, u=None, p: fl
 
     x [rows, n_in], y and base [rows, n_out] (base None: zeros; may be y), a [n, rank, n_in] and
     b [n, rank, n_out], all of one dtype; scale [n] fp32 or None; u [rows, rank] fp32 or None: a_a drop(x_t),
-    kept for the backward pass.  p, seed, offset: dropout as logra_dropout draws it for x.
+    kept for the backward pass.  p, seed, offset: dropout as logra_dropout draws it for x.  ws: a workspace of
+    logra_adapter_forward_ws_size (or logra_adapter_ws_size) bytes, allocated for the call when None.
     """
     torch = _torch()
     rows, n_in, n_out, rank, n = _adapter_sizes(x, a, b)
@@ -626,7 +644,7 @@ def logra_adapter_forward(x, a, b, plan, y, base=None, scale=None, u=None, p: fl
     py, ld_y = _matrix(y, rows, n_out, dt, "y")
     pb, ld_b = _matrix(base, rows, n_out, dt, "base")
     if ws is None:
-        ws = torch.empty(logra_adapter_ws_size(rows, n_in, n_out, rank, n), dtype=torch.uint8, device=x.device)
+        ws = _scratch(logra_adapter_forward_ws_size(rows, n_in, n_out, rank, n), x.device, stream)
     _check(lib().logra_adapter_forward(
         px, ld_x, _dtype_code(x), rows, n_in, n_out, rank, n, plan.data_ptr(), plan.numel(),
         _packed(a, (n, rank, n_in), dt, "a"), _packed(b, (n, rank, n_out), dt, "b"), _packed(scale, (n,), f32, "scale"),
@@ -638,7 +656,8 @@ def logra_adapter_backward(x, dy, a, b, plan, u, da, db, dx=None, base=None, sca
                            seed: int = 0, offset: int = 0, accumulate: bool = False, ws=None, stream=None):
     """Gradients of logra_adapter_forward: da [n, rank, n_in] and db [n, rank, n_out] fp32 (overwritten, or
     added to with accumulate) and, unless dx is None, dx [rows, n_in] = base (None: zeros; may be dx) + what the
-    adapter of each row sends back.  u, scale, p, seed, offset: as in the forward call; dy [rows, n_out].
+    adapter of each row sends back.  u, scale, p, seed, offset: as in the forward call; dy [rows, n_out].  ws: a
+    workspace of logra_adapter_ws_size bytes, allocated for the call when None.
     """
     torch = _torch()
     rows, n_in, n_out, rank, n = _adapter_sizes(x, a, b)
@@ -648,7 +667,7 @@ def logra_adapter_backward(x, dy, a, b, plan, u, da, db, dx=None, base=None, sca
     pdx, ld_dx = _matrix(dx, rows, n_in, dt, "dx")
     pb, ld_b = _matrix(base, rows, n_in, dt, "base")
     if ws is None:
-        ws = torch.empty(logra_adapter_ws_size(rows, n_in, n_out, rank, n), dtype=torch.uint8, device=x.device)
+        ws = _scratch(logra_adapter_ws_size(rows, n_in, n_out, rank, n), x.device, stream)
     _check(lib().logra_adapter_backward(
         px, ld_x, pdy, ld_dy, _dtype_code(x), rows, n_in, n_out, rank, n, plan.data_ptr(), plan.numel(),
         _packed(a, (n, rank, n_in), dt, "a"), _packed(b, (n, rank, n_out), dt, "b"), _packed(scale, (n,), f32, "scale"),

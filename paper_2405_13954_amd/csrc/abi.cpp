@@ -808,6 +808,13 @@ int check_adapter_sizes(int dtype, int64_t rows, int n_in, int n_out, int rank, 
     return check_drop(drop_p);
 }
 
+size_t adapter_ws_size(int64_t rows, int n_in, int n_out, int rank, int n_adapters, bool backward) {
+    if (rows <= 0 || n_in <= 0 || n_out <= 0 || rank <= 0 || n_adapters <= 0 || rows > LOGRA_MAX_ADAPTER_ROWS ||
+        rank > LOGRA_MAX_ADAPTER_RANK || n_adapters > LOGRA_MAX_ADAPTERS || n_in > (1 << 20) || n_out > (1 << 20))
+        return 0;
+    return round256(logra::adapter_ws_bytes(rows, n_in, n_out, rank, n_adapters, backward));
+}
+
 int check_plan(const void *plan, size_t plan_bytes, int64_t rows, int n_adapters) {
     const size_t need = logra_adapter_plan_size(rows, n_adapters);
     if (plan == nullptr || plan_bytes < need)
@@ -836,10 +843,11 @@ int logra_adapter_plan(const int32_t *row_adapter, int64_t rows, int n_adapters,
 }
 
 size_t logra_adapter_ws_size(int64_t rows, int n_in, int n_out, int rank, int n_adapters) {
-    if (rows <= 0 || n_in <= 0 || n_out <= 0 || rank <= 0 || n_adapters <= 0 || rows > LOGRA_MAX_ADAPTER_ROWS ||
-        rank > LOGRA_MAX_ADAPTER_RANK || n_adapters > LOGRA_MAX_ADAPTERS || n_in > (1 << 20) || n_out > (1 << 20))
-        return 0;
-    return round256(logra::adapter_ws_bytes(rows, n_in, n_out, rank, n_adapters));
+    return adapter_ws_size(rows, n_in, n_out, rank, n_adapters, true);
+}
+
+size_t logra_adapter_forward_ws_size(int64_t rows, int n_in, int n_out, int rank, int n_adapters) {
+    return adapter_ws_size(rows, n_in, n_out, rank, n_adapters, false);
 }
 
 int logra_adapter_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, int n_in, int n_out, int rank,
@@ -860,7 +868,7 @@ int logra_adapter_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, 
     TRY(check_matrix(y, "y", rows, ld_y, n_out, dtype));
     if (u) TRY(check_dev(u, "u", 4));
     TRY(check_plan(plan, plan_bytes, rows, n_adapters));
-    TRY(check_ws(ws, ws_bytes, logra_adapter_ws_size(rows, n_in, n_out, rank, n_adapters)));
+    TRY(check_ws(ws, ws_bytes, logra_adapter_forward_ws_size(rows, n_in, n_out, rank, n_adapters)));
     const logra::AdapterDims dims = {rows, n_in, n_out, rank, n_adapters};
     const hipError_t e = logra::launch_adapter_forward(dims, dtype == LOGRA_BF16, plan, x, ld_x, A, B, scale, base, ld_base,
                                                        y, ld_y, u, drop_p, seed, offset, ws,

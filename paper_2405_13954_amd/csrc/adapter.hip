@@ -1152,8 +1152,9 @@ hipError_t launch_adapter_plan(const int *row_adapter, int64_t rows, int n, void
     return hipGetLastError();
 }
 
-size_t adapter_ws_bytes(int64_t rows, int n_in, int n_out, int rank, int n) {
-    return ws_layout(shape_of(rows, n_in, n_out, rank, n), rows, n_in, n_out, n).bytes;
+size_t adapter_ws_bytes(int64_t rows, int n_in, int n_out, int rank, int n, bool backward) {
+    const WsLayout l = ws_layout(shape_of(rows, n_in, n_out, rank, n), rows, n_in, n_out, n);
+    return backward ? l.bytes : l.part_a;   // the forward pass has the parts of U alone, which come first
 }
 
 hipError_t launch_adapter_forward(const AdapterDims &m, bool bf16, const void *plan, const void *x, int64_t ld_x,

@@ -170,7 +170,7 @@ struct AdapterDims {
 };
 size_t adapter_plan_bytes(int64_t rows, int n);
 hipError_t launch_adapter_plan(const int *row_adapter, int64_t rows, int n, void *plan, hipStream_t s);
-size_t adapter_ws_bytes(int64_t rows, int n_in, int n_out, int rank, int n);
+size_t adapter_ws_bytes(int64_t rows, int n_in, int n_out, int rank, int n, bool backward);
 hipError_t launch_adapter_forward(const AdapterDims &m, bool bf16, const void *plan, const void *x, int64_t ld_x,
                                   const void *A, const void *B, const float *scale, const void *base, int64_t ld_b,
                                   void *y, int64_t ld_y, float *u, double p, uint64_t seed, uint64_t offset, void *ws,

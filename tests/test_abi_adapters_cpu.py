@@ -64,6 +64,14 @@ def test_plan_refusals_and_sizes(L):
     assert all(s % 256 == 0 and s > 0 for s in sizes)
 
 
+def test_forward_workspace_has_no_gradients(L):
+    # 96 rows of 64 adapters: four parts of U at most, for rows padded to 32 a group, and not the adapters' gradients
+    small, full = (f(96, 4096, 14336, 16, 64) for f in (P.logra_adapter_forward_ws_size, P.logra_adapter_ws_size))
+    assert 0 < small <= 4 * (96 + 65 * 32) * 16 * 4 < full and small % 256 == 0
+    for bad in ((0, 64, 64, 8, 2), (4, 64, 64, 129, 2), (4, 64, 64, 8, 1024), (4, 1 << 21, 64, 8, 2)):
+        assert P.logra_adapter_forward_ws_size(*bad) == 0
+
+
 def test_dropout_and_loss_refusals(L):
     d = lambda **kw: L.logra_dropout(*{**dict(x=NULL, ld_x=16, dtype=0, rows=2, cols=15, p=0.1, seed=1, off=2, res=NULL,  # noqa: E731
                                               ld_res=16, out=NULL, ld_out=16, st=NULL), **kw}.values())

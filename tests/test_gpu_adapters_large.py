@@ -114,3 +114,39 @@ def test_memory_of_plan_and_workspace(shape, dtype):
     for full, what in ((full_plan, "plan"), (full_ws, "workspace"), (full_da, "dA"), (full_db, "dB")):
         assert bool((full[:4096] == 0xA5).all()) and bool((full[-4096:] == 0xA5).all()), f"a store outside the {what}"
     assert bool(torch.isfinite(da).all()) and bool(torch.isfinite(db).all())
+
+
+@pytest.mark.parametrize("shape", [(1, 8, 8, 1, 1), (96, 4096, 264, 16, 64), (3000, 264, 136, 16, 1023), (300, 2048, 512, 100, 3)])
+@pytest.mark.parametrize("p", [0.0, 0.3])
+def test_forward_in_its_own_workspace(shape, p):
+    # exactly as large as asked for, on a stream that is named instead of current: the bits of the other workspace
+    import torch
+    import paper_2405_13954_amd as P
+    rows, n_in, n_out, rank, n = shape
+    print("[forward workspace]", shape, p, flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    x, a, b, base = mk(rows, n_in), mk(n, rank, n_in), mk(n, rank, n_out), mk(rows, n_out)
+    ids = torch.randint(-1, n, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    plan = P.logra_adapter_plan(ids, n)
+    want, got, size = torch.empty_like(base), torch.empty_like(base), P.logra_adapter_forward_ws_size(*shape)
+    whole = torch.empty(P.logra_adapter_ws_size(*shape), dtype=torch.uint8, device="cuda")
+    P.logra_adapter_forward(x, a, b, plan, want, base=base, p=p, seed=3, ws=whole)
+    full = torch.full((size + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+    P.logra_adapter_forward(x, a, b, plan, got, base=base, p=p, seed=3, ws=full[4096:4096 + size])
+    assert torch.equal(got, want)
+    assert bool((full[:4096] == 0xA5).all()) and bool((full[-4096:] == 0xA5).all()), "a store outside the workspace"
+    with pytest.raises(P.LograError) as e:
+        P.logra_adapter_forward(x, a, b, plan, got, base=base, p=p, seed=3, ws=full[4096:4096 + size - 256])
+    assert e.value.status == P.ERR_WORKSPACE
+    side = torch.cuda.Stream()
+    got.fill_(7.0)
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (side, side.cuda_stream):
+        P.logra_adapter_forward(x, a, b, P.logra_adapter_plan(ids, n, stream=stream), got, base=base, p=p, seed=3,
+                                stream=stream)
+        side.synchronize()
+        assert torch.equal(got, want)
+        got.zero_()
+        side.wait_stream(torch.cuda.current_stream())
