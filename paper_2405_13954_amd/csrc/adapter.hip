@@ -34,7 +34,7 @@
 //     the output); rank 16 then fills the 32-deep contraction of one MFMA exactly.
 //     fp32 uses fp32 MFMAs.  16,384 x 4096 bf16 at rank 16: 57 us for 268 MB
 //     (4.7 TB/s; a copy in the same pieces takes 48).
-//  3. grad: a workgroup owns a run of an order's blocks of 32 rows and 256
+//  3. grad: a workgroup owns a run of an order's blocks of 32 rows and 256 (or 128)
 //     columns; a block goes through LDS, where transposed reads (bf16:
 //     ds_read_b64_tr_b16) turn it into operands whose contraction runs over
 //     rows.  A bf16 v takes U as three bf16 thirds (24 significant bits: the
@@ -787,7 +787,14 @@ struct GradArgs {
     int runs;
 };
 
-constexpr int kGradCols = 256;
+// Columns of a workgroup of the gradient: 128 where 256 need more registers than
+// two waves on a SIMD have (the backward pass, rank 128 in bf16: 300 rows of 4096 +
+// 4096 columns 72 us, with 256 columns 99; 2,048 rows 100 and 119, 16,384 rows 455
+// and 416; fp32 at rank 64: 300 rows 52 and 81, 2,048 rows 99 and 114, 8,192 rows
+// 273 and 285).
+__host__ __device__ constexpr int grad_cols(bool bf16, int rt) { return rt < (bf16 ? 8 : 4) ? 256 : 128; }
+template <bool BF16, int RT>
+constexpr int kGradCols = grad_cols(BF16, RT);
 
 // Parts of du that are fetched one by one, and so the splits of the backward
 // pass's k_shrink.
@@ -795,19 +802,20 @@ __host__ __device__ constexpr int parts_of(int rt) { return rt == 1 ? kMaxParts 
 template <int RT>
 constexpr int kParts = parts_of(RT);
 constexpr int kGradChunk = 32;   // blocks whose rows are looked up together
-template <bool BF16>
-constexpr int kVPitch = kGradCols * kEs<BF16> + 32;
+template <bool BF16, int RT>
+constexpr int kVPitch = kGradCols<BF16, RT> * kEs<BF16> + 32;
 template <bool BF16, int RT>
 constexpr int kULds = BF16 ? 3 * 16 * RT * 80 : 32 * (64 * RT + 16);
 template <bool BF16, int RT>
-constexpr int kGradLds = 32 * kVPitch<BF16> + kULds<BF16, RT> + kGradChunk * (32 * 4 + 16);
+constexpr int kGradLds = 32 * kVPitch<BF16, RT> + kULds<BF16, RT> + kGradChunk * (32 * 4 + 16);
 
-// Block `index`: run and slice of kGradCols columns of v.
+// Block `index`: run and slice of grad_cols columns of v.
 template <bool BF16, int RT, bool DROP>
 __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, const DropArgs &d, uint32_t index,
                                      char *lds) {
-    constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kVPitch<BF16>;
-    constexpr int kLoads = 32 * (kGradCols / kV) / 256;      // 16-byte loads of a thread for 32 rows
+    constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kVPitch<BF16, RT>;
+    constexpr int kNc = kGradCols<BF16, RT>, kNw = kNc / 4, kBlocks = kNw / 16;   // columns: all, of a wave; its MFMAs
+    constexpr int kLoads = 32 * (kNc / kV) / 256;      // 16-byte loads of a thread for 32 rows
     constexpr int kRowsPer = 32 / kLoads;                    // rows that the workgroup loads at once
     // U of 32 places.  bf16: [third][rank][place]; fp32: [place][rank]
     constexpr int kUPitch = BF16 ? 80 : 4 * kRp + 16, kUThird = kRp * kUPitch, kChunk = kGradChunk;
@@ -817,11 +825,11 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
     const uint32_t blocks = tile_count(list, false), runs = blocks < static_cast<uint32_t>(a.runs) ? blocks : a.runs;
     const uint32_t run = index / a.slices, slice = index - run * a.slices;
     if (run >= runs) return;
-    const int n0 = slice * kGradCols;
+    const int n0 = slice * kNc;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
     const int end = run_begin(blocks, run + 1, runs);
 
-    const int lr = threadIdx.x / (kGradCols / kV), lc = threadIdx.x % (kGradCols / kV) * kV;
+    const int lr = threadIdx.x / (kNc / kV), lc = threadIdx.x % (kNc / kV) * kV;
     const bool in = n0 + lc < a.width;
     const int ur = threadIdx.x & 15, up = threadIdx.x >> 4;   // rank within 16 and pair of places that the thread loads
     // The next block is on its way while one is multiplied (two ahead measured the same).  Every lane loads: for a pad,
@@ -857,10 +865,10 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
             f.v[k] = ld128_nt(a.v + (row < 0 ? first : row) * a.ld * kEs<BF16> + col_bytes);
         }
     };
-    f32x4 acc[4][RT];
+    f32x4 acc[kBlocks][RT];
     const auto clear = [&] {
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int r = 0; r < RT; ++r) acc[b][r] = zeros4();
     };
@@ -868,8 +876,8 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
     const auto flush = [&](int group) {
         float *out = a.part + (static_cast<int64_t>(run) + group) * kRp * a.width;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int col = n0 + wave * 64 + 16 * b + 4 * g;
+        for (int b = 0; b < kBlocks; ++b) {
+            const int col = n0 + wave * kNw + 16 * b + 4 * g;
             if (col >= a.width) continue;
 #pragma unroll
             for (int r = 0; r < RT; ++r)
@@ -930,11 +938,11 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
             __syncthreads();
             if (i + 1 < count) load(f, i + 1);
             if constexpr (BF16) {
-                u32x4 vf[4];
+                u32x4 vf[kBlocks];
                 const uint32_t l0 = lds_addr(lds_v) + static_cast<uint32_t>((8 * g + (t >> 2)) * kPitch +
-                                                                            (wave * 64 + 4 * (t & 3)) * 2);
+                                                                            (wave * kNw + 4 * (t & 3)) * 2);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
+                for (int b = 0; b < kBlocks; ++b) {
                     const s16x4 v8[2] = {read_tr(l0 + 32 * b), read_tr(l0 + 32 * b + 4 * kPitch)};
                     vf[b] = __builtin_bit_cast(u32x4, v8);
                 }
@@ -945,7 +953,8 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
                         const u32x4 uf =
                             *reinterpret_cast<const u32x4 *>(lds_u + third * kUThird + (16 * r + t) * kUPitch + 16 * g);
 #pragma unroll
-                        for (int b = 0; b < 4; ++b) acc[b][r] = mfma16_bf16(as_bf16x8(vf[b]), as_bf16x8(uf), acc[b][r]);
+                        for (int b = 0; b < kBlocks; ++b)
+                            acc[b][r] = mfma16_bf16(as_bf16x8(vf[b]), as_bf16x8(uf), acc[b][r]);
                     }
             } else {
 #pragma unroll
@@ -955,8 +964,8 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
                     for (int r = 0; r < RT; ++r)
                         uf[r] = ldf(lds_u + (4 * k + g) * kUPitch + (16 * r + t) * 4);
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const float vf = ldf(lds_v + (4 * k + g) * kPitch + (wave * 64 + 16 * b + t) * 4);
+                    for (int b = 0; b < kBlocks; ++b) {
+                        const float vf = ldf(lds_v + (4 * k + g) * kPitch + (wave * kNw + 16 * b + t) * 4);
 #pragma unroll
                         for (int r = 0; r < RT; ++r) acc[b][r] = mfma16_f32(vf, uf[r], acc[b][r]);
                     }
@@ -972,9 +981,15 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
 // The two launches of the backward pass.  In each, a gradient's blocks come first
 // (they are few and long), then those of the product that shares its rows:
 // du = B dy beside dB, both of which read dy; then dx beside dA.
+//
+// At least kWaves waves on a SIMD: the registers of three instead of two at rank
+// 64 cost three that spill, and are worth it where there are many rows (16,384 of
+// bf16: the backward pass 246 -> 217 us; 2,048: both 60).
+template <int RT>
+constexpr int kWaves = RT == 4 ? 3 : RT == 8 ? 2 : 1;
 template <bool BF16, int M, int RT>
-__global__ __launch_bounds__(256) void k_back_dy(TileList blocks, GradArgs g, TileList tiles, ShrinkArgs s,
-                                                 DropArgs d) {
+__global__ __launch_bounds__(256, kWaves<RT>) void k_back_dy(TileList blocks, GradArgs g, TileList tiles,
+                                                             ShrinkArgs s, DropArgs d) {
     constexpr int kLds = kGradLds<BF16, RT> > kShrinkLds<M, RT> ? kGradLds<BF16, RT> : kShrinkLds<M, RT>;
     __shared__ __align__(16) char lds[kLds];
     const uint32_t index = block_index(), n = g.runs * g.slices;
@@ -984,7 +999,8 @@ __global__ __launch_bounds__(256) void k_back_dy(TileList blocks, GradArgs g, Ti
         shrink<BF16, M, RT, false>(tiles, s, d, index - n, lds);
 }
 template <bool BF16, int M, int RT, bool DROP>
-__global__ __launch_bounds__(256) void k_back_x(TileList blocks, GradArgs g, TileList tiles, ExpandArgs e, DropArgs d) {
+__global__ __launch_bounds__(256, kWaves<RT>) void k_back_x(TileList blocks, GradArgs g, TileList tiles,
+                                                            ExpandArgs e, DropArgs d) {
     constexpr int kLds = kGradLds<BF16, RT> > kExpandLds<BF16, M, RT> ? kGradLds<BF16, RT> : kExpandLds<BF16, M, RT>;
     __shared__ __align__(16) char lds[kLds];
     const uint32_t index = block_index(), n = g.runs * g.slices;
@@ -1062,7 +1078,7 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     s.places = plan_places(rows, n);
     // runs of the gradients: with both of them, four workgroups for each CU (two took 68 us, four 52 for 16,384 rows of
     // 4096 + 4096 columns at rank 16, and with six the parts cost more than the occupancy gains)
-    const int64_t slices = ceil_div(n_in, kGradCols) + ceil_div(n_out, kGradCols);
+    const int64_t slices = ceil_div(n_in, 256) + ceil_div(n_out, 256);   // (of either type: one workspace)
     // a part costs what rank / 16 blocks do: runs of at least 1.5 times that many (2,047 rows at rank 64: runs of one
     // block took 21 us and their sum 12, runs of six 17 and 6)
     const int64_t least = s.rt == 1 ? 1 : s.rt * 3 / 2, most = ceil_div(plan_max_tiles(rows, n, 1), least);
@@ -1216,9 +1232,10 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
     const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_out, bf16 ? 2 : 4, kGroups, parts_of(s.rt));
     const ShrinkArgs sa = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<const char *>(B), m.rank, part,
                            s.places, h.splits, h.per};
-    const GradArgs gb = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<int>(ceil_div(m.n_out, kGradCols)),
+    const int cols = grad_cols(bf16, s.rt);
+    const GradArgs gb = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<int>(ceil_div(m.n_out, cols)),
                          u, 0, s.places, m.rank, reinterpret_cast<float *>(w + l.part_b), s.runs};
-    const GradArgs ga = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<int>(ceil_div(m.n_in, kGradCols)),
+    const GradArgs ga = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<int>(ceil_div(m.n_in, cols)),
                          part, h.splits, s.places, m.rank, reinterpret_cast<float *>(w + l.part_a), s.runs};
     ExpandArgs e = {part, h.splits, s.places, scale, static_cast<const char *>(A), m.rank, m.n_in,
                     static_cast<const char *>(base), ld_b, static_cast<char *>(dx), ld_dx, nullptr, 0};
