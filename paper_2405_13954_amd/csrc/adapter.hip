@@ -778,7 +778,7 @@ __device__ __forceinline__ uint32_t run_of(uint32_t blocks, uint32_t j, uint32_t
 struct GradArgs {
     const char *v;            // rows x or dy
     int64_t ld;
-    int width, slices;
+    int width, slices;        // of grad_cols columns and grad_tiles blocks of ranks
     const float *U;           // splits = 0: u [rows][rank]; else du in parts [splits][places][rp]
     int splits;
     int64_t places;
@@ -787,12 +787,16 @@ struct GradArgs {
     int runs;
 };
 
-// Columns of a workgroup of the gradient: 128 where 256 need more registers than
-// two waves on a SIMD have (the backward pass, rank 128 in bf16: 300 rows of 4096 +
-// 4096 columns 72 us, with 256 columns 99; 2,048 rows 100 and 119, 16,384 rows 455
-// and 416; fp32 at rank 64: 300 rows 52 and 81, 2,048 rows 99 and 114, 8,192 rows
-// 273 and 285).
-__host__ __device__ constexpr int grad_cols(bool bf16, int rt) { return rt < (bf16 ? 8 : 4) ? 256 : 128; }
+// A workgroup of the gradient takes as many columns and ranks as the registers of
+// two waves on a SIMD hold: 256 columns, or 128 of fp32 from rank 64 on (the
+// backward pass of 300 rows of 4096 + 4096 columns at rank 64: 52 us, with 256
+// columns 81; 2,048 rows 99 and 114, 8,192 rows 273 and 285), and of rank 128 one
+// half, the other half being another workgroup's, which reads the same rows (bf16,
+// 300 rows: 67 us, 99 as one; 2,048 rows 98 and 119, 16,384 rows 410 and 416).
+__host__ __device__ constexpr int grad_cols(bool bf16, int rt) { return bf16 || rt < 4 ? 256 : 128; }
+__host__ __device__ constexpr int grad_tiles(int rt) { return rt == 8 ? rt / 2 : rt; }
+template <int RT>
+constexpr int kGradTiles = grad_tiles(RT);
 template <bool BF16, int RT>
 constexpr int kGradCols = grad_cols(BF16, RT);
 
@@ -807,14 +811,15 @@ constexpr int kVPitch = kGradCols<BF16, RT> * kEs<BF16> + 32;
 template <bool BF16, int RT>
 constexpr int kULds = BF16 ? 3 * 16 * RT * 80 : 32 * (64 * RT + 16);
 template <bool BF16, int RT>
-constexpr int kGradLds = 32 * kVPitch<BF16, RT> + kULds<BF16, RT> + kGradChunk * (32 * 4 + 16);
+constexpr int kGradLds = 32 * kVPitch<BF16, RT> + kULds<BF16, kGradTiles<RT>> + kGradChunk * (32 * 4 + 16);
 
-// Block `index`: run and slice of grad_cols columns of v.
-template <bool BF16, int RT, bool DROP>
+// Block `index`: run, range of ranks and slice of grad_cols columns of v.
+template <bool BF16, int ALL, bool DROP>
 __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, const DropArgs &d, uint32_t index,
                                      char *lds) {
-    constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kVPitch<BF16, RT>;
-    constexpr int kNc = kGradCols<BF16, RT>, kNw = kNc / 4, kBlocks = kNw / 16;   // columns: all, of a wave; its MFMAs
+    constexpr int RT = kGradTiles<ALL>, kRanges = ALL / RT, kAll = 16 * ALL;   // blocks of ranks: here, in all
+    constexpr int kRp = 16 * RT, kV = kVec<BF16>, kPitch = kVPitch<BF16, ALL>;
+    constexpr int kNc = kGradCols<BF16, ALL>, kNw = kNc / 4, kBlocks = kNw / 16;   // columns: all, of a wave; its MFMAs
     constexpr int kLoads = 32 * (kNc / kV) / 256;      // 16-byte loads of a thread for 32 rows
     constexpr int kRowsPer = 32 / kLoads;                    // rows that the workgroup loads at once
     // U of 32 places.  bf16: [third][rank][place]; fp32: [place][rank]
@@ -825,7 +830,8 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
     const uint32_t blocks = tile_count(list, false), runs = blocks < static_cast<uint32_t>(a.runs) ? blocks : a.runs;
     const uint32_t run = index / a.slices, slice = index - run * a.slices;
     if (run >= runs) return;
-    const int n0 = slice * kNc;
+    const int range = kRanges > 1 ? static_cast<int>(slice) * kRanges / a.slices : 0, r0 = range * kRp;
+    const int n0 = (static_cast<int>(slice) - range * (a.slices / kRanges)) * kNc;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, g = lane >> 4;
     const int end = run_begin(blocks, run + 1, runs);
 
@@ -846,16 +852,16 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
         for (int e = 0; e < 2; ++e) {
             const int row = lds_row[32 * i + 2 * up + e];
             const int64_t place = static_cast<int64_t>(lds_tile[i].p0) + (row < 0 ? 0 : 2 * up + e);
-            const float *q = a.splits ? a.U + place * kRp + ur
+            const float *q = a.splits ? a.U + place * kAll + r0 + ur
                                       : a.U + static_cast<int64_t>(row < 0 ? first : row) * a.rank;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const int k = 16 * r + ur, known = k < a.rank ? k : 0;
+                const int k = r0 + 16 * r + ur, known = k < a.rank ? k : 0;
                 f.u[0][r][e] = a.splits ? q[16 * r] : q[known];
 #pragma unroll
                 for (int c = 1; c < kParts<RT>; ++c) {
                     f.u[c][r][e] = 0.f;
-                    if (a.splits > c) f.u[c][r][e] = q[16 * r + c * a.places * kRp];
+                    if (a.splits > c) f.u[c][r][e] = q[16 * r + c * a.places * kAll];
                 }
             }
         }
@@ -874,7 +880,7 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
     };
     // lane holds columns 4 g .. + 3 of block b for rank 16 r + t
     const auto flush = [&](int group) {
-        float *out = a.part + (static_cast<int64_t>(run) + group) * kRp * a.width;
+        float *out = a.part + ((static_cast<int64_t>(run) + group) * kAll + r0) * a.width;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             const int col = n0 + wave * kNw + 16 * b + 4 * g;
@@ -913,7 +919,7 @@ __device__ __forceinline__ void grad(const TileList &list, const GradArgs &a, co
                     q[e] = f.u[0][r][e];
 #pragma unroll
                     for (int c = 1; c < kParts<RT>; ++c) q[e] += f.u[c][r][e];
-                    if (lds_row[32 * i + 2 * up + e] < 0 || 16 * r + ur >= a.rank) q[e] = 0.f;
+                    if (lds_row[32 * i + 2 * up + e] < 0 || r0 + 16 * r + ur >= a.rank) q[e] = 0.f;
                 }
                 if constexpr (BF16) {
 #pragma unroll
@@ -1082,7 +1088,7 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     // a part costs what rank / 16 blocks do: runs of at least 1.5 times that many (2,047 rows at rank 64: runs of one
     // block took 21 us and their sum 12, runs of six 17 and 6)
     const int64_t least = s.rt == 1 ? 1 : s.rt * 3 / 2, most = ceil_div(plan_max_tiles(rows, n, 1), least);
-    const int64_t runs = 1024 / slices;
+    const int64_t runs = 1024 / (slices * (s.rt / grad_tiles(s.rt)));
     s.runs = static_cast<int>(runs < 1 ? 1 : runs > most ? most : runs);
     return s;
 }
@@ -1232,10 +1238,11 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
     const ShrinkShape h = shrink_shape(m.rows, m.n, m.n_out, bf16 ? 2 : 4, kGroups, parts_of(s.rt));
     const ShrinkArgs sa = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<const char *>(B), m.rank, part,
                            s.places, h.splits, h.per};
-    const int cols = grad_cols(bf16, s.rt);
-    const GradArgs gb = {static_cast<const char *>(dy), ld_dy, m.n_out, static_cast<int>(ceil_div(m.n_out, cols)),
+    const int cols = grad_cols(bf16, s.rt), ranges = s.rt / grad_tiles(s.rt);
+    const GradArgs gb = {static_cast<const char *>(dy), ld_dy, m.n_out,
+                         static_cast<int>(ceil_div(m.n_out, cols)) * ranges,
                          u, 0, s.places, m.rank, reinterpret_cast<float *>(w + l.part_b), s.runs};
-    const GradArgs ga = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<int>(ceil_div(m.n_in, cols)),
+    const GradArgs ga = {static_cast<const char *>(x), ld_x, m.n_in, static_cast<int>(ceil_div(m.n_in, cols)) * ranges,
                          part, h.splits, s.places, m.rank, reinterpret_cast<float *>(w + l.part_a), s.runs};
     ExpandArgs e = {part, h.splits, s.places, scale, static_cast<const char *>(A), m.rank, m.n_in,
                     static_cast<const char *>(base), ld_b, static_cast<char *>(dx), ld_dx, nullptr, 0};
