@@ -509,7 +509,8 @@ int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype
  *          transposed once by the caller)
  *   scale  device fp32 [n_adapters] or NULL (1)
  *   base   rows of n_out at stride ld_base, or NULL (zeros); may be y itself
- *          (with ld_base = ld_y): then rows without an adapter are not touched
+ *          (with ld_base = ld_y): then rows without an adapter are not touched;
+ *          it shares no memory with y otherwise
  *   y      rows of n_out at stride ld_y, dtype, rounded once from fp32
  *   u      device fp32 [rows][rank] or NULL: u_t for the backward pass
  *   drop_p, seed, offset: dropout of x as logra_dropout draws it for x
@@ -527,6 +528,9 @@ int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype
  *          rows), 1: added to
  *   dx     rows of n_in at stride ld_dx, dtype, or NULL (not wanted); base: rows
  *          of n_in (what the shared projection sends back) or NULL; may be dx
+ *          (with ld_base = ld_dx).  dx shares no memory with x, which the call
+ *          reads for dA while it writes dx, nor otherwise with base; calls in
+ *          which it does are refused
  * Sums are fp32, in an order that depends on the sizes and the rows' order
  * alone: reruns are bitwise identical.  The rounding of u and du to matrix
  * operands leaves 16 significant bits in y and dx, and all 24 in dA and dB.
@@ -568,7 +572,8 @@ int logra_adapter_backward(const void *x, int64_t ld_x, const void *dy, int64_t 
  *   that is >= round(65536 p).  1 - p above is exactly 1 - round(65536 p) / 65536.
  *   Give every use (layer, step) its own offset.
  *   x, residual (NULL: none), out: rows of cols elements of dtype F32 or BF16 at
- *   strides ld_x, ld_res, ld_out; out may be x or residual.  A dropped element's
+ *   strides ld_x, ld_res, ld_out; out may be x or residual, with its stride, and
+ *   shares no memory with them otherwise (refused).  A dropped element's
  *   value does not matter (NaN included).  0 <= p < 1 with round(65536 p) < 65536.
  *   Any cols; rows < 2^31; rows = 0 is a no-op. */
 int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols, double p, uint64_t seed,
@@ -586,7 +591,8 @@ int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols
  *   weight   device fp32 [rows] or NULL (1); a weight of 0 masks the token
  *   loss     device fp32 [rows]
  *   dlogits  rows of vocab elements of dtype at stride ld_d, or NULL (losses
- *            only); may be logits (with ld_d = ld)
+ *            only); may be logits (with ld_d = ld), and shares no memory with
+ *            them otherwise (refused)
  * Logits of -inf (forbidden tokens) have probability zero; a token whose logits
  * are all -inf has loss +inf and a zero gradient.  rows < 2^31; rows = 0 is a
  * no-op. */

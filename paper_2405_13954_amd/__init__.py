@@ -656,7 +656,7 @@ def logra_adapter_backward(x, dy, a, b, plan, u, da, db, dx=None, base=None, sca
                            seed: int = 0, offset: int = 0, accumulate: bool = False, ws=None, stream=None):
     """Gradients of logra_adapter_forward: da [n, rank, n_in] and db [n, rank, n_out] fp32 (overwritten, or
     added to with accumulate) and, unless dx is None, dx [rows, n_in] = base (None: zeros; may be dx) + what the
-    adapter of each row sends back.  u, scale, p, seed, offset: as in the forward call; dy [rows, n_out].  ws: a
+    adapter of each row sends back; dx may not share memory with x.  u, scale, p, seed, offset: as in the forward call; dy [rows, n_out].  ws: a
     workspace of logra_adapter_ws_size bytes, allocated for the call when None.
     """
     torch = _torch()

@@ -7,6 +7,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <utility>
 #include <vector>
 
 #include "internal.h"
@@ -762,11 +763,13 @@ int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype
 namespace {
 
 // Sizes and strides of `rows` rows of `width` elements (checked before any HIP call).
-int check_stride(const char *name, int64_t ld, int width, int dtype) {
+int check_stride(const char *name, int64_t ld, int64_t rows, int width, int dtype) {
     if (ld < width) return fail(LOGRA_ERR_INVALID_ARG, "the row stride of %s must be >= %d", name, width);
     if (static_cast<uint64_t>(ld) * esize(dtype) % 16)
         return fail(LOGRA_ERR_INVALID_ARG, "the row stride of %s must be a multiple of 16 bytes", name);
-    if (ld > (int64_t{1} << 40)) return fail(LOGRA_ERR_INVALID_ARG, "the row stride of %s exceeds device memory", name);
+    const double span = (static_cast<double>(rows - 1) * static_cast<double>(ld) + width) * static_cast<double>(esize(dtype));
+    if (ld > (int64_t{1} << 40) || span > 281474976710656.0)   // 2^48 bytes: beyond any device allocation
+        return fail(LOGRA_ERR_INVALID_ARG, "the rows of %s exceed device memory", name);
     return LOGRA_OK;
 }
 
@@ -775,11 +778,49 @@ int check_stride(const char *name, int64_t ld, int width, int dtype) {
 int check_matrix(const void *p, const char *name, int64_t rows, int64_t ld, int width, int dtype) {
     TRY(check_dev(p, name, 16));
     if (rows <= 1) return LOGRA_OK;
-    const double span = (static_cast<double>(rows - 1) * static_cast<double>(ld) + width) * static_cast<double>(esize(dtype));
-    if (span > 281474976710656.0)   // 2^48 bytes: beyond any device allocation
-        return fail(LOGRA_ERR_INVALID_ARG, "the rows of %s exceed device memory", name);
     return check_dev(static_cast<const char *>(p) + ((rows - 1) * ld + width - 1) * static_cast<int64_t>(esize(dtype)),
                      name, 1);
+}
+
+// Rows of `width` elements at a stride of `ld`, as bytes.
+struct Region {
+    uint64_t at, ld, width;
+    int64_t rows;
+};
+Region region(const void *p, int64_t ld, int width, int64_t rows, int dtype) {
+    return {static_cast<uint64_t>(reinterpret_cast<uintptr_t>(p)), static_cast<uint64_t>(ld) * esize(dtype),
+            static_cast<uint64_t>(width) * esize(dtype), rows};
+}
+uint64_t region_end(const Region &r) { return r.at + static_cast<uint64_t>(r.rows - 1) * r.ld + r.width; }
+
+// Whether two regions have a byte in common.  Views of one wider buffer whose
+// columns lie apart have none, though their rows alternate in memory.
+bool share_memory(Region a, Region b) {
+    if (a.at > b.at) std::swap(a, b);
+    if (b.at >= region_end(a)) return false;
+    if (a.ld == b.ld) {   // b begins in row k of a, `in` bytes from that row's start
+        const uint64_t k = (b.at - a.at) / a.ld, in = (b.at - a.at) % a.ld;
+        const uint64_t last = static_cast<uint64_t>(a.rows) - 1;
+        return (k <= last && in < a.width) || (k + 1 <= last && in + b.width > a.ld);
+    }
+    for (int64_t i = 0; i < b.rows; ++i) {   // row i of b: the last row of a that begins before its end
+        const uint64_t begin = b.at + static_cast<uint64_t>(i) * b.ld, last = (begin + b.width - 1 - a.at) / a.ld;
+        const uint64_t row = last < static_cast<uint64_t>(a.rows) ? last : static_cast<uint64_t>(a.rows) - 1;
+        if (a.at + row * a.ld + a.width > begin) return true;
+        if (begin >= region_end(a)) return false;
+    }
+    return false;
+}
+
+// What one launch both reads and writes: the same rows in place (where the call
+// allows it: a thread reads its elements before it writes them), or memory apart.
+// Anything between is read by some workgroups after others have written it.
+int check_apart(const char *in_name, const Region &in, const char *out_name, const Region &out, bool in_place) {
+    if (in_place && in.at == out.at && (in.ld == out.ld || in.rows == 1)) return LOGRA_OK;
+    if (share_memory(in, out))
+        return fail(LOGRA_ERR_INVALID_ARG, in_place ? "%s and %s share memory without being the same rows"
+                                                    : "%s and %s share memory", in_name, out_name);
+    return LOGRA_OK;
 }
 
 int check_drop(double p) {
@@ -856,10 +897,12 @@ int logra_adapter_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, 
                           double drop_p, uint64_t seed, uint64_t offset, void *ws, size_t ws_bytes, void *stream) {
     TRY(check_adapter_sizes(dtype, rows, n_in, n_out, rank, n_adapters, drop_p));
     if (rows == 0) return ok();
-    TRY(check_stride("x", ld_x, n_in, dtype));
-    TRY(check_stride("y", ld_y, n_out, dtype));
-    if (base) TRY(check_stride("base", ld_base, n_out, dtype));
-    if (base == y && ld_base != ld_y) return fail(LOGRA_ERR_INVALID_ARG, "base in place of y needs y's row stride");
+    TRY(check_stride("x", ld_x, rows, n_in, dtype));
+    TRY(check_stride("y", ld_y, rows, n_out, dtype));
+    if (base) {
+        TRY(check_stride("base", ld_base, rows, n_out, dtype));
+        TRY(check_apart("base", region(base, ld_base, n_out, rows, dtype), "y", region(y, ld_y, n_out, rows, dtype), true));
+    }
     TRY(check_matrix(x, "x", rows, ld_x, n_in, dtype));
     TRY(check_dev(A, "A", 16));
     TRY(check_dev(B, "B", 16));
@@ -885,12 +928,17 @@ int logra_adapter_backward(const void *x, int64_t ld_x, const void *dy, int64_t 
     TRY(check_adapter_sizes(dtype, rows, n_in, n_out, rank, n_adapters, drop_p));
     if (base && !dx) return fail(LOGRA_ERR_INVALID_ARG, "base without dx");
     if (rows > 0) {
-        TRY(check_stride("x", ld_x, n_in, dtype));
-        TRY(check_stride("dy", ld_dy, n_out, dtype));
-        if (dx) TRY(check_stride("dx", ld_dx, n_in, dtype));
-        if (base) TRY(check_stride("base", ld_base, n_in, dtype));
-        if (base && base == dx && ld_base != ld_dx)
-            return fail(LOGRA_ERR_INVALID_ARG, "base in place of dx needs dx's row stride");
+        TRY(check_stride("x", ld_x, rows, n_in, dtype));
+        TRY(check_stride("dy", ld_dy, rows, n_out, dtype));
+        if (dx) {   // dA's workgroups read x beside those that store dx
+            TRY(check_stride("dx", ld_dx, rows, n_in, dtype));
+            const Region out = region(dx, ld_dx, n_in, rows, dtype);
+            TRY(check_apart("x", region(x, ld_x, n_in, rows, dtype), "dx", out, false));
+            if (base) {
+                TRY(check_stride("base", ld_base, rows, n_in, dtype));
+                TRY(check_apart("base", region(base, ld_base, n_in, rows, dtype), "dx", out, true));
+            }
+        }
     }
     TRY(check_dev(dA, "dA", 16));
     TRY(check_dev(dB, "dB", 16));
@@ -921,11 +969,14 @@ int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols
     if (rows > INT32_MAX) return fail(LOGRA_ERR_UNSUPPORTED, "rows must be < 2^31");
     TRY(check_drop(p));
     if (rows == 0) return ok();
-    TRY(check_stride("x", ld_x, cols, dtype));
-    TRY(check_stride("out", ld_out, cols, dtype));
-    if (residual) TRY(check_stride("residual", ld_res, cols, dtype));
-    if ((x == out && ld_x != ld_out) || (residual == out && residual && ld_res != ld_out))
-        return fail(LOGRA_ERR_INVALID_ARG, "an input in place of out needs out's row stride");
+    TRY(check_stride("x", ld_x, rows, cols, dtype));
+    TRY(check_stride("out", ld_out, rows, cols, dtype));
+    const Region to = region(out, ld_out, cols, rows, dtype);
+    TRY(check_apart("x", region(x, ld_x, cols, rows, dtype), "out", to, true));
+    if (residual) {
+        TRY(check_stride("residual", ld_res, rows, cols, dtype));
+        TRY(check_apart("residual", region(residual, ld_res, cols, rows, dtype), "out", to, true));
+    }
     TRY(check_matrix(x, "x", rows, ld_x, cols, dtype));
     if (residual) TRY(check_matrix(residual, "residual", rows, ld_res, cols, dtype));
     TRY(check_matrix(out, "out", rows, ld_out, cols, dtype));
@@ -942,9 +993,12 @@ int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, in
     if (rows > INT32_MAX) return fail(LOGRA_ERR_UNSUPPORTED, "rows must be < 2^31");
     if (vocab > (1 << 30)) return fail(LOGRA_ERR_UNSUPPORTED, "vocab must be <= 2^30");
     if (rows == 0) return ok();
-    TRY(check_stride("logits", ld, vocab, dtype));
-    if (dlogits) TRY(check_stride("dlogits", ld_d, vocab, dtype));
-    if (dlogits == logits && ld_d != ld) return fail(LOGRA_ERR_INVALID_ARG, "dlogits in place of logits needs their row stride");
+    TRY(check_stride("logits", ld, rows, vocab, dtype));
+    if (dlogits) {
+        TRY(check_stride("dlogits", ld_d, rows, vocab, dtype));
+        TRY(check_apart("logits", region(logits, ld, vocab, rows, dtype), "dlogits", region(dlogits, ld_d, vocab, rows, dtype),
+                        true));
+    }
     TRY(check_matrix(logits, "logits", rows, ld, vocab, dtype));
     TRY(check_dev(target, "target", 8));
     if (weight) TRY(check_dev(weight, "weight", 4));
