@@ -1054,8 +1054,8 @@ __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
             for (int k = 0; k < 8; ++k) s += v[k];
             p += 8 * step;
         }
+        s *= job.f * (job.scale ? job.scale[ad] : 1.f);   // (an adapter without rows has zeros whatever its scale)
     }
-    s *= job.f * (job.scale ? job.scale[ad] : 1.f);
     float *out = job.dW + static_cast<int64_t>(blockIdx.x) * job.width + col;
     if (a.accumulate) s += ldf4(out);
     stf4(out, s);
