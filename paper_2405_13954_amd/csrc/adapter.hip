@@ -1062,7 +1062,7 @@ __global__ __launch_bounds__(256) void k_reduce(ReduceArgs a) {
 }
 
 __global__ __launch_bounds__(256) void k_zero(float *p, int64_t quads) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t i = static_cast<int64_t>(block_index()) * 256 + threadIdx.x;
     if (i < quads) reinterpret_cast<f32x4 *>(p)[i] = zeros4();
 }
 
@@ -1225,8 +1225,8 @@ hipError_t launch_adapter_backward(const AdapterDims &m, bool bf16, const void *
         if (!accumulate) {
             const int64_t na = static_cast<int64_t>(m.n) * m.rank * m.n_in / 4;
             const int64_t nb = static_cast<int64_t>(m.n) * m.rank * m.n_out / 4;
-            k_zero<<<static_cast<unsigned>((na + 255) / 256), 256, 0, st>>>(dA, na);
-            k_zero<<<static_cast<unsigned>((nb + 255) / 256), 256, 0, st>>>(dB, nb);
+            k_zero<<<block_grid(ceil_div(na, 256)), 256, 0, st>>>(dA, na);
+            k_zero<<<block_grid(ceil_div(nb, 256)), 256, 0, st>>>(dB, nb);
         }
         return hipGetLastError();
     }
