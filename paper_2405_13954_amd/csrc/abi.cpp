@@ -829,6 +829,9 @@ int check_drop(double p) {
     return LOGRA_OK;
 }
 
+static_assert(LOGRA_MAX_ADAPTERS == logra::kMaxAdapters && LOGRA_MAX_ADAPTER_RANK == logra::kMaxAdapterRank &&
+                  LOGRA_MAX_ADAPTER_ROWS == logra::kMaxAdapterRows,
+              "the kernels' limits are the public ones");
 int check_adapter_group(int64_t rows, int n_adapters) {
     if (rows < 0) return fail(LOGRA_ERR_INVALID_ARG, "rows must be >= 0");
     if (n_adapters <= 0) return fail(LOGRA_ERR_INVALID_ARG, "n_adapters must be > 0");

@@ -57,6 +57,8 @@ constexpr int kPlanMagic = 0x4c6f4164;
 // 14336 columns, 16.7 against 15.4 us).
 constexpr int kMaxParts = 4;
 constexpr int kPad = 32;             // groups start at multiples of this
+static_assert(kMaxAdapters + 1 <= 1024, "the plan's kernels have a thread and an LDS word for each group");
+static_assert(kMaxAdapterRank <= 16 * 8, "the products take at most eight blocks of ranks");
 
 struct PlanHead {
     int magic, rows, n;
@@ -769,7 +771,8 @@ __global__ __launch_bounds__(256) void k_expand(TileList list, ExpandArgs a, Dro
 // part of the adapter's sum.  Runs and adapters both only increase, so run +
 // adapter numbers the parts, an adapter's parts one after the other.  No run is
 // empty: there are at most as many as blocks.
-constexpr uint32_t kMaxRuns = 1024;   // with the 2^19 + 1023 blocks at most, products fit 32 bits
+constexpr uint32_t kMaxRuns = 1024;
+static_assert((kMaxAdapterRows / 32 + kMaxAdapters) * kMaxRuns <= UINT32_MAX, "products of blocks and runs fit 32 bits");
 __device__ __forceinline__ uint32_t run_begin(uint32_t blocks, uint32_t i, uint32_t n) { return blocks * i / n; }
 __device__ __forceinline__ uint32_t run_of(uint32_t blocks, uint32_t j, uint32_t n) {
     return ((j + 1) * n - 1) / blocks;
@@ -1088,7 +1091,7 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     // a part costs what rank / 16 blocks do: runs of at least 1.5 times that many (2,047 rows at rank 64: runs of one
     // block took 21 us and their sum 12, runs of six 17 and 6)
     const int64_t least = s.rt == 1 ? 1 : s.rt * 3 / 2, most = ceil_div(plan_max_tiles(rows, n, 1), least);
-    const int64_t runs = 1024 / (slices * (s.rt / grad_tiles(s.rt)));
+    const int64_t runs = kMaxRuns / (slices * (s.rt / grad_tiles(s.rt)));
     s.runs = static_cast<int>(runs < 1 ? 1 : runs > most ? most : runs);
     return s;
 }
