@@ -534,8 +534,11 @@ int logra_pca_topk(const float *C, int n, int k, int iters, void *P, int P_dtype
  * Sums are fp32, in an order that depends on the sizes and the rows' order
  * alone: reruns are bitwise identical.  The rounding of u and du to matrix
  * operands leaves 16 significant bits in y and dx, and all 24 in dA and dB.
- * A row whose u or du is infinite may get NaN where the formulas give an
- * infinity (its operands are differences); other rows' y and dx are unaffected.
+ * Infinities: a bf16 call multiplies by the parts of u and du, of which all but
+ * the first may be zero or of the other sign.  So an infinite u, du or weight may
+ * give NaN in that row's (the weight's adapter's) y and dx where the formulas give
+ * an infinity, and an infinite u, du, x or dy in that adapter's dA and dB; other
+ * rows' y and dx and other adapters' gradients are unaffected.
  *
  * ws: logra_adapter_ws_size bytes for either call, logra_adapter_forward_ws_size
  * for the forward call alone (serving needs no room for gradients; contents on
@@ -570,12 +573,14 @@ int logra_adapter_backward(const void *x, int64_t ld_x, const void *dy, int64_t 
  *   high word) of the counter (j / 8, t, offset low, offset high) gives 4 words;
  *   element j takes half j % 2 (low first) of word (j % 8) / 2 and is kept iff
  *   that is >= round(65536 p).  1 - p above is exactly 1 - round(65536 p) / 65536.
- *   Give every use (layer, step) its own offset.
+ *   So p acts in steps of 1/65536, and a p of at most 2^-17 drops nothing.  Give
+ *   every use (layer, step) its own offset.
  *   x, residual (NULL: none), out: rows of cols elements of dtype F32 or BF16 at
  *   strides ld_x, ld_res, ld_out; out may be x or residual, with its stride, and
  *   shares no memory with them otherwise (refused).  A dropped element's
  *   value does not matter (NaN included).  0 <= p < 1 with round(65536 p) < 65536.
- *   Any cols; rows < 2^31; rows = 0 is a no-op. */
+ *   Any cols (a stride is a multiple of 16 bytes here too: rows of an odd width
+ *   lie in a wider buffer); rows < 2^31; rows = 0 is a no-op. */
 int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols, double p, uint64_t seed,
                   uint64_t offset, const void *residual, int64_t ld_res, void *out, int64_t ld_out, void *stream);
 
@@ -585,7 +590,10 @@ int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols
  *
  *     loss[t] = w_t (log sum_j exp(z_tj) - z_t,target),  dlogits[t] = w_t (softmax(z_t) - onehot(target_t))
  *
- *   logits   rows of vocab elements of dtype F32 or BF16 at stride ld; any vocab
+ *   logits   rows of vocab elements of dtype F32 or BF16 at stride ld; any vocab,
+ *            at a stride that is a multiple of 16 bytes (the product that makes
+ *            the logits of an odd vocabulary stores them into a wider buffer:
+ *            packed rows of 50,257 bf16 logits are refused)
  *   target   device int64 [rows]; outside [0, vocab): the token is masked, its
  *            loss and gradient are zero and its logits are not read
  *   weight   device fp32 [rows] or NULL (1); a weight of 0 masks the token

@@ -678,7 +678,9 @@ def logra_adapter_backward(x, dy, a, b, plan, u, da, db, dx=None, base=None, sca
 
 def logra_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, stream=None):
     """out = residual + drop(x) for x, residual (None: zeros) and out [rows, cols] of one dtype; the mask is a
-    function of (seed, offset, row, column) alone, so the backward pass is logra_dropout on the gradient."""
+    function of (seed, offset, row, column) alone, so the backward pass is logra_dropout on the gradient.  Any
+    number of columns, at row strides that are multiples of 16 bytes; out may be x or residual, and shares no memory
+    with them otherwise."""
     rows, cols = x.shape
     px, ld_x = _matrix(x, rows, cols, x.dtype, "x")
     po, ld_o = _matrix(out, rows, cols, x.dtype, "out")
@@ -690,7 +692,8 @@ def logra_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, s
 def logra_token_loss(logits, target, loss, dlogits=None, weight=None, stream=None):
     """loss [rows] fp32 = weight (logsumexp(logits) - logits[target]) and, unless None, dlogits = its gradient,
     for logits [rows, vocab] and target [rows] int64 (outside the vocabulary: masked, zeros); dlogits may be
-    logits."""
+    logits, and shares no memory with them otherwise.  Any vocabulary, at row strides that are multiples of 16
+    bytes: for an odd one, logits are the first columns of a wider buffer."""
     torch = _torch()
     rows, vocab = logits.shape
     pz, ld = _matrix(logits, rows, vocab, logits.dtype, "logits")

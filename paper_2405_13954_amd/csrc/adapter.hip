@@ -26,13 +26,16 @@
 //  1. shrink: a workgroup owns a tile of 16 or 32 rows and a range of the long
 //     axis, its four waves taking 128-byte pieces of it in turn; the waves' sums
 //     are added through LDS.  Few rows: the axis is split over workgroups, whose
-//     parts those that read U add in order.  16,384 x 4096 bf16 at rank 16: 24 us
-//     (5.6 TB/s), 31 with the dropout of x drawn on the way.
+//     parts those that read U add, each kernel in a fixed order of its own (of four
+//     parts, expand adds the fourth before the second, grad last, so that dx and dA
+//     may see a du that differs in its last bits).  16,384 x 4096 bf16 at rank 16: 31 us
+//     (4.3 TB/s) with the dropout of x drawn on the way, by the launch's 2048
+//     workgroups, 37 without it, by 512.
 //  2. expand: a workgroup owns 16 or 32 rows and a slice of columns; W's slice is
 //     put in LDS once, and U as MFMA operands.  A bf16 W takes U as two bf16
 //     halves (16 significant bits, so that U's rounding stays far below that of
 //     the output); rank 16 then fills the 32-deep contraction of one MFMA exactly.
-//     fp32 uses fp32 MFMAs.  16,384 x 4096 bf16 at rank 16: 57 us for 268 MB
+//     fp32 uses fp32 MFMAs.  16,384 x 4096 bf16 at rank 16: 55-58 us for 268 MB
 //     (4.7 TB/s; a copy in the same pieces takes 48).
 //  3. grad: a workgroup owns a run of an order's blocks of 32 rows and 256 (or 128)
 //     columns; a block goes through LDS, where transposed reads (bf16:
@@ -42,7 +45,7 @@
 //     runs' sums in order.
 //  Forward: k_shrink, k_expand.  Backward: k_back_dy (du and dB, both of which
 //  read dy), k_back_x (dx and dA), k_reduce: 16,384 rows, 4096 + 4096 columns,
-//  rank 16: 46 + 80 + 7 us for the 537 MB that the pass cannot do without.
+//  rank 16, dropout: 47 + 81-84 + 7 us for the 544 MB that the pass cannot do without.
 #include "counter_rng.h"
 #include "internal.h"
 
@@ -52,9 +55,13 @@ namespace {
 constexpr int kHeights = 2;          // tile lists of 16 << h rows
 constexpr int kSeg = 4096;           // rows of one workgroup of the plan's kernels
 constexpr int kPlanMagic = 0x4c6f4164;
-// Ranges of the long axis in k_shrink at most, which all that read U add up (with
-// eight they paid more for it than k_shrink gained: 96 rows of 64 adapters, 4096 to
-// 14336 columns, 16.7 against 15.4 us).
+// Ranges of the long axis in k_shrink at most, which all that read U add up.  At 4096
+// columns of x, those pay as much for eight as k_shrink gains, or more (shrink + expand,
+// us: 96 rows of 64 adapters to 14336 columns 5.4 + 9.3, with eight 4.5 + 11.7; 8 rows
+// 4.0 + 3.5 and 3.3 + 4.6; 300 rows 5.4 + 4.4 and 4.5 + 5.6; 1,999 rows at rank 64 to
+// 1024 columns 10.9 + 6.0 and 11.3 + 7.3; with two, 5.0 + 3.4 for 8 rows).  At 14336 columns
+// of x eight would be better (1 row 6.1 + 3.6 and 4.7 + 4.4, 16 rows 9.6 + 3.6 and
+// 6.3 + 4.5), and more were not measured.
 constexpr int kMaxParts = 4;
 constexpr int kPad = 32;             // groups start at multiples of this
 static_assert(kMaxAdapters + 1 <= 1024, "the plan's kernels have a thread and an LDS word for each group");
@@ -198,7 +205,9 @@ __device__ __forceinline__ int scan1024(int x, int *red, int *total) {
 }
 
 // One thread per group: starts, tile lists, and the segments' counts turned
-// into the segments' first places within the group.
+// into the segments' first places within the group, one segment after the other:
+// 5-6 us up to 16,384 rows of some adapters (16 with 1,023), 20 us for 2^18 rows, 68 for
+// 2^20, 1.1 ms for 2^24 (2.2 with 1,023 adapters).
 __global__ __launch_bounds__(1024) void k_plan_scan(PlanView v, int segs) {
     __shared__ int red[16], lds_first[1025], lds_start[1024], lds_count[1024];
     const int g = threadIdx.x, groups = v.n + 1;
@@ -264,7 +273,7 @@ __device__ __forceinline__ uint64_t lanes_alike(int group, uint64_t live, int n)
 
 // Places of the rows: each of the 16 waves takes 256 consecutive rows, 64 at a
 // time; lanes of one group are ranked by their lane numbers, so a group's rows
-// keep their order.  Bound by latency (96 rows of 64 adapters 3.5 us; with a turn
+// keep their order.  Bound by latency (96 rows of 64 adapters 2.8 us; with a turn
 // for each group of the 64 rows, 18).
 __global__ __launch_bounds__(1024) void k_plan_scatter(const int *row_adapter, PlanView v) {
     constexpr int kIter = kSeg / 1024;
@@ -1085,8 +1094,11 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
     s.rt = rank_tiles(rank);
     s.rp = 16 * s.rt;
     s.places = plan_places(rows, n);
-    // runs of the gradients: with both of them, four workgroups for each CU (two took 68 us, four 52 for 16,384 rows of
-    // 4096 + 4096 columns at rank 16, and with six the parts cost more than the occupancy gains)
+    // runs of the gradients: 1024 workgroups for both together, shared in proportion to their columns, though each has a
+    // launch of its own.  16,384 rows at rank 16, dy's launch + x's + k_reduce, with 512, 1024 and 2048 in all: 4096 +
+    // 4096 columns 52 + 83 + 5, 47 + 81 + 7 and 59 + 84 + 9 us.  Where the widths differ the narrow side has few
+    // workgroups: x of 4096 beside dy of 14336 columns 176 + 115 + 7, 253 + 76 + 7 and 214 + 71 + 10, beside 128,000
+    // (one run: 16 workgroups for dA) 1437 + 629 + 18, 1440 + 638 + 18 and, with two runs, 1688 + 229 + 17.
     const int64_t slices = ceil_div(n_in, 256) + ceil_div(n_out, 256);   // (of either type: one workspace)
     // a part costs what rank / 16 blocks do: runs of at least 1.5 times that many (2,047 rows at rank 64: runs of one
     // block took 21 us and their sum 12, runs of six 17 and 6)
@@ -1098,7 +1110,10 @@ Shape shape_of(int64_t rows, int n_in, int n_out, int rank, int n) {
 
 // Tiles of the shrinking product (16 << h rows) and ranges of its long axis: as
 // many workgroups as `groups`, if ranges of a kilobyte and tiles of 16 rows give
-// them.
+// them.  Tiles of 32 rows from 192 of their workgroups on (us at 4096 columns of bf16,
+// rank 16, 16- and 32-row tiles: 300 rows 5.2-5.6 and 5.8, 1,024 6.8 and 6.4, 1,536
+// 6.9 and 6.5, 2,048 9.0 and 9.1, 4,096 14.0 and 12.0; 1,999 rows at rank 64 13.9 and
+// 11.0; 509 rows of 768 fp32 4.4 and 5.7).
 struct ShrinkShape {
     int h, splits, per;
 };
@@ -1115,8 +1130,9 @@ ShrinkShape shrink_shape(int64_t rows, int n, int width, int es, int groups, int
     s.splits = static_cast<int>(ceil_div(width, s.per));
     return s;
 }
-// The forward pass hides the drawing of its dropout behind more workgroups (16,384 x 4096 at rank 16: 39 us with 512,
-// 32 with 2048); without it, and in the backward pass, fewer parts are better for those that add them.
+// The forward pass hides the drawing of its dropout behind more workgroups (16,384 x 4096 at rank 16: 38 us with 512,
+// 31 with 2048).  Without it more workgroups gain less, and those that add their parts lose some of that again: 37 + 55
+// us with 512, 31 + 58 with 2048 (shrink + expand); the backward pass of the same rows 46 + 81 and 44 + 86.
 constexpr int kForwardGroups = 2048, kGroups = 512;
 
 struct WsLayout {
@@ -1161,7 +1177,9 @@ void with_tile(int h, F f) {
     else
         f(std::integral_constant<int, 2>{});
 }
-// Tiles of the expanding product: 32 rows, or 16 where those leave CUs without work.
+// Tiles of the expanding product: 32 rows, or 16 where those leave CUs without work (us with 16 and 32 rows, bf16 at
+// rank 16 to 4096 columns: 300 rows 4.3 and 4.6, 1,024 6.5 and 6.8, 2,048 10.0 and 11.0, 4,096 17.3 and 17.3; 1,999
+// rows to 1024 columns 4.8 and 5.4, at rank 64 5.8 and 6.6; 509 rows to 2304 fp32 columns 6.7 and 10.3).
 int expand_height(int64_t rows, int slices) { return (rows >> 5) * slices < 512 ? 0 : 1; }
 
 }  // namespace

@@ -6,7 +6,7 @@
 // vocabulary packed in registers; the others go by once for the statistics and
 // once more, out of the cache, for the gradient.  So memory sees one read of the
 // logits and one write of the gradient, which is what bounds it (2,048 tokens of
-// 128,000 bf16 logits, a fifth of them masked: 196 us for 0.94 GB, 4.8 TB/s).
+// 128,000 bf16 logits, a fifth of them masked: 201 us for 0.94 GB, 4.7 TB/s).
 // The statistics are one pass: a running maximum and the sum of exp(z - max),
 // brought to a new maximum once per four vectors.  Maximum, sum and gradient are
 // fp32; z - max is formed before the product with log2(e), so that the likely
@@ -229,10 +229,11 @@ hipError_t launch_token_loss(const void *logits, int64_t ld, bool bf16, int64_t 
     const int64_t vec = (static_cast<int64_t>(vocab) + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4);
     const auto pick = [&](auto b) {
         constexpr bool B = decltype(b)::value;
-        // Many tokens of a large vocabulary: two workgroups of 1024 threads on a CU, so that one loads or stores while
-        // the other computes (2,048 tokens of 128,000 bf16 logits: 202 us; one workgroup with all of the token in its
-        // registers 222).  Few tokens: as much as one workgroup has registers for (61 tokens of 50,001 fp32
-        // logits: 11 against 16 us).
+        // More tokens than CUs, of a large vocabulary: two workgroups of 1024 threads on a CU, so that one loads or
+        // stores while the other computes; otherwise as much as one workgroup has registers for.  us with 4 and with 12
+        // kept vectors: bf16, 2,048 tokens of 50,257 logits 81 and 106, 300 tokens 18.6 and 25; 2,048 tokens of 128,000
+        // 201 and 198, 300 tokens 41.2 and 40.5, 256 tokens 29 and 26, 200 tokens of 50,257 12.6 and 14.1; fp32,
+        // 61 tokens of 50,001 11.1 and 10.0, 2,048 tokens of 50,257 164 and 157.
         if (vec <= 256 * 4) go(k_token_loss<B, 256, 4, 8>, 256);
         else if (vec <= 512 * 4) go(k_token_loss<B, 512, 4, 8>, 512);
         else if (vec <= 1024 * 4 || rows > 256) go(k_token_loss<B, 1024, 4, 8>, 1024);
