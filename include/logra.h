@@ -62,6 +62,9 @@ typedef enum { LOGRA_F32 = 0, LOGRA_BF16 = 1, LOGRA_F64 = 2 } logra_dtype;
 #define LOGRA_MAX_ADAPTERS 1023       /* adapters of one plan */
 #define LOGRA_MAX_ADAPTER_RANK 128
 #define LOGRA_MAX_ADAPTER_ROWS 16777216
+#define LOGRA_MAX_NORM_COLS 32768
+#define LOGRA_MAX_ADAMW_GROUPS 65536
+#define LOGRA_ADAMW_BLOCK 256         /* elements that share a scale of the 8-bit states */
 
 const char *logra_last_error(void);
 const char *logra_version(void);
@@ -606,6 +609,157 @@ int logra_dropout(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols
  * no-op. */
 int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, int vocab, const int64_t *target,
                      const float *weight, float *loss, void *dlogits, int64_t ld_d, void *stream);
+
+/* ------------------------------------------------------------------------
+ * The rest of a tuning step: the norm between the layers, the loss of
+ * preference data, the optimizer.
+ *
+ * logra_layer_norm_forward, for every row t:
+ *
+ *     h_t = x_t + residual_t,   y_t = (h_t - mean_t) rstd_t gain + bias,
+ *     rstd_t = 1 / sqrt(avg((h_t - mean_t)^2) + eps)
+ *
+ *   with rms: the same with mean_t = 0, and without a bias.
+ *   x, residual (NULL: none), h (NULL: not wanted), y: rows of cols elements of
+ *            dtype F32 or BF16 at strides that are multiples of 16 bytes; any
+ *            cols up to LOGRA_MAX_NORM_COLS (rows of an odd width lie in a wider
+ *            buffer).  h is rounded to dtype, and the norm is that of the rounded
+ *            h.  y and h may each be x or residual, with its stride; otherwise
+ *            outputs share no memory with inputs or each other (refused)
+ *   mask     device uint8 [rows] or NULL: a row with 0 is not read, its y, h,
+ *            mean and rstd are zeros
+ *   gain, bias  device [cols] of dtype, 16-byte aligned, or NULL (1, 0)
+ *   mean, rstd  device fp32 [rows] or NULL: for the backward pass
+ *   eps      in [1e-30, 1e30]
+ *
+ * logra_layer_norm_backward, with xh_t = (h_t - mean_t) rstd_t and c_t = dy_t gain:
+ *
+ *     dx_t = base_t + rstd_t (c_t - avg(c_t) - xh_t avg(c_t xh_t))    (rms: no avg(c_t))
+ *     dgain (+)= sum_t dy_t xh_t        dbias (+)= sum_t dy_t
+ *
+ *   h, dy, base (NULL: zeros), dx (NULL: not wanted): rows of cols at strides as
+ *            above; h is what the forward call normalised.  dx is the gradient of
+ *            h, so of x and of residual alike; base is what reaches h otherwise.
+ *            dx may be h, dy or base, with its stride, and shares no memory with
+ *            inputs otherwise (refused)
+ *   mask     rows with 0: h, dy and the statistics are not read, dx = base, and
+ *            they add nothing to dgain and dbias
+ *   mean, rstd  as the forward call left them (mean NULL with rms)
+ *   dgain, dbias  device fp32 [cols] or NULL; accumulate 0: overwritten, 1: added to
+ *   ws       logra_layer_norm_ws_size bytes, 256-byte aligned, where dgain or dbias
+ *            is wanted (contents on entry are ignored; calls that overlap need
+ *            their own)
+ * Sums are fp32, in an order that depends on the sizes alone: reruns are bitwise
+ * identical.  rows < 2^31; rows = 0: dgain and dbias are cleared unless accumulate.
+ * ---------------------------------------------------------------------- */
+int logra_layer_norm_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols, int rms, double eps,
+                             const uint8_t *mask, const void *gain, const void *bias, const void *residual, int64_t ld_res,
+                             void *h, int64_t ld_h, void *y, int64_t ld_y, float *mean, float *rstd, void *stream);
+size_t logra_layer_norm_ws_size(int64_t rows, int cols);
+int logra_layer_norm_backward(const void *h, int64_t ld_h, const void *dy, int64_t ld_dy, int dtype, int64_t rows, int cols,
+                              int rms, const uint8_t *mask, const void *gain, const float *mean, const float *rstd,
+                              const void *base, int64_t ld_base, void *dx, int64_t ld_dx, float *dgain, float *dbias,
+                              int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/* logra_preference_loss: pairs of answers, one chosen and one rejected, by the
+ * log ratios of their probabilities to a frozen model's, and the gradient of every
+ * logit (the dy of the last layer, as logra_token_loss gives it):
+ *
+ *     lp_s   = sum over the tokens t of sequence s of (z_t,target - log sum_j exp(z_tj))
+ *     d_i    = beta ((lp_2i - ref_2i) - (lp_2i+1 - ref_2i+1))
+ *     loss_i = w_i ((1 - e) log(1 + exp(-d_i)) + e log(1 + exp(d_i)))
+ *
+ *   logits, ld, target, dlogits, ld_d: as in logra_token_loss (dlogits NULL:
+ *            losses only; may be logits, with ld_d = ld).  A target outside
+ *            [0, vocab) masks its token: not read, no part of lp, zero gradient
+ *   offsets  device int64 [2 n_pairs + 1], not decreasing: sequence s is the rows
+ *            offsets[s] .. offsets[s + 1] - 1; sequence 2i is the chosen and 2i + 1
+ *            the rejected one of pair i.  A sequence may be empty (lp 0).  Rows
+ *            before the first and behind the last sequence are not read, and their
+ *            gradient is zero.  Offsets that decrease or point outside the rows are
+ *            never followed there: results are unspecified, memory is safe
+ *   ref      device fp32 [2 n_pairs] or NULL (0): the frozen model's lp, as this call
+ *            with the frozen model's logits leaves it in logp
+ *   weight   device fp32 [n_pairs] or NULL (1); a pair of weight 0 has loss and
+ *            gradient zero whatever its logits are
+ *   beta, smoothing (e, in [0, 1]): finite
+ *   loss     device fp32 [n_pairs] or NULL;  logp  device fp32 [2 n_pairs]: lp
+ *   ws       logra_preference_loss_ws_size bytes, 256-byte aligned (calls that
+ *            overlap need their own)
+ * A token whose logits are all -inf has lp -inf and a zero gradient.  Where both
+ * ratios are infinite their difference, and with it the pair's loss and gradient,
+ * is NaN.  Sequences are summed in float64, in a fixed order.  rows < 2^31. */
+size_t logra_preference_loss_ws_size(int64_t rows, int n_pairs);
+int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t rows, int vocab, const int64_t *target,
+                          const int64_t *offsets, int n_pairs, const float *ref, const float *weight, double beta,
+                          double smoothing, float *loss, float *logp, void *dlogits, int64_t ld_d, void *ws,
+                          size_t ws_bytes, void *stream);
+
+/* logra_adamw_*: one AdamW step of many tensors, of many models at once.  Each
+ * tensor is `slices` slices of `slice` elements, one behind the other (the adapters
+ * [n][rank][width] of n subsets: n slices), and slice s belongs to group
+ * first_group + s: a group is one model, clipped by its own norm.  For every group,
+ * t = step + 1:
+ *
+ *     norm = |grad of all its slices|,   c = norm > max_norm > 0 ? max_norm / norm : 1
+ *     m = beta1 m + (1 - beta1) c grad,  v = beta2 v + (1 - beta2) (c grad)^2
+ *     param = param (1 - lr' wd) - lr' (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *     work = bf16(param),                lr' = lr lr_scale[group],  wd = decay ? weight_decay : 0
+ *
+ *   param, grad    fp32;  work  bf16 copy of param for the products, or NULL
+ *   m, v           fp32 states (m_scale = v_scale = NULL), or 8-bit ones: m is OCP
+ *                  e4m3, v OCP e5m2, times the scale of their block (fp32
+ *                  [slices][ceil(slice / 256)]; a block is 256 elements of a slice).
+ *                  Zeros are a valid start.  A step gives a block the smallest
+ *                  scale 2^k, k >= -126, that brings its largest magnitude to 448
+ *                  (m) or 57344 (v) or below (1 for a block of zeros), and rounds
+ *                  each element at random: Philox4x32 with 7 rounds under the key
+ *                  `seed` of the counter (i / 4, slice, tensor, t), i the element's
+ *                  place in its slice and tensor its place in the list, gives 4
+ *                  words; element i takes word i % 4, its low half for m and its
+ *                  high half for v.  What lies r / 65536 of the way to the next
+ *                  value in magnitude goes there iff r > that half.  A v that is not
+ *                  zero does not become zero: it takes the smallest code.  What is
+ *                  not finite in fp32 becomes NaN (m) or infinity or NaN (v).  param
+ *                  is computed from m and v before they are rounded
+ *   Elements need their own alignment only: tensors may be parts of flat buffers.
+ *
+ * logra_adamw_plan lays the list out in device memory, once for all steps; the
+ *   tensors must stay where they are while the plan is used.  No two of the step's
+ *   arrays may share memory, except gradients with each other (refused).
+ *   Synchronous, and refused while the stream is captured.  plan: device memory of
+ *   logra_adamw_plan_size bytes, 256-byte aligned; it is also the step's workspace,
+ *   so steps of one plan are ordered by the caller, as their parameters require.
+ *   slice < 2^31, n_groups <= LOGRA_MAX_ADAMW_GROUPS.
+ * logra_adamw_step
+ *   step      device int64: steps done so far; the call adds one.  It and lr_scale
+ *             are read on the device, so a captured step can be replayed
+ *   lr_scale  device fp32 [n_groups] or NULL (1)
+ *   max_norm  0: no clipping.  norms: device fp32 [n_groups] or NULL: the norms.
+ *             Where either is asked for, a group whose norm is not finite is left
+ *             as it is, parameters and states; otherwise what is not finite stays
+ *             in its own elements
+ *   beta1, beta2 in [0, 1), eps in [1e-30, 1e30], weight_decay >= 0
+ * Memory that holds no plan for n_groups is recognised on the device: nothing is
+ * written then.  Reruns from the same state are bitwise identical. */
+typedef struct {
+    float *param;
+    void *work;
+    const float *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t slice;
+    int slices;
+    int first_group;
+    int decay;
+} logra_adamw_tensor;
+
+size_t logra_adamw_plan_size(const logra_adamw_tensor *tensors, int n_tensors, int n_groups);
+int logra_adamw_plan(const logra_adamw_tensor *tensors, int n_tensors, int n_groups, void *plan, size_t plan_bytes,
+                     void *stream);
+int logra_adamw_step(void *plan, size_t plan_bytes, int n_groups, int64_t *step, double lr, double beta1, double beta2,
+                     double eps, double weight_decay, double max_norm, const float *lr_scale, float *norms, uint64_t seed,
+                     void *stream);
 
 #ifdef __cplusplus
 }

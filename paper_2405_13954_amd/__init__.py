@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -24,6 +25,10 @@ __all__ = [
     "logra_influence_ws_size", "logra_influence_scores",
     "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size",
     "logra_adapter_forward_ws_size", "logra_adapter_forward", "logra_adapter_backward", "logra_dropout", "logra_token_loss",
+    "AdamwTensor",
+    "logra_layer_norm_ws_size", "logra_layer_norm_forward", "logra_layer_norm_backward",
+    "logra_preference_loss_ws_size", "logra_preference_loss",
+    "logra_adamw_plan_size", "logra_adamw_plan", "logra_adamw_step",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -33,6 +38,7 @@ F32, BF16, F64 = 0, 1, 2
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_HIP, ERR_NOT_PD, ERR_WORKSPACE, ERR_IO = 0, -1, -2, -3, -4, -5, -6
 MAX_GROUP = 48
 MAX_ACT_COV_GROUP = 32
+ADAMW_BLOCK = 256   # elements that share a scale of the optimizer's 8-bit states
 
 EXPORTED = (
     "logra_last_error", "logra_version",
@@ -50,6 +56,9 @@ EXPORTED = (
     "logra_influence_stream_file", "logra_offload_rows_file",
     "logra_adapter_plan_size", "logra_adapter_plan", "logra_adapter_ws_size",
     "logra_adapter_forward_ws_size", "logra_adapter_forward", "logra_adapter_backward", "logra_dropout", "logra_token_loss",
+    "logra_layer_norm_ws_size", "logra_layer_norm_forward", "logra_layer_norm_backward",
+    "logra_preference_loss_ws_size", "logra_preference_loss",
+    "logra_adamw_plan_size", "logra_adamw_plan", "logra_adamw_step",
 )
 
 
@@ -68,6 +77,13 @@ class LayerDesc(ctypes.Structure):
 class ActCovDesc(ctypes.Structure):
     """logra_act_cov_desc: one KFAC factor of a grouped SYRK launch."""
     _fields_ = [("a", ctypes.c_void_p), ("C", ctypes.c_void_p), ("n", ctypes.c_int)]
+
+
+class AdamwDesc(ctypes.Structure):
+    """logra_adamw_tensor: one tensor of an AdamW step, as the C entry point takes it."""
+    _fields_ = [("param", ctypes.c_void_p), ("work", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("slice", ctypes.c_int64), ("slices", ctypes.c_int), ("first_group", ctypes.c_int), ("decay", ctypes.c_int)]
 
 
 _lib = None
@@ -146,8 +162,23 @@ def lib():
                                              i64, vp, i64, vp, vp, i32, f64, u64, u64, vp, sz, vp]
         L.logra_dropout.argtypes = [vp, i64, i32, i64, i32, f64, u64, u64, vp, i64, vp, i64, vp]
         L.logra_token_loss.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp, vp, i64, vp]
+        L.logra_layer_norm_forward.argtypes = [vp, i64, i32, i64, i32, i32, f64, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp,
+                                               vp, vp]
+        L.logra_layer_norm_ws_size.argtypes = [i64, i32]
+        L.logra_layer_norm_ws_size.restype = sz
+        L.logra_layer_norm_backward.argtypes = [vp, i64, vp, i64, i32, i64, i32, i32, vp, vp, vp, vp, vp, i64, vp, i64, vp,
+                                                vp, i32, vp, sz, vp]
+        L.logra_preference_loss_ws_size.argtypes = [i64, i32]
+        L.logra_preference_loss_ws_size.restype = sz
+        L.logra_preference_loss.argtypes = [vp, i64, i32, i64, i32, vp, vp, i32, vp, vp, f64, f64, vp, vp, vp, i64, vp, sz,
+                                            vp]
+        L.logra_adamw_plan_size.argtypes = [ctypes.POINTER(AdamwDesc), i32, i32]
+        L.logra_adamw_plan_size.restype = sz
+        L.logra_adamw_plan.argtypes = [ctypes.POINTER(AdamwDesc), i32, i32, vp, sz, vp]
+        L.logra_adamw_step.argtypes = [vp, sz, i32, vp, f64, f64, f64, f64, f64, f64, vp, vp, u64, vp]
         for name in ("logra_adapter_plan", "logra_adapter_forward", "logra_adapter_backward", "logra_dropout",
-                     "logra_token_loss"):
+                     "logra_token_loss", "logra_layer_norm_forward", "logra_layer_norm_backward", "logra_preference_loss",
+                     "logra_adamw_plan", "logra_adamw_step"):
             getattr(L, name).restype = ctypes.c_int
         for name in ("logra_store_read_rows", "logra_store_write_rows", "logra_influence_stream_file",
                      "logra_offload_rows_file", "logra_offload_rows", "logra_influence_stream", "logra_pca_topk", "logra_act_cov_accumulate", "logra_act_cov_accumulate_group", "logra_project_layer", "logra_project_layers", "logra_project_layers_noalloc", "logra_cov_accumulate",
@@ -702,3 +733,176 @@ def logra_token_loss(logits, target, loss, dlogits=None, weight=None, stream=Non
                                   _packed(target, (rows,), torch.int64, "target"),
                                   _packed(weight, (rows,), torch.float32, "weight"),
                                   _packed(loss, (rows,), torch.float32, "loss"), pd, ld_d, _stream(stream)))
+
+
+# ------------------------------------------- layer norm, preference loss, AdamW --
+def _on_current(t, stream):
+    """Work on the current device's own streams is for tensors of that device."""
+    if stream is None and t.is_cuda and t.device.index != _torch().cuda.current_device():
+        raise ValueError(f"the tensors are on {t.device}, the current device is {_torch().cuda.current_device()}")
+
+
+def logra_layer_norm_forward(x, y, gain=None, bias=None, eps: float = 1e-5, rms: bool = False, mask=None, residual=None,
+                             h=None, mean=None, rstd=None, stream=None):
+    """h = x + residual, y = (h - mean) rstd gain + bias for each row of x [rows, cols]; with rms, mean = 0 and there is
+    no bias.
+
+    y, residual (None: none) and h (None: not wanted) [rows, cols] of x's dtype; y and h may each be x or residual.  gain
+    and bias [cols] of x's dtype, or None.  mask [rows] uint8: rows with 0 are not read, and give zeros.  mean and rstd
+    [rows] fp32 or None: kept for the backward pass.  Any number of columns up to 32768, at row strides that are
+    multiples of 16 bytes.
+    """
+    torch = _torch()
+    _on_current(x, stream)
+    rows, cols = x.shape
+    dt, f32 = x.dtype, torch.float32
+    px, ld_x = _matrix(x, rows, cols, dt, "x")
+    py, ld_y = _matrix(y, rows, cols, dt, "y")
+    pr, ld_r = _matrix(residual, rows, cols, dt, "residual")
+    ph, ld_h = _matrix(h, rows, cols, dt, "h")
+    _check(lib().logra_layer_norm_forward(
+        px, ld_x, _dtype_code(x), rows, cols, int(rms), eps, _packed(mask, (rows,), torch.uint8, "mask"),
+        _packed(gain, (cols,), dt, "gain"), _packed(bias, (cols,), dt, "bias"), pr, ld_r, ph, ld_h, py, ld_y,
+        _packed(mean, (rows,), f32, "mean"), _packed(rstd, (rows,), f32, "rstd"), _stream(stream)))
+
+
+def logra_layer_norm_ws_size(rows, cols) -> int:
+    return int(lib().logra_layer_norm_ws_size(rows, cols))
+
+
+def logra_layer_norm_backward(h, dy, rstd, mean=None, gain=None, rms: bool = False, mask=None, dx=None, base=None,
+                              dgain=None, dbias=None, accumulate: bool = False, ws=None, stream=None):
+    """Gradients of logra_layer_norm_forward, for h [rows, cols] as it was normalised (x, or x + residual): dx = base
+    (None: zeros) + the gradient of h, [rows, cols], unless None; it may be h, dy or base.  dgain and dbias [cols] fp32
+    (overwritten, or added to with accumulate), or None.  mean, rstd, gain, rms, mask: as in the forward call; a masked
+    row has dx = base.  ws: a workspace of logra_layer_norm_ws_size bytes, allocated for the call when None.
+    """
+    torch = _torch()
+    _on_current(h, stream)
+    rows, cols = h.shape
+    dt, f32 = h.dtype, torch.float32
+    ph, ld_h = _matrix(h, rows, cols, dt, "h")
+    pdy, ld_dy = _matrix(dy, rows, cols, dt, "dy")
+    pb, ld_b = _matrix(base, rows, cols, dt, "base")
+    pdx, ld_dx = _matrix(dx, rows, cols, dt, "dx")
+    if ws is None:
+        ws = _scratch(logra_layer_norm_ws_size(rows, cols), h.device, stream)
+    _check(lib().logra_layer_norm_backward(
+        ph, ld_h, pdy, ld_dy, _dtype_code(h), rows, cols, int(rms), _packed(mask, (rows,), torch.uint8, "mask"),
+        _packed(gain, (cols,), dt, "gain"), _packed(mean, (rows,), f32, "mean"), _packed(rstd, (rows,), f32, "rstd"), pb,
+        ld_b, pdx, ld_dx, _packed(dgain, (cols,), f32, "dgain"), _packed(dbias, (cols,), f32, "dbias"), int(accumulate),
+        ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def logra_preference_loss_ws_size(rows, n_pairs) -> int:
+    return int(lib().logra_preference_loss_ws_size(rows, n_pairs))
+
+
+def logra_preference_loss(logits, target, offsets, logp, loss=None, dlogits=None, ref=None, weight=None, beta: float = 0.1,
+                          smoothing: float = 0.0, ws=None, stream=None):
+    """Loss of pairs of sequences (chosen 2i, rejected 2i + 1) by their log ratios, and the gradient of the logits.
+
+    logits [rows, vocab] and target [rows] int64 as in logra_token_loss; offsets [2 n + 1] int64: where the sequences
+    begin in the rows, and where the last ends.  logp [2 n] fp32: the summed log probabilities of each sequence; ref
+    [2 n] fp32 or None (0): the same of the frozen model.  loss [n] fp32 or None: weight ((1 - smoothing) log(1 +
+    exp(-d)) + smoothing log(1 + exp(d))), d = beta times the difference of logp - ref; weight [n] fp32 or None.
+    dlogits [rows, vocab] or None; may be logits.  ws: a workspace of logra_preference_loss_ws_size bytes, allocated for
+    the call when None.
+    """
+    torch = _torch()
+    _on_current(logits, stream)
+    rows, vocab = logits.shape
+    if offsets.dim() != 1 or offsets.shape[0] % 2 != 1:
+        raise ValueError(f"offsets must hold an even number of sequences and an end, got {tuple(offsets.shape)}")
+    n, f32 = offsets.shape[0] // 2, torch.float32
+    pz, ld = _matrix(logits, rows, vocab, logits.dtype, "logits")
+    pd, ld_d = _matrix(dlogits, rows, vocab, logits.dtype, "dlogits")
+    if ws is None:
+        ws = _scratch(logra_preference_loss_ws_size(rows, n), logits.device, stream)
+    _check(lib().logra_preference_loss(
+        pz, ld, _dtype_code(logits), rows, vocab, _packed(target, (rows,), torch.int64, "target"),
+        _packed(offsets, (2 * n + 1,), torch.int64, "offsets"), n, _packed(ref, (2 * n,), f32, "ref"),
+        _packed(weight, (n,), f32, "weight"), beta, smoothing, _packed(loss, (n,), f32, "loss"),
+        _packed(logp, (2 * n,), f32, "logp"), pd, ld_d, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+class AdamwTensor(NamedTuple):
+    """A tensor of a logra_adamw_plan: `slices` equal slices, one behind the other; slice s belongs to group first_group + s.
+
+    param, grad: contiguous fp32.  m, v: fp32, or float8_e4m3fn and float8_e5m2 with m_scale and v_scale, fp32, a scale
+    for each 256 elements of a slice (ADAMW_BLOCK).  work: a bf16 copy of param, or None.  decay: whether the step's
+    weight_decay applies."""
+    param: object
+    grad: object
+    m: object
+    v: object
+    m_scale: object = None
+    v_scale: object = None
+    work: object = None
+    slices: int = 1
+    first_group: int = 0
+    decay: bool = True
+
+
+def _adamw_desc(t: AdamwTensor, i: int) -> AdamwDesc:
+    torch = _torch()
+    n, slices = t.param.numel(), t.slices
+    if slices < 1 or n % slices:
+        raise ValueError(f"tensor {i}: {n} elements are not {slices} equal slices")
+    eight = t.m_scale is not None or t.v_scale is not None
+    blocks = -(-(n // slices) // ADAMW_BLOCK) * slices
+
+    def at(a, name, dtype, count):
+        if a is None:
+            return None
+        if a.dtype != dtype or a.numel() != count or not a.is_contiguous():
+            raise ValueError(f"{name} of tensor {i} must be {count} contiguous elements of {dtype}")
+        return a.data_ptr()
+
+    return AdamwDesc(at(t.param, "param", torch.float32, n), at(t.work, "work", torch.bfloat16, n),
+                     at(t.grad, "grad", torch.float32, n),
+                     at(t.m, "m", torch.float8_e4m3fn if eight else torch.float32, n),
+                     at(t.v, "v", torch.float8_e5m2 if eight else torch.float32, n),
+                     at(t.m_scale, "m_scale", torch.float32, blocks), at(t.v_scale, "v_scale", torch.float32, blocks),
+                     n // slices, slices, t.first_group, int(t.decay))
+
+
+def logra_adamw_plan_size(tensors, n_groups: int) -> int:
+    descs = (AdamwDesc * len(tensors))(*[_adamw_desc(t, i) for i, t in enumerate(tensors)])
+    return int(lib().logra_adamw_plan_size(descs, len(tensors), n_groups))
+
+
+class AdamwPlan(NamedTuple):
+    """What logra_adamw_plan returns: the plan's memory, and the tensors, which have to outlive it."""
+    memory: object
+    tensors: tuple
+    n_groups: int
+
+
+def logra_adamw_plan(tensors, n_groups: int, stream=None) -> AdamwPlan:
+    """Lay a list of AdamwTensor out for logra_adamw_step, once for all steps.  Groups 0 .. n_groups - 1 are models of
+    their own, each clipped by its own norm.  Synchronous."""
+    torch = _torch()
+    descs = (AdamwDesc * len(tensors))(*[_adamw_desc(t, i) for i, t in enumerate(tensors)])
+    if tensors:
+        _on_current(tensors[0].param, stream)
+    device = tensors[0].param.device if tensors else torch.device("cuda")
+    memory = _scratch(int(lib().logra_adamw_plan_size(descs, len(tensors), n_groups)), device, stream)
+    _check(lib().logra_adamw_plan(descs, len(tensors), n_groups, memory.data_ptr(), memory.numel(), _stream(stream)))
+    return AdamwPlan(memory, tuple(tensors), n_groups)
+
+
+def logra_adamw_step(plan: AdamwPlan, step, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                     weight_decay: float = 0.0, max_norm: float = 0.0, lr_scale=None, norms=None, seed: int = 0,
+                     stream=None):
+    """One AdamW step of all tensors of the plan.  step [1] int64 (device): steps done so far, one is added.  lr_scale
+    [n_groups] fp32 or None: factors of lr, read on the device.  max_norm: each group's gradient is scaled down to this
+    norm (0: not); norms [n_groups] fp32 or None: the norms before that.  With either, a group whose norm is not finite is
+    left as it is.  seed: of the random rounding of 8-bit states."""
+    torch = _torch()
+    _on_current(plan.memory, stream)
+    n, f32 = plan.n_groups, torch.float32
+    _check(lib().logra_adamw_step(
+        plan.memory.data_ptr(), plan.memory.numel(), n, _packed(step, (1,), torch.int64, "step"), lr, beta1, beta2, eps,
+        weight_decay, max_norm, _packed(lr_scale, (n,), f32, "lr_scale"), _packed(norms, (n,), f32, "norms"), seed,
+        _stream(stream)))

@@ -3,6 +3,7 @@
 // HIP call; pointer checks follow (hipPointerGetAttributes); then launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -1010,6 +1011,370 @@ int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, in
     const hipError_t e = logra::launch_token_loss(logits, ld, dtype == LOGRA_BF16, rows, vocab, target, weight, loss,
                                                   dlogits, ld_d, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "token loss launch");
+    return ok();
+}
+
+}  // extern "C"
+
+// ------------------------------------------- layer norm, preference loss, AdamW --
+namespace {
+
+// What a call reads and what it writes.  Every output is apart from the other outputs and from the inputs, but for inputs
+// that the call allows it to be in place of: a thread reads its elements of those before it writes them.
+struct Operand {
+    const char *name;
+    Region at;
+    bool in_place;   // an input that an output of the same rows may replace
+};
+Region flat(const void *p, int64_t n, size_t bytes) {
+    const uint64_t size = static_cast<uint64_t>(n) * bytes;
+    return {static_cast<uint64_t>(reinterpret_cast<uintptr_t>(p)), size > 0 ? size : 1, size, 1};
+}
+int check_operands(const std::vector<Operand> &in, const std::vector<Operand> &out) {
+    for (size_t i = 0; i < out.size(); ++i) {
+        if (!out[i].at.at) continue;
+        for (const Operand &r : in)
+            if (r.at.at) TRY(check_apart(r.name, r.at, out[i].name, out[i].at, r.in_place && out[i].in_place));
+        for (size_t j = 0; j < i; ++j)
+            if (out[j].at.at) TRY(check_apart(out[j].name, out[j].at, out[i].name, out[i].at, false));
+    }
+    return LOGRA_OK;
+}
+
+static_assert(LOGRA_MAX_NORM_COLS == logra::kMaxNormCols && LOGRA_MAX_ADAMW_GROUPS == logra::kMaxAdamwGroups &&
+                  LOGRA_ADAMW_BLOCK == logra::kAdamwBlock,
+              "the kernels' limits are the public ones");
+int check_norm_sizes(int dtype, int64_t rows, int cols) {
+    if (!valid_dtype(dtype)) return fail(LOGRA_ERR_INVALID_ARG, "bad dtype");
+    if (rows < 0 || cols <= 0) return fail(LOGRA_ERR_INVALID_ARG, "need rows >= 0 and cols > 0");
+    if (rows > INT32_MAX) return fail(LOGRA_ERR_UNSUPPORTED, "rows must be < 2^31");
+    if (cols > LOGRA_MAX_NORM_COLS) return fail(LOGRA_ERR_UNSUPPORTED, "cols must be <= %d", LOGRA_MAX_NORM_COLS);
+    return LOGRA_OK;
+}
+
+int norm_forward(const logra::NormForward &n, int dtype) {
+    const int es = static_cast<int>(esize(dtype));
+    TRY(check_stride("x", n.ld_x, n.rows, n.cols, dtype));
+    TRY(check_stride("y", n.ld_y, n.rows, n.cols, dtype));
+    if (n.residual) TRY(check_stride("residual", n.ld_res, n.rows, n.cols, dtype));
+    if (n.h) TRY(check_stride("h", n.ld_h, n.rows, n.cols, dtype));
+    const auto matrix = [&](const void *p, int64_t ld) { return region(p, ld, n.cols, n.rows, dtype); };
+    TRY(check_operands({{"x", matrix(n.x, n.ld_x), true}, {"residual", matrix(n.residual, n.ld_res), true},
+                        {"gain", flat(n.gain, n.cols, es), false}, {"bias", flat(n.bias, n.cols, es), false},
+                        {"mask", flat(n.mask, n.rows, 1), false}},
+                       {{"y", matrix(n.y, n.ld_y), true}, {"h", matrix(n.h, n.ld_h), true},
+                        {"mean", flat(n.mean, n.rows, 4), false}, {"rstd", flat(n.rstd, n.rows, 4), false}}));
+    TRY(check_matrix(n.x, "x", n.rows, n.ld_x, n.cols, dtype));
+    TRY(check_matrix(n.y, "y", n.rows, n.ld_y, n.cols, dtype));
+    if (n.residual) TRY(check_matrix(n.residual, "residual", n.rows, n.ld_res, n.cols, dtype));
+    if (n.h) TRY(check_matrix(n.h, "h", n.rows, n.ld_h, n.cols, dtype));
+    if (n.mask) TRY(check_dev(n.mask, "mask", 1));
+    if (n.gain) TRY(check_dev(n.gain, "gain", 16));
+    if (n.bias) TRY(check_dev(n.bias, "bias", 16));
+    if (n.mean) TRY(check_dev(n.mean, "mean", 4));
+    if (n.rstd) TRY(check_dev(n.rstd, "rstd", 4));
+    return LOGRA_OK;
+}
+
+int norm_backward(const logra::NormBackward &n, int dtype, size_t ws_bytes) {
+    const int es = static_cast<int>(esize(dtype));
+    if (n.rows > 0) {
+        TRY(check_stride("h", n.ld_h, n.rows, n.cols, dtype));
+        TRY(check_stride("dy", n.ld_dy, n.rows, n.cols, dtype));
+        if (n.dx) TRY(check_stride("dx", n.ld_dx, n.rows, n.cols, dtype));
+        if (n.base) TRY(check_stride("base", n.ld_base, n.rows, n.cols, dtype));
+        const auto matrix = [&](const void *p, int64_t ld) { return region(p, ld, n.cols, n.rows, dtype); };
+        TRY(check_operands({{"h", matrix(n.h, n.ld_h), true}, {"dy", matrix(n.dy, n.ld_dy), true},
+                            {"base", matrix(n.base, n.ld_base), true}, {"gain", flat(n.gain, n.cols, es), false},
+                            {"mask", flat(n.mask, n.rows, 1), false}, {"mean", flat(n.mean, n.rows, 4), false},
+                            {"rstd", flat(n.rstd, n.rows, 4), false}},
+                           {{"dx", matrix(n.dx, n.ld_dx), true}, {"dgain", flat(n.dgain, n.cols, 4), false},
+                            {"dbias", flat(n.dbias, n.cols, 4), false},
+                            {"ws", flat(n.ws, static_cast<int64_t>(ws_bytes), 1), false}}));
+        TRY(check_matrix(n.h, "h", n.rows, n.ld_h, n.cols, dtype));
+        TRY(check_matrix(n.dy, "dy", n.rows, n.ld_dy, n.cols, dtype));
+        if (n.dx) TRY(check_matrix(n.dx, "dx", n.rows, n.ld_dx, n.cols, dtype));
+        if (n.base) TRY(check_matrix(n.base, "base", n.rows, n.ld_base, n.cols, dtype));
+        if (n.mask) TRY(check_dev(n.mask, "mask", 1));
+        if (n.gain) TRY(check_dev(n.gain, "gain", 16));
+        if (!n.rms) TRY(check_dev(n.mean, "mean", 4));
+        TRY(check_dev(n.rstd, "rstd", 4));
+    }
+    if (n.dgain) TRY(check_dev(n.dgain, "dgain", 4));
+    if (n.dbias) TRY(check_dev(n.dbias, "dbias", 4));
+    if (n.rows > 0 && (n.dgain || n.dbias)) TRY(check_ws(n.ws, ws_bytes, logra_layer_norm_ws_size(n.rows, n.cols)));
+    return LOGRA_OK;
+}
+
+// The chunks of a list of tensors, or -1 where there are more than a plan holds; sizes only.
+int64_t adamw_chunks(const logra_adamw_tensor *tensors, int n_tensors) {
+    int64_t chunks = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const logra_adamw_tensor &t = tensors[i];
+        if (t.slice < 0 || t.slices < 0 || t.slice > INT32_MAX) return -1;
+        chunks += (t.slice + logra::kAdamwChunk - 1) / logra::kAdamwChunk * t.slices;
+        if (chunks > INT32_MAX) return -1;
+    }
+    return chunks;
+}
+
+// Everything of a tensor of the list that needs no HIP call.
+int check_adamw_tensor(const logra_adamw_tensor &t, int i, int n_groups) {
+    if (t.slice < 0 || t.slices < 0) return fail(LOGRA_ERR_INVALID_ARG, "tensor %d: slice and slices must be >= 0", i);
+    if (t.slice > INT32_MAX) return fail(LOGRA_ERR_UNSUPPORTED, "tensor %d: a slice must have fewer than 2^31 elements", i);
+    if (t.slices > 0 && (t.first_group < 0 || t.first_group > n_groups - t.slices))
+        return fail(LOGRA_ERR_INVALID_ARG, "tensor %d: its groups are not within [0, %d)", i, n_groups);
+    if ((t.m_scale == nullptr) != (t.v_scale == nullptr))
+        return fail(LOGRA_ERR_INVALID_ARG, "tensor %d: m_scale and v_scale go together", i);
+    return LOGRA_OK;
+}
+
+struct Span {
+    uint64_t begin, end;
+    bool written;
+    int tensor;
+    const char *name;
+};
+
+// The memory of a tensor's n elements: device memory at both ends, listed in `spans`.
+int add_span(std::vector<Span> &spans, const void *p, const char *name, int tensor, int64_t n, size_t bytes, size_t align,
+             bool written) {
+    char what[64];
+    snprintf(what, sizeof what, "%s of tensor %d", name, tensor);
+    TRY(check_dev(p, what, align));
+    TRY(check_dev(static_cast<const char *>(p) + (n - 1) * static_cast<int64_t>(bytes), what, 1));
+    const uint64_t at = static_cast<uint64_t>(reinterpret_cast<uintptr_t>(p));
+    spans.push_back({at, at + static_cast<uint64_t>(n) * bytes, written, tensor, name});
+    return LOGRA_OK;
+}
+
+// No memory that the step writes is anything else of it.
+int check_spans(std::vector<Span> &spans) {
+    std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.begin < b.begin; });
+    const Span *far = nullptr, *far_written = nullptr;   // of those before: the one that ends last
+    for (const Span &s : spans) {
+        const Span *hit = s.written ? far : far_written;
+        if (hit && hit->end > s.begin)
+            return fail(LOGRA_ERR_INVALID_ARG, "%s of tensor %d and %s of tensor %d share memory", hit->name, hit->tensor,
+                        s.name, s.tensor);
+        if (!far || s.end > far->end) far = &s;
+        if (s.written && (!far_written || s.end > far_written->end)) far_written = &s;
+    }
+    return LOGRA_OK;
+}
+
+int adamw_plan(const logra_adamw_tensor *tensors, int n_tensors, int n_groups, void *plan, size_t plan_bytes,
+               hipStream_t stream) {
+    const int64_t chunks = adamw_chunks(tensors, n_tensors);
+    if (chunks < 0) return fail(LOGRA_ERR_UNSUPPORTED, "too many elements for one plan");
+    const size_t need = logra::adamw_plan_bytes(n_groups, static_cast<uint32_t>(chunks));
+    if (plan == nullptr || plan_bytes < need)
+        return fail(LOGRA_ERR_WORKSPACE, "the plan needs %zu bytes, got %zu", need, plan ? plan_bytes : 0);
+    std::vector<Span> spans;
+    for (int i = 0; i < n_tensors; ++i) {
+        const logra_adamw_tensor &t = tensors[i];
+        const int64_t n = t.slice * t.slices, blocks = (t.slice + logra::kAdamwBlock - 1) / logra::kAdamwBlock * t.slices;
+        if (n == 0) continue;
+        const bool eight = t.m_scale != nullptr;
+        TRY(add_span(spans, t.param, "param", i, n, 4, 4, true));
+        TRY(add_span(spans, t.grad, "grad", i, n, 4, 4, false));
+        TRY(add_span(spans, t.m, "m", i, n, eight ? 1 : 4, eight ? 1 : 4, true));
+        TRY(add_span(spans, t.v, "v", i, n, eight ? 1 : 4, eight ? 1 : 4, true));
+        if (t.work) TRY(add_span(spans, t.work, "work", i, n, 2, 2, true));
+        if (eight) {
+            TRY(add_span(spans, t.m_scale, "m_scale", i, blocks, 4, 4, true));
+            TRY(add_span(spans, t.v_scale, "v_scale", i, blocks, 4, 4, true));
+        }
+    }
+    TRY(check_dev(plan, "plan", 256));
+    const uint64_t at = static_cast<uint64_t>(reinterpret_cast<uintptr_t>(plan));
+    spans.push_back({at, at + need, true, -1, "the plan"});
+    TRY(check_spans(spans));
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    hipError_t e = hipStreamIsCapturing(stream, &capture);
+    if (e != hipSuccess) return hip_fail(e, "adamw plan");
+    if (capture != hipStreamCaptureStatusNone)
+        return fail(LOGRA_ERR_UNSUPPORTED, "a plan is made before the capture of the steps that use it");
+
+    std::vector<uint64_t> host((need + 7) / 8, 0);
+    char *base = reinterpret_cast<char *>(host.data());
+    auto *header = reinterpret_cast<logra::AdamwHeader *>(base);
+    *header = {logra::kAdamwMagic, need, static_cast<uint32_t>(chunks), n_groups};
+    auto *starts = reinterpret_cast<uint32_t *>(base + logra::adamw_starts_at(n_groups));
+    auto *out = reinterpret_cast<logra::AdamwChunk *>(base + logra::adamw_chunks_at(n_groups, static_cast<uint32_t>(chunks)));
+    for (int i = 0; i < n_tensors; ++i) {
+        const auto per = static_cast<uint32_t>((tensors[i].slice + logra::kAdamwChunk - 1) / logra::kAdamwChunk);
+        for (int s = 0; s < tensors[i].slices; ++s) starts[tensors[i].first_group + s + 1] += per;
+    }
+    for (int g = 0; g < n_groups; ++g) starts[g + 1] += starts[g];
+    std::vector<uint32_t> next(starts, starts + n_groups);
+    for (int i = 0; i < n_tensors; ++i) {
+        const logra_adamw_tensor &t = tensors[i];
+        const bool eight = t.m_scale != nullptr;
+        const size_t state = eight ? 1 : 4;
+        const int64_t blocks = (t.slice + logra::kAdamwBlock - 1) / logra::kAdamwBlock;
+        for (int s = 0; s < t.slices; ++s)
+            for (int64_t first = 0; first < t.slice; first += logra::kAdamwChunk) {
+                const int64_t n = s * t.slice + first, block = s * blocks + first / logra::kAdamwBlock;
+                const int group = t.first_group + s;
+                const int64_t left = t.slice - first;
+                *out++ = {t.param + n,
+                          t.work ? static_cast<char *>(t.work) + 2 * n : nullptr,
+                          t.grad + n,
+                          static_cast<char *>(t.m) + n * state,
+                          static_cast<char *>(t.v) + n * state,
+                          eight ? t.m_scale + block : nullptr,
+                          eight ? t.v_scale + block : nullptr,
+                          static_cast<uint32_t>(group),
+                          next[group]++,
+                          static_cast<uint32_t>(i),
+                          static_cast<uint32_t>(s),
+                          static_cast<uint32_t>(first),
+                          static_cast<int>(left < logra::kAdamwChunk ? left : logra::kAdamwChunk),
+                          t.decay != 0};
+            }
+    }
+    e = hipMemcpyAsync(plan, base, need, hipMemcpyHostToDevice, stream);
+    const hipError_t waited = hipStreamSynchronize(stream);   // the list on the host ends with this call
+    if (e == hipSuccess) e = waited;
+    if (e != hipSuccess) return hip_fail(e, "adamw plan");
+    return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t logra_layer_norm_ws_size(int64_t rows, int cols) {
+    if (rows <= 0 || cols <= 0 || rows > INT32_MAX || cols > LOGRA_MAX_NORM_COLS) return 0;
+    return round256(logra::norm_ws_bytes(rows, cols));
+}
+
+int logra_layer_norm_forward(const void *x, int64_t ld_x, int dtype, int64_t rows, int cols, int rms, double eps,
+                             const uint8_t *mask, const void *gain, const void *bias, const void *residual, int64_t ld_res,
+                             void *h, int64_t ld_h, void *y, int64_t ld_y, float *mean, float *rstd, void *stream) {
+    TRY(check_norm_sizes(dtype, rows, cols));
+    if (!(eps >= 1e-30 && eps <= 1e30)) return fail(LOGRA_ERR_INVALID_ARG, "eps must be in [1e-30, 1e30]");
+    if (rms && (bias || mean)) return fail(LOGRA_ERR_INVALID_ARG, "a norm without the mean has no bias and no mean");
+    if (rows == 0) return ok();
+    const logra::NormForward n = {x, residual, h, y, ld_x, ld_res, ld_h, ld_y, rows, cols, dtype == LOGRA_BF16, rms != 0,
+                                  static_cast<float>(eps), mask, gain, bias, mean, rstd};
+    TRY(norm_forward(n, dtype));
+    const hipError_t e = logra::launch_norm_forward(n, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "layer norm launch");
+    return ok();
+}
+
+int logra_layer_norm_backward(const void *h, int64_t ld_h, const void *dy, int64_t ld_dy, int dtype, int64_t rows, int cols,
+                              int rms, const uint8_t *mask, const void *gain, const float *mean, const float *rstd,
+                              const void *base, int64_t ld_base, void *dx, int64_t ld_dx, float *dgain, float *dbias,
+                              int accumulate, void *ws, size_t ws_bytes, void *stream) {
+    TRY(check_norm_sizes(dtype, rows, cols));
+    if (base && !dx) return fail(LOGRA_ERR_INVALID_ARG, "base without dx");
+    if (rms && (dbias || mean)) return fail(LOGRA_ERR_INVALID_ARG, "a norm without the mean has no bias and no mean");
+    if (!dx && !dgain && !dbias) return ok();
+    const logra::NormBackward n = {h, dy, base, dx, ld_h, ld_dy, ld_base, ld_dx, rows, cols, dtype == LOGRA_BF16, rms != 0,
+                                   accumulate != 0, mask, gain, mean, rstd, dgain, dbias, ws};
+    TRY(norm_backward(n, dtype, ws_bytes));
+    const hipError_t e = logra::launch_norm_backward(n, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "layer norm backward launch");
+    return ok();
+}
+
+size_t logra_preference_loss_ws_size(int64_t rows, int n_pairs) {
+    if (rows <= 0 || n_pairs <= 0 || rows > INT32_MAX) return 0;
+    return round256(logra::preference_ws_bytes(rows));
+}
+
+int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t rows, int vocab, const int64_t *target,
+                          const int64_t *offsets, int n_pairs, const float *ref, const float *weight, double beta,
+                          double smoothing, float *loss, float *logp, void *dlogits, int64_t ld_d, void *ws,
+                          size_t ws_bytes, void *stream) {
+    if (!valid_dtype(dtype)) return fail(LOGRA_ERR_INVALID_ARG, "bad dtype");
+    if (rows < 0 || vocab <= 0 || n_pairs < 0) return fail(LOGRA_ERR_INVALID_ARG, "need rows >= 0, vocab > 0, n_pairs >= 0");
+    if (rows > INT32_MAX) return fail(LOGRA_ERR_UNSUPPORTED, "rows must be < 2^31");
+    if (vocab > (1 << 30)) return fail(LOGRA_ERR_UNSUPPORTED, "vocab must be <= 2^30");
+    if (n_pairs > (1 << 29)) return fail(LOGRA_ERR_UNSUPPORTED, "n_pairs must be <= 2^29");
+    if (!std::isfinite(beta)) return fail(LOGRA_ERR_INVALID_ARG, "beta must be finite");
+    if (!(smoothing >= 0.0 && smoothing <= 1.0)) return fail(LOGRA_ERR_INVALID_ARG, "smoothing must be in [0, 1]");
+    if (n_pairs == 0) {
+        if (rows == 0 || !dlogits) return ok();
+        return fail(LOGRA_ERR_INVALID_ARG, "rows without pairs");
+    }
+    if (rows > 0) {
+        TRY(check_stride("logits", ld, rows, vocab, dtype));
+        if (dlogits) TRY(check_stride("dlogits", ld_d, rows, vocab, dtype));
+        const int64_t n = n_pairs;
+        TRY(check_operands({{"logits", region(logits, ld, vocab, rows, dtype), true}, {"target", flat(target, rows, 8), false},
+                            {"offsets", flat(offsets, 2 * n + 1, 8), false}, {"ref", flat(ref, 2 * n, 4), false},
+                            {"weight", flat(weight, n, 4), false}},
+                           {{"dlogits", region(dlogits, ld_d, vocab, rows, dtype), true}, {"loss", flat(loss, n, 4), false},
+                            {"logp", flat(logp, 2 * n, 4), false},
+                            {"ws", flat(ws, static_cast<int64_t>(ws_bytes), 1), false}}));
+        TRY(check_matrix(logits, "logits", rows, ld, vocab, dtype));
+        TRY(check_dev(target, "target", 8));
+        if (dlogits) TRY(check_matrix(dlogits, "dlogits", rows, ld_d, vocab, dtype));
+        TRY(check_ws(ws, ws_bytes, logra_preference_loss_ws_size(rows, n_pairs)));
+    }
+    TRY(check_dev(offsets, "offsets", 8));
+    if (ref) TRY(check_dev(ref, "ref", 4));
+    if (weight) TRY(check_dev(weight, "weight", 4));
+    if (loss) TRY(check_dev(loss, "loss", 4));
+    TRY(check_dev(logp, "logp", 4));
+    const logra::PreferenceLoss p = {logits, ld, rows, vocab, n_pairs, dtype == LOGRA_BF16, target, offsets, ref, weight,
+                                     beta, smoothing, loss, logp, dlogits, ld_d, ws};
+    const hipError_t e = logra::launch_preference_loss(p, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "preference loss launch");
+    return ok();
+}
+
+size_t logra_adamw_plan_size(const logra_adamw_tensor *tensors, int n_tensors, int n_groups) {
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors) || n_groups <= 0 || n_groups > LOGRA_MAX_ADAMW_GROUPS) return 0;
+    const int64_t chunks = adamw_chunks(tensors, n_tensors);
+    return chunks < 0 ? 0 : round256(logra::adamw_plan_bytes(n_groups, static_cast<uint32_t>(chunks)));
+}
+
+int logra_adamw_plan(const logra_adamw_tensor *tensors, int n_tensors, int n_groups, void *plan, size_t plan_bytes,
+                     void *stream) {
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return fail(LOGRA_ERR_INVALID_ARG, "tensors is NULL");
+    if (n_groups <= 0) return fail(LOGRA_ERR_INVALID_ARG, "n_groups must be > 0");
+    if (n_groups > LOGRA_MAX_ADAMW_GROUPS)
+        return fail(LOGRA_ERR_UNSUPPORTED, "n_groups must be <= %d", LOGRA_MAX_ADAMW_GROUPS);
+    for (int i = 0; i < n_tensors; ++i) TRY(check_adamw_tensor(tensors[i], i, n_groups));
+    try {
+        return adamw_plan(tensors, n_tensors, n_groups, plan, plan_bytes, static_cast<hipStream_t>(stream));
+    } catch (...) {
+        return fail(LOGRA_ERR_UNSUPPORTED, "no host memory for the plan");
+    }
+}
+
+int logra_adamw_step(void *plan, size_t plan_bytes, int n_groups, int64_t *step, double lr, double beta1, double beta2,
+                     double eps, double weight_decay, double max_norm, const float *lr_scale, float *norms, uint64_t seed,
+                     void *stream) {
+    if (n_groups <= 0) return fail(LOGRA_ERR_INVALID_ARG, "n_groups must be > 0");
+    if (n_groups > LOGRA_MAX_ADAMW_GROUPS)
+        return fail(LOGRA_ERR_UNSUPPORTED, "n_groups must be <= %d", LOGRA_MAX_ADAMW_GROUPS);
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0))
+        return fail(LOGRA_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
+    if (!(eps >= 1e-30 && eps <= 1e30)) return fail(LOGRA_ERR_INVALID_ARG, "eps must be in [1e-30, 1e30]");
+    if (!(std::fabs(lr) <= 1e30) || !(weight_decay >= 0.0 && weight_decay <= 1e30))
+        return fail(LOGRA_ERR_INVALID_ARG, "lr and weight_decay must be finite, weight_decay >= 0");
+    if (!(max_norm >= 0.0)) return fail(LOGRA_ERR_INVALID_ARG, "max_norm must be >= 0 (0: no clipping)");
+    const size_t least = logra::adamw_plan_bytes(n_groups, 0);
+    if (plan == nullptr || plan_bytes < least)
+        return fail(LOGRA_ERR_WORKSPACE, "a plan has at least %zu bytes, got %zu", least, plan ? plan_bytes : 0);
+    TRY(check_operands({{"lr_scale", flat(lr_scale, n_groups, 4), false}},
+                       {{"plan", flat(plan, static_cast<int64_t>(plan_bytes), 1), false}, {"step", flat(step, 1, 8), false},
+                        {"norms", flat(norms, n_groups, 4), false}}));
+    TRY(check_dev(plan, "plan", 256));
+    TRY(check_dev(step, "step", 8));
+    if (lr_scale) TRY(check_dev(lr_scale, "lr_scale", 4));
+    if (norms) TRY(check_dev(norms, "norms", 4));
+    const logra::AdamwHyper y = {lr, beta1, beta2, eps, weight_decay, max_norm,
+                                 {static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32)}};
+    const hipError_t e = logra::launch_adamw_step(plan, plan_bytes, n_groups, step, y, lr_scale, norms,
+                                                  static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "adamw launch");
     return ok();
 }
 

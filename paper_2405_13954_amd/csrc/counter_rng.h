@@ -21,10 +21,8 @@ struct DropArgs {
     uint32_t off[2];      // offset
 };
 
-// The 128 bits of chunk (row, chunk): word j holds column 2j in its low half
-// and column 2j + 1 in its high half, as a pair of bf16 values is packed.
-__device__ __forceinline__ u32x4 drop_bits(const DropArgs &d, uint32_t row, uint32_t chunk) {
-    uint32_t x0 = chunk, x1 = row, x2 = d.off[0], x3 = d.off[1], k0 = d.key[0], k1 = d.key[1];
+// Philox4x32-7: 128 bits for the counter (x0, x1, x2, x3) under the key (k0, k1).
+__device__ __forceinline__ u32x4 philox(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3, uint32_t k0, uint32_t k1) {
 #pragma unroll
     for (int i = 0; i < 7; ++i) {
         const uint64_t a = static_cast<uint64_t>(x0) * 0xD2511F53u, b = static_cast<uint64_t>(x2) * 0xCD9E8D57u;
@@ -41,6 +39,12 @@ __device__ __forceinline__ u32x4 drop_bits(const DropArgs &d, uint32_t row, uint
     w[2] = x2;
     w[3] = x3;
     return w;
+}
+
+// The 128 bits of chunk (row, chunk): word j holds column 2j in its low half
+// and column 2j + 1 in its high half, as a pair of bf16 values is packed.
+__device__ __forceinline__ u32x4 drop_bits(const DropArgs &d, uint32_t row, uint32_t chunk) {
+    return philox(chunk, row, d.off[0], d.off[1], d.key[0], d.key[1]);
 }
 
 // 0xFFFF in each half of w that is kept (half >= thr), 0 in the others.

@@ -187,4 +187,93 @@ hipError_t launch_dropout(const void *x, int64_t ld_x, bool bf16, int64_t rows, 
 hipError_t launch_token_loss(const void *logits, int64_t ld, bool bf16, int64_t rows, int vocab, const int64_t *target,
                              const float *weight, float *loss, void *dlogits, int64_t ld_d, hipStream_t s);
 
+// Layer norm (norm.hip), preference loss (preference.hip), AdamW (adamw.hip).
+constexpr int kMaxNormCols = 32768;   // a row is held in one workgroup's registers
+struct NormForward {
+    const void *x, *residual;
+    void *h, *y;
+    int64_t ld_x, ld_res, ld_h, ld_y, rows;
+    int cols;
+    bool bf16, rms;
+    float eps;
+    const uint8_t *mask;
+    const void *gain, *bias;
+    float *mean, *rstd;
+};
+hipError_t launch_norm_forward(const NormForward &n, hipStream_t s);
+struct NormBackward {
+    const void *h, *dy, *base;
+    void *dx;
+    int64_t ld_h, ld_dy, ld_base, ld_dx, rows;
+    int cols;
+    bool bf16, rms, accumulate;
+    const uint8_t *mask;
+    const void *gain;
+    const float *mean, *rstd;
+    float *dgain, *dbias;
+    void *ws;
+};
+size_t norm_ws_bytes(int64_t rows, int cols);
+hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s);
+
+struct PreferenceLoss {
+    const void *logits;
+    int64_t ld, rows;
+    int vocab, pairs;
+    bool bf16;
+    const int64_t *target, *offsets;
+    const float *ref, *weight;
+    double beta, smoothing;
+    float *loss, *logp;
+    void *dlogits;
+    int64_t ld_d;
+    void *ws;
+};
+size_t preference_ws_bytes(int64_t rows);
+hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s);
+
+// The AdamW plan: a header, a record for each group, each group's range of sums, the sums, and the chunks.
+constexpr int kAdamwChunk = 2048;   // elements of a chunk, all of one slice
+constexpr int kAdamwBlock = 256;    // elements that share a scale of the 8-bit states
+constexpr int kMaxAdamwGroups = 65536;
+constexpr uint64_t kAdamwMagic = 0x314e4c5057416461ull;
+struct AdamwHeader {
+    uint64_t magic, bytes;
+    uint32_t chunks;
+    int groups;
+};
+struct AdamwGroup {     // written by every step
+    double clip;
+    float lr, rate, root;   // lr, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+    int skip;
+    int64_t step;
+};
+struct AdamwChunk {
+    float *param;
+    void *work;
+    const float *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;   // the chunk's first block's; NULL: fp32 states
+    uint32_t group, slot;       // slot: where its sum goes, the groups' chunks one behind the other
+    uint32_t tensor, slice, first;
+    int count, decay;
+};
+__host__ __device__ inline size_t adamw_groups_at() { return 256; }
+__host__ __device__ inline size_t adamw_starts_at(int groups) { return adamw_groups_at() + align256(groups * sizeof(AdamwGroup)); }
+__host__ __device__ inline size_t adamw_parts_at(int groups) {
+    return adamw_starts_at(groups) + align256((groups + size_t{1}) * sizeof(uint32_t));
+}
+__host__ __device__ inline size_t adamw_chunks_at(int groups, uint32_t chunks) {
+    return adamw_parts_at(groups) + align256(chunks * sizeof(double));
+}
+__host__ __device__ inline size_t adamw_plan_bytes(int groups, uint32_t chunks) {
+    return adamw_chunks_at(groups, chunks) + align256(chunks * sizeof(AdamwChunk));
+}
+struct AdamwHyper {
+    double lr, beta1, beta2, eps, decay, max_norm;
+    uint32_t key[2];
+};
+hipError_t launch_adamw_step(void *plan, size_t plan_bytes, int groups, int64_t *step, const AdamwHyper &y,
+                             const float *lr_scale, float *norms, hipStream_t s);
+
 }  // namespace logra

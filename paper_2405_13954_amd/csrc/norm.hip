@@ -1,0 +1,397 @@
+// Layer norm of rows, with or without the mean, and its backward pass:
+//
+//   forward   h = x + residual,  y = (h - mean) rstd gain + bias,  rstd = 1 / sqrt(mean((h - mean)^2) + eps)
+//   backward  xh = (h - mean) rstd,  c = dy gain,  dx = base + rstd (c - avg(c) - xh avg(c xh)),
+//             dgain = sum_t dy xh,  dbias = sum_t dy
+//
+// (rms: mean = 0, and no avg(c).)  A row is held in the registers of a team of threads, each with NV of its 16-byte
+// vectors, so memory sees every tensor once, which is what bounds both passes.  The variance is that of the differences
+// from the mean, formed after the mean: no cancellation.  Sums and statistics are fp32.
+//
+// Backward: a workgroup walks rows a grid apart and keeps the sums for dgain and dbias of its columns in registers; the
+// next row's vectors are loaded before the current row's sums are known.  The workgroups' sums go to the workspace, and a
+// second launch adds them in order, so that reruns give the same bits.
+#include "internal.h"
+#include "vec16.h"
+
+namespace logra {
+namespace {
+
+struct FwdArgs {
+    const char *x, *res;
+    char *h, *y;
+    int64_t ld_x, ld_r, ld_h, ld_y, rows;
+    const uint8_t *mask;
+    const char *gain, *bias;
+    float *mean, *rstd;
+    int cols;
+    float eps;
+};
+
+struct BwdArgs {
+    const char *h, *dy, *base;
+    char *dx;
+    int64_t ld_h, ld_dy, ld_b, ld_dx, rows;
+    const uint8_t *mask;
+    const char *gain;
+    const float *mean, *rstd;
+    float *part_g, *part_b;   // [workgroups][cols], or NULL
+    int cols;
+};
+
+constexpr u32x4 kZero4 = {0, 0, 0, 0};
+
+// The vector of n elements at p (n <= 0: zeros, nothing is read).
+template <bool BF16>
+__device__ __forceinline__ u32x4 take(const char *p, int n) {
+    if (n >= Vec<BF16>::kN) return ld128(p);
+    return n > 0 ? Vec<BF16>::load(p, n, kZero4) : kZero4;
+}
+
+// Sum over a row's team, the same in every thread, in a fixed order.  red: a slot for each wave, of this call alone until
+// the next but one barrier.
+template <int TPR>
+__device__ __forceinline__ float team_sum(float v, float *red) {
+#pragma unroll
+    for (int m = (TPR < 64 ? TPR : 64) / 2; m; m >>= 1) v += __shfl_xor(v, m);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = red[0];
+#pragma unroll
+        for (int w = 1; w < TPR / 64; ++w) v += red[w];
+    }
+    return v;
+}
+
+template <bool BF16, int TPR, int NV, bool CENTER>
+__global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
+    using V = Vec<BF16>;
+    constexpr int kTeams = TPR <= 64 ? 256 / TPR : 1, kEs = BF16 ? 2 : 4;
+    __shared__ float red[2][TPR > 64 ? TPR / 64 : 1];
+    const int lane = static_cast<int>(threadIdx.x) % TPR;
+    const int64_t row = (blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y) * kTeams + threadIdx.x / TPR;
+    if (row >= a.rows) return;   // (whole teams: one wave or less, or the whole workgroup)
+    const char *x = a.x + row * a.ld_x * kEs;
+    char *y = a.y + row * a.ld_y * kEs;
+    char *h_out = a.h ? a.h + row * a.ld_h * kEs : nullptr;
+    if (a.mask && a.mask[row] == 0) {   // nothing of it is read
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int i = k * TPR + lane, n = a.cols - i * V::kN;
+            if (n > 0) {
+                if (h_out) V::put(h_out + i * 16, kZero4, n);
+                V::put(y + i * 16, kZero4, n);
+            }
+        }
+        if (lane == 0) {
+            if (a.mean) a.mean[row] = 0.f;
+            if (a.rstd) a.rstd[row] = 0.f;
+        }
+        return;
+    }
+    u32x4 h[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) h[k] = take<BF16>(x + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN);
+    if (a.res) {
+        const char *r = a.res + row * a.ld_r * kEs;
+        u32x4 v[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) v[k] = take<BF16>(r + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float s[V::kN];
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) s[e] = V::get(h[k], e) + V::get(v[k], e);
+            h[k] = V::pack(s);   // the sum is rounded where it is stored, and the norm is that of the stored sum
+        }
+    }
+    const float per = 1.f / static_cast<float>(a.cols);
+    float mean = 0.f;
+    if constexpr (CENTER) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) s += V::get(h[k], e);
+        mean = team_sum<TPR>(s, red[0]) * per;
+    }
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int n = a.cols - (k * TPR + lane) * V::kN;
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) {
+            const float d = V::get(h[k], e) - mean;
+            q += e < n ? d * d : 0.f;
+        }
+    }
+    const float var = team_sum<TPR>(q, red[1]) * per;
+    const float rstd = 1.f / sqrtf(var + a.eps);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int i = k * TPR + lane, n = a.cols - i * V::kN;
+        if (n <= 0) continue;
+        const u32x4 g = a.gain ? take<BF16>(a.gain + i * 16, n) : kZero4;
+        const u32x4 b = a.bias ? take<BF16>(a.bias + i * 16, n) : kZero4;
+        float o[V::kN];
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) {
+            const float t = (V::get(h[k], e) - mean) * rstd;
+            o[e] = fmaf(t, a.gain ? V::get(g, e) : 1.f, V::get(b, e));
+        }
+        if (h_out) V::put(h_out + i * 16, h[k], n);
+        V::store(y + i * 16, o, n);
+    }
+    if (lane == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+}
+
+// A team's share of one row.
+template <int NV>
+struct RowPart {
+    u32x4 h[NV], dy[NV], base[NV];
+    float mean, rstd;
+    bool live;
+};
+
+template <bool BF16, int TPR, int NV, bool CENTER>
+__global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
+    using V = Vec<BF16>;
+    constexpr int kTh = TPR < 512 ? 512 : TPR, kTeams = kTh / TPR, kEs = BF16 ? 2 : 4, kW = TPR > 64 ? TPR / 64 : 1;
+    constexpr int kCols = TPR * NV * V::kN;
+    __shared__ float red[2][2][kTh / 64];          // by parity of the row, sum, wave
+    __shared__ float joined[kTeams > 1 ? kCols : 1];
+    const int lane = static_cast<int>(threadIdx.x) % TPR, team = static_cast<int>(threadIdx.x) / TPR;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kTeams;
+    const float per = 1.f / static_cast<float>(a.cols);
+    u32x4 gain[NV];
+    float dg[NV][V::kN] = {}, db[NV][V::kN] = {};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int i = k * TPR + lane;
+        gain[k] = a.gain ? take<BF16>(a.gain + i * 16, a.cols - i * V::kN) : kZero4;
+    }
+    const auto load = [&](int64_t row, RowPart<NV> &p) {
+        p.live = row < a.rows && (!a.mask || a.mask[row] != 0);
+        p.mean = CENTER && p.live ? a.mean[row] : 0.f;
+        p.rstd = p.live ? a.rstd[row] : 0.f;
+        const int width = p.live ? a.cols : 0, width_b = row < a.rows && a.base ? a.cols : 0;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int i = k * TPR + lane;
+            p.h[k] = take<BF16>(a.h + row * a.ld_h * kEs + i * 16, width - i * V::kN);
+            p.dy[k] = take<BF16>(a.dy + row * a.ld_dy * kEs + i * 16, width - i * V::kN);
+            p.base[k] = take<BF16>(a.base + row * a.ld_b * kEs + i * 16, width_b - i * V::kN);
+        }
+    };
+    const int64_t rounds = (a.rows + stride - 1) / stride;   // the same for the whole workgroup: there are barriers inside
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team;
+    RowPart<NV> cur, next;
+    load(row, cur);
+    for (int64_t it = 0; it < rounds; ++it, row += stride) {
+        if (it + 1 < rounds) load(row + stride, next);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) {
+                const float dy = V::get(cur.dy[k], e), c = a.gain ? dy * V::get(gain[k], e) : dy;
+                const float xh = (V::get(cur.h[k], e) - cur.mean) * cur.rstd;
+                if constexpr (CENTER) {
+                    s1 += c;
+                    db[k][e] += dy;
+                }
+                s2 = fmaf(c, xh, s2);
+                dg[k][e] = fmaf(dy, xh, dg[k][e]);
+            }
+#pragma unroll
+        for (int m = (TPR < 64 ? TPR : 64) / 2; m; m >>= 1) {
+            s2 += __shfl_xor(s2, m);
+            if constexpr (CENTER) s1 += __shfl_xor(s1, m);
+        }
+        if constexpr (TPR > 64) {
+            float(&r)[2][kTh / 64] = red[it & 1];   // the other half may still be read by a slower wave
+            if ((threadIdx.x & 63) == 0) {
+                r[0][threadIdx.x >> 6] = s1;
+                r[1][threadIdx.x >> 6] = s2;
+            }
+            __syncthreads();
+            s1 = 0.f;
+            s2 = 0.f;
+#pragma unroll
+            for (int w = 0; w < kW; ++w) {
+                if constexpr (CENTER) s1 += r[0][team * kW + w];
+                s2 += r[1][team * kW + w];
+            }
+        }
+        s1 *= per;
+        s2 *= per;
+        if (a.dx && row < a.rows) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int i = k * TPR + lane, n = a.cols - i * V::kN;
+                if (n <= 0) continue;
+                float o[V::kN];
+#pragma unroll
+                for (int e = 0; e < V::kN; ++e) {
+                    const float dy = V::get(cur.dy[k], e), c = a.gain ? dy * V::get(gain[k], e) : dy;
+                    const float xh = (V::get(cur.h[k], e) - cur.mean) * cur.rstd;
+                    const float t = cur.rstd * (c - s1 - xh * s2);
+                    o[e] = V::get(cur.base[k], e) + (cur.live ? t : 0.f);
+                }
+                V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
+            }
+        }
+        cur = next;
+    }
+    const auto write = [&](float (&sum)[NV][V::kN], float *part) {
+        if (!part) return;
+        if constexpr (kTeams > 1) {   // the teams' sums, added in order
+            for (int t = 0; t < kTeams; ++t) {
+                if (team == t)
+#pragma unroll
+                    for (int k = 0; k < NV; ++k)
+#pragma unroll
+                        for (int e = 0; e < V::kN; ++e) {
+                            float &j = joined[(k * TPR + lane) * V::kN + e];
+                            j = t == 0 ? sum[k][e] : j + sum[k][e];
+                        }
+                __syncthreads();
+            }
+            for (int c = static_cast<int>(threadIdx.x); c < a.cols; c += kTh)
+                part[static_cast<int64_t>(blockIdx.x) * a.cols + c] = joined[c];
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < V::kN; ++e) {
+                    const int c = (k * TPR + lane) * V::kN + e;
+                    if (c < a.cols) part[static_cast<int64_t>(blockIdx.x) * a.cols + c] = sum[k][e];
+                }
+        }
+    };
+    write(dg, a.part_g);
+    if constexpr (CENTER) write(db, a.part_b);
+}
+
+// dgain and dbias from the workgroups' sums: a workgroup takes 16 columns, its threads' 16 ranges of the parts are added
+// in order.  blockIdx.y: 0 dgain, 1 dbias.
+__global__ __launch_bounds__(256) void k_norm_parts(const float *part_g, const float *part_b, int parts, int cols,
+                                                    float *dgain, float *dbias, bool accumulate) {
+    __shared__ float sums[16][17];
+    const float *part = blockIdx.y ? part_b : part_g;
+    float *out = blockIdx.y ? dbias : dgain;
+    if (!out) return;
+    const int c = static_cast<int>(blockIdx.x) * 16 + (threadIdx.x & 15), slot = threadIdx.x >> 4;
+    float s = 0.f;
+    if (c < cols) {
+        const int each = (parts + 15) / 16, end = (slot + 1) * each < parts ? (slot + 1) * each : parts;
+        for (int i = slot * each; i < end; ++i) s += part[static_cast<int64_t>(i) * cols + c];
+    }
+    sums[slot][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (slot || c >= cols) return;
+    for (int i = 1; i < 16; ++i) s += sums[i][threadIdx.x];
+    out[c] = accumulate ? out[c] + s : s;
+}
+
+// The smallest team whose threads hold a row in at most `most` vectors each, from 32 threads on.
+int team_of(int vectors, int most) {
+    int t = 32;
+    while (t < 1024 && vectors > t * most) t *= 2;
+    return t;
+}
+
+template <int N>
+using int_c = std::integral_constant<int, N>;
+
+// go(team, vectors a thread), as compile-time constants, for a row of `vectors`
+template <class Go>
+void with_team(int team, int vectors, const Go &go) {
+    const int nv = (vectors + team - 1) / team;
+    const auto pick = [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        if (nv <= 1) go(t, int_c<1>{});
+        else if (nv <= 2) go(t, int_c<2>{});
+        else if (T < 1024 || nv <= 4) go(t, int_c<4>{});
+        else go(t, int_c<8>{});
+    };
+    switch (team) {
+        case 32: return pick(int_c<32>{});
+        case 64: return pick(int_c<64>{});
+        case 128: return pick(int_c<128>{});
+        case 256: return pick(int_c<256>{});
+        case 512: return pick(int_c<512>{});
+        default: return pick(int_c<1024>{});
+    }
+}
+
+int vectors_of(bool bf16, int cols) { return (cols + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4); }
+
+// Workgroups of the backward pass: two on each CU, as many as there are rows for.
+constexpr int kBwdGroups = 512;
+int bwd_groups(int team, int64_t rows) {
+    const int teams = team < 512 ? 512 / team : 1;
+    const int64_t g = (rows + teams - 1) / teams;
+    return static_cast<int>(g < kBwdGroups ? g : kBwdGroups);
+}
+
+}  // namespace
+
+size_t norm_ws_bytes(int64_t rows, int cols) {
+    // (a workgroup has at least one row)
+    const int64_t groups = rows < kBwdGroups ? rows : kBwdGroups;
+    return static_cast<size_t>(groups) * cols * 2 * sizeof(float);
+}
+
+hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
+    FwdArgs a = {static_cast<const char *>(n.x), static_cast<const char *>(n.residual), static_cast<char *>(n.h),
+                 static_cast<char *>(n.y), n.ld_x, n.ld_res, n.ld_h, n.ld_y, n.rows, n.mask,
+                 static_cast<const char *>(n.gain), static_cast<const char *>(n.bias), n.mean, n.rstd, n.cols, n.eps};
+    const int vec = vectors_of(n.bf16, n.cols);
+    const int team = team_of(vec, n.rows <= 1024 ? 1 : 4);
+    const auto go = [&](auto t, auto v) {
+        constexpr int T = decltype(t)::value, NV = decltype(v)::value;
+        const int teams = T <= 64 ? 256 / T : 1;
+        const int64_t groups = (n.rows + teams - 1) / teams;
+        const uint32_t gx = static_cast<uint32_t>(groups < (1 << 21) ? groups : (1 << 21));
+        const dim3 grid(gx, static_cast<uint32_t>((groups + gx - 1) / gx));
+        const int th = T <= 64 ? 256 : T;
+        if (n.bf16)
+            n.rms ? k_norm_fwd<true, T, NV, false><<<grid, th, 0, s>>>(a) : k_norm_fwd<true, T, NV, true><<<grid, th, 0, s>>>(a);
+        else
+            n.rms ? k_norm_fwd<false, T, NV, false><<<grid, th, 0, s>>>(a) : k_norm_fwd<false, T, NV, true><<<grid, th, 0, s>>>(a);
+    };
+    with_team(team, vec, go);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s) {
+    const int vec = vectors_of(n.bf16, n.cols);
+    const int team = team_of(vec, 2);
+    const int groups = bwd_groups(team, n.rows);   // (0 without rows: the gradients' sums are empty)
+    float *part_g = n.dgain ? static_cast<float *>(n.ws) : nullptr;
+    float *part_b = n.dbias ? static_cast<float *>(n.ws) + static_cast<int64_t>(groups) * n.cols : nullptr;
+    BwdArgs a = {static_cast<const char *>(n.h), static_cast<const char *>(n.dy), static_cast<const char *>(n.base),
+                 static_cast<char *>(n.dx), n.ld_h, n.ld_dy, n.ld_base, n.ld_dx, n.rows, n.mask,
+                 static_cast<const char *>(n.gain), n.mean, n.rstd, part_g, part_b, n.cols};
+    const auto go = [&](auto t, auto v) {
+        constexpr int T = decltype(t)::value, NV = decltype(v)::value;
+        constexpr int th = T < 512 ? 512 : T;
+        if (n.bf16)
+            n.rms ? k_norm_bwd<true, T, NV, false><<<groups, th, 0, s>>>(a) : k_norm_bwd<true, T, NV, true><<<groups, th, 0, s>>>(a);
+        else
+            n.rms ? k_norm_bwd<false, T, NV, false><<<groups, th, 0, s>>>(a) : k_norm_bwd<false, T, NV, true><<<groups, th, 0, s>>>(a);
+    };
+    if (n.rows > 0) with_team(team, vec, go);
+    if (n.dgain || n.dbias)
+        k_norm_parts<<<dim3(static_cast<uint32_t>(n.cols + 15) / 16, 2), 256, 0, s>>>(part_g, part_b, groups, n.cols, n.dgain,
+                                                                                      n.dbias, n.accumulate);
+    return hipGetLastError();
+}
+
+}  // namespace logra

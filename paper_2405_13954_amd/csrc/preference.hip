@@ -1,0 +1,239 @@
+// The loss of pairs of answers by their log ratios, and the gradient of every logit:
+//
+//   lp_s = sum over the tokens t of sequence s of (z_t[target_t] - lse(z_t))
+//   d    = beta ((lp_chosen - ref_chosen) - (lp_rejected - ref_rejected))
+//   loss = w ((1 - e) softplus(-d) + e softplus(d)),   slope = w beta (e - sigma(-d))
+//   dz_t = +-slope (onehot - softmax(z_t))             (+ chosen, - rejected)
+//
+// A token's gradient needs the sums of its whole pair, so the logits go by twice: k_pair_stats forms the maximum and the
+// sum of exponentials of ranges of each row, k_pair_sums joins them, adds up each sequence (in float64: the ratio is a
+// small difference of large sums) and leaves two factors for every row, and k_pair_grad writes the gradient.  The second
+// pass takes the rows from the last to the first, so that those that the 256 MB cache still holds are read from there.
+#include "internal.h"
+#include "vec16.h"
+
+namespace logra {
+namespace {
+
+constexpr int kMaxSplits = 16;   // ranges of a row that are summed by workgroups of their own
+constexpr int kTh = 256;
+
+struct Row {           // of one token; zeros: no gradient
+    float top, total;  // maximum and sum of exp(z - top); then the factors
+    float factor, hot; // dz = factor exp(z - top) + (hot at the target)
+};
+
+struct PairArgs {
+    const char *logits;
+    int64_t ld, rows;
+    const int64_t *target, *offsets;
+    float2 *part;   // [rows][splits]: maximum, sum
+    float *zt;      // [rows]: the target's logit
+    Row *row;       // [rows]
+    int vocab, splits, pairs;
+};
+
+// Whether the row counts: its target is a token, and it lies in the sequences.
+__device__ __forceinline__ bool counts(const PairArgs &a, int64_t row, int64_t t) {
+    return t >= 0 && t < a.vocab && row >= a.offsets[0] && row < a.offsets[2 * a.pairs];
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kTh) void k_pair_stats(PairArgs a) {
+    using V = Vec<BF16>;
+    constexpr int kEs = BF16 ? 2 : 4, kGroup = 4;
+    constexpr float kNone = -__builtin_inff();
+    __shared__ float red[kTh / 64];
+    const int64_t at = blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y;
+    const int64_t row = at / a.splits;
+    const int split = static_cast<int>(at - row * a.splits), tid = static_cast<int>(threadIdx.x);
+    if (row >= a.rows) return;
+    if (split == 0 && tid == 0) a.row[row] = {0.f, 0.f, 0.f, 0.f};   // no gradient, until k_pair_sums says more
+    const int64_t t = a.target[row];
+    if (!counts(a, row, t)) return;   // nothing of it is read
+    const char *z = a.logits + row * a.ld * kEs;
+    const int n_vec = (a.vocab + V::kN - 1) / V::kN, each = (n_vec + a.splits - 1) / a.splits;
+    const int begin = split * each, end = begin + each < n_vec ? begin + each : n_vec;
+    float top = kNone, total = 0.f;
+    for (int i = begin + tid; i < end; i += kGroup * kTh) {
+        u32x4 v[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            const int k = i + j * kTh, n = k < end ? a.vocab - k * V::kN : 0;
+            v[j] = n >= V::kN ? ld128(z + static_cast<int64_t>(k) * 16)
+                              : (n > 0 ? V::load(z + static_cast<int64_t>(k) * 16, n) : V::none());
+        }
+        float m = top;
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j)
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) m = fmaxf(m, V::get(v[j], e));
+        const float base = m == kNone ? 0.f : m;
+        total *= exp_from(top, base);
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            float q = 0.f;
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) q += exp_from(V::get(v[j], e), base);
+            total += q;
+        }
+        top = m;
+    }
+    const float mine = top;
+    top = group_reduce<kTh, true>(mine, red);
+    total = group_reduce<kTh, false>(total * exp_from(mine, top == kNone ? 0.f : top), red);
+    if (tid == 0) {
+        a.part[row * a.splits + split] = make_float2(top, total);
+        if (split == 0) {
+            float zt;
+            if constexpr (BF16)
+                zt = bf16_to_f32(reinterpret_cast<const bf16_bits *>(z)[t]);
+            else
+                zt = reinterpret_cast<const float *>(z)[t];
+            a.zt[row] = zt;
+        }
+    }
+}
+
+__device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+
+// One workgroup per pair.
+__global__ __launch_bounds__(kTh) void k_pair_sums(PairArgs a, const float *ref, const float *weight, double beta,
+                                                   double smoothing, float *loss, float *logp) {
+    constexpr float kNone = -__builtin_inff();
+    __shared__ double red[kTh / 64];
+    const int pair = static_cast<int>(blockIdx.x);
+    double sum[2];
+    int64_t cut[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {   // whatever the offsets hold, rows outside the logits are not touched
+        const int64_t o = a.offsets[2 * static_cast<int64_t>(pair) + i];
+        cut[i] = o < 0 ? 0 : o > a.rows ? a.rows : o;
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        double mine = 0.0;
+        for (int64_t row = cut[s] + threadIdx.x; row < cut[s + 1]; row += kTh) {
+            if (!counts(a, row, a.target[row])) continue;
+            const float2 *part = a.part + row * a.splits;
+            float top = kNone, total = 0.f;
+            for (int i = 0; i < a.splits; ++i) top = fmaxf(top, part[i].x);
+            const float base = top == kNone ? 0.f : top;
+            for (int i = 0; i < a.splits; ++i) total += part[i].y * exp_from(part[i].x, base);
+            a.row[row].top = base;
+            a.row[row].total = total;
+            // without a finite logit there is no distribution, and no token of it has a chance
+            mine += total == 0.f ? -__builtin_inf() : static_cast<double>(a.zt[row] - base) - log(static_cast<double>(total));
+        }
+#pragma unroll
+        for (int m = 32; m; m >>= 1) mine += __shfl_xor(mine, m);
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = mine;
+        __syncthreads();
+        sum[s] = ((red[0] + red[1]) + red[2]) + red[3];
+        __syncthreads();
+    }
+    const double ratio_c = sum[0] - (ref ? static_cast<double>(ref[2 * pair]) : 0.0);
+    const double ratio_r = sum[1] - (ref ? static_cast<double>(ref[2 * pair + 1]) : 0.0);
+    const double d = beta * (ratio_c - ratio_r);
+    const double w = weight ? static_cast<double>(weight[pair]) : 1.0;
+    const bool off = w == 0.0;   // a pair that does not count, whatever its logits hold
+    const double slope = off ? 0.0 : w * beta * (smoothing - 1.0 / (1.0 + exp(d)));
+    if (threadIdx.x == 0) {
+        logp[2 * pair] = static_cast<float>(sum[0]);
+        logp[2 * pair + 1] = static_cast<float>(sum[1]);
+        const double flipped = smoothing > 0.0 ? smoothing * softplus(d) : 0.0;
+        if (loss) loss[pair] = off ? 0.f : static_cast<float>(w * ((1.0 - smoothing) * softplus(-d) + flipped));
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const float hot = static_cast<float>(s ? -slope : slope);
+        for (int64_t row = cut[s] + threadIdx.x; row < cut[s + 1]; row += kTh) {
+            if (!counts(a, row, a.target[row])) continue;
+            const float total = a.row[row].total;
+            const bool none = total == 0.f || hot == 0.f;
+            a.row[row].factor = none ? 0.f : -hot / total;
+            a.row[row].hot = none ? 0.f : hot;
+        }
+    }
+}
+
+// A workgroup writes kGroup x kTh vectors of one row.
+template <bool BF16>
+__global__ __launch_bounds__(kTh) void k_pair_grad(PairArgs a, char *dlogits, int64_t ld_d, int pieces) {
+    using V = Vec<BF16>;
+    constexpr int kEs = BF16 ? 2 : 4, kGroup = 4;
+    const int64_t at = blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y, back = at / pieces;
+    if (back >= a.rows) return;
+    const int64_t row = a.rows - 1 - back;
+    const int first = static_cast<int>(at - back * pieces) * kGroup * kTh + static_cast<int>(threadIdx.x);
+    const char *z = a.logits + row * a.ld * kEs;
+    char *dz = dlogits + row * ld_d * kEs;
+    const Row r = a.row[row];
+    if (r.factor == 0.f && r.hot == 0.f) {
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            const int i = first + j * kTh, n = a.vocab - i * V::kN;
+            if (n > 0) V::put(dz + static_cast<int64_t>(i) * 16, u32x4{0, 0, 0, 0}, n);
+        }
+        return;
+    }
+    const int t = static_cast<int>(a.target[row]);
+    u32x4 v[kGroup];
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+        const int i = first + j * kTh, n = a.vocab - i * V::kN;
+        v[j] = n >= V::kN ? ld128_nt(z + static_cast<int64_t>(i) * 16)
+                          : (n > 0 ? V::load(z + static_cast<int64_t>(i) * 16, n) : V::none());
+    }
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+        const int i = first + j * kTh, n = a.vocab - i * V::kN;
+        if (n <= 0) continue;
+        float g[V::kN];
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) g[e] = exp_from(V::get(v[j], e), r.top) * r.factor;
+        const int hit = t - i * V::kN;
+        if (hit >= 0 && hit < V::kN) {
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) g[e] += e == hit ? r.hot : 0.f;
+        }
+        V::store(dz + static_cast<int64_t>(i) * 16, g, n);
+    }
+}
+
+dim3 grid_of(int64_t groups) {
+    const uint32_t gx = static_cast<uint32_t>(groups < (1 << 21) ? groups : (1 << 21));
+    return dim3(gx, static_cast<uint32_t>((groups + gx - 1) / gx));
+}
+
+}  // namespace
+
+size_t preference_ws_bytes(int64_t rows) {
+    return align256(rows * kMaxSplits * sizeof(float2)) + align256(rows * sizeof(float)) + align256(rows * sizeof(Row));
+}
+
+hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s) {
+    const int vec = (p.vocab + (p.bf16 ? 7 : 3)) / (p.bf16 ? 8 : 4);
+    int splits = (vec + 16 * kTh - 1) / (16 * kTh);
+    splits = splits < kMaxSplits ? splits : kMaxSplits;
+    char *ws = static_cast<char *>(p.ws);
+    PairArgs a = {static_cast<const char *>(p.logits), p.ld, p.rows, p.target, p.offsets, reinterpret_cast<float2 *>(ws),
+                  reinterpret_cast<float *>(ws + align256(p.rows * kMaxSplits * sizeof(float2))),
+                  reinterpret_cast<Row *>(ws + align256(p.rows * kMaxSplits * sizeof(float2)) + align256(p.rows * sizeof(float))),
+                  p.vocab, splits, p.pairs};
+    if (p.rows > 0) {
+        const dim3 grid = grid_of(p.rows * splits);
+        p.bf16 ? k_pair_stats<true><<<grid, kTh, 0, s>>>(a) : k_pair_stats<false><<<grid, kTh, 0, s>>>(a);
+    }
+    k_pair_sums<<<p.pairs, kTh, 0, s>>>(a, p.ref, p.weight, p.beta, p.smoothing, p.loss, p.logp);
+    if (p.dlogits && p.rows > 0) {
+        const int pieces = (vec + 4 * kTh - 1) / (4 * kTh);
+        const dim3 grid = grid_of(p.rows * pieces);
+        char *dz = static_cast<char *>(p.dlogits);
+        p.bf16 ? k_pair_grad<true><<<grid, kTh, 0, s>>>(a, dz, p.ld_d, pieces)
+               : k_pair_grad<false><<<grid, kTh, 0, s>>>(a, dz, p.ld_d, pieces);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace logra
