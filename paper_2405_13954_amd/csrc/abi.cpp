@@ -1272,7 +1272,7 @@ int logra_layer_norm_backward(const void *h, int64_t ld_h, const void *dy, int64
     TRY(check_norm_sizes(dtype, rows, cols));
     if (base && !dx) return fail(LOGRA_ERR_INVALID_ARG, "base without dx");
     if (rms && (dbias || mean)) return fail(LOGRA_ERR_INVALID_ARG, "a norm without the mean has no bias and no mean");
-    if (!dx && !dgain && !dbias) return ok();
+    if (!dgain && !dbias && (!dx || rows == 0)) return ok();
     const logra::NormBackward n = {h, dy, base, dx, ld_h, ld_dy, ld_base, ld_dx, rows, cols, dtype == LOGRA_BF16, rms != 0,
                                    accumulate != 0, mask, gain, mean, rstd, dgain, dbias, ws};
     TRY(norm_backward(n, dtype, ws_bytes));
