@@ -1113,7 +1113,7 @@ int64_t adamw_chunks(const logra_adamw_tensor *tensors, int n_tensors) {
         const logra_adamw_tensor &t = tensors[i];
         if (t.slice < 0 || t.slices < 0 || t.slice > INT32_MAX) return -1;
         chunks += (t.slice + logra::kAdamwChunk - 1) / logra::kAdamwChunk * t.slices;
-        if (chunks > INT32_MAX) return -1;
+        if (chunks > logra::kMaxAdamwChunks) return -1;
     }
     return chunks;
 }
@@ -1201,7 +1201,7 @@ int adamw_plan(const logra_adamw_tensor *tensors, int n_tensors, int n_groups, v
     auto *header = reinterpret_cast<logra::AdamwHeader *>(base);
     *header = {logra::kAdamwMagic, need, static_cast<uint32_t>(chunks), n_groups};
     auto *starts = reinterpret_cast<uint32_t *>(base + logra::adamw_starts_at(n_groups));
-    auto *out = reinterpret_cast<logra::AdamwChunk *>(base + logra::adamw_chunks_at(n_groups, static_cast<uint32_t>(chunks)));
+    auto *out = reinterpret_cast<logra::AdamwChunk *>(base + logra::adamw_chunks_at(n_groups));
     for (int i = 0; i < n_tensors; ++i) {
         const auto per = static_cast<uint32_t>((tensors[i].slice + logra::kAdamwChunk - 1) / logra::kAdamwChunk);
         for (int s = 0; s < tensors[i].slices; ++s) starts[tensors[i].first_group + s + 1] += per;

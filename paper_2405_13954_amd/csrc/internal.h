@@ -232,10 +232,11 @@ struct PreferenceLoss {
 size_t preference_ws_bytes(int64_t rows);
 hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s);
 
-// The AdamW plan: a header, a record for each group, each group's range of sums, the sums, and the chunks.
+// The AdamW plan: a header, a record for each group, each group's range of sums, the chunks, and the sums.
 constexpr int kAdamwChunk = 2048;   // elements of a chunk, all of one slice
 constexpr int kAdamwBlock = 256;    // elements that share a scale of the 8-bit states
 constexpr int kMaxAdamwGroups = 65536;
+constexpr uint32_t kMaxAdamwChunks = (1u << 24) - 1;   // one workgroup each, fewer than 2^32 threads
 constexpr uint64_t kAdamwMagic = 0x314e4c5057416461ull;
 struct AdamwHeader {
     uint64_t magic, bytes;
@@ -260,14 +261,15 @@ struct AdamwChunk {
 };
 __host__ __device__ inline size_t adamw_groups_at() { return 256; }
 __host__ __device__ inline size_t adamw_starts_at(int groups) { return adamw_groups_at() + align256(groups * sizeof(AdamwGroup)); }
-__host__ __device__ inline size_t adamw_parts_at(int groups) {
+__host__ __device__ inline size_t adamw_chunks_at(int groups) {
     return adamw_starts_at(groups) + align256((groups + size_t{1}) * sizeof(uint32_t));
 }
-__host__ __device__ inline size_t adamw_chunks_at(int groups, uint32_t chunks) {
-    return adamw_parts_at(groups) + align256(chunks * sizeof(double));
+__host__ __device__ inline size_t adamw_parts_at(int groups, uint32_t chunks) {
+    return adamw_chunks_at(groups) + align256(chunks * sizeof(AdamwChunk));
 }
 __host__ __device__ inline size_t adamw_plan_bytes(int groups, uint32_t chunks) {
-    return adamw_chunks_at(groups, chunks) + align256(chunks * sizeof(AdamwChunk));
+    chunks = chunks < 1 ? 1 : chunks;   // a step looks at the first without knowing that there is one
+    return adamw_parts_at(groups, chunks) + align256(chunks * sizeof(double));
 }
 struct AdamwHyper {
     double lr, beta1, beta2, eps, decay, max_norm;

@@ -39,6 +39,9 @@ struct BwdArgs {
     int cols;
 };
 
+// The workgroups' sums lie in rows of whole vectors.
+__host__ __device__ inline int padded(int cols) { return (cols + 3) & ~3; }
+
 constexpr u32x4 kZero4 = {0, 0, 0, 0};
 
 // The vector of n elements at p (n <= 0: zeros, nothing is read).
@@ -163,7 +166,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
     constexpr int kTh = TPR < 512 ? 512 : TPR, kTeams = kTh / TPR, kEs = BF16 ? 2 : 4, kW = TPR > 64 ? TPR / 64 : 1;
     constexpr int kCols = TPR * NV * V::kN;
     __shared__ float red[2][2][kTh / 64];          // by parity of the row, sum, wave
-    __shared__ float joined[kTeams > 1 ? kCols : 1];
+    __shared__ __attribute__((aligned(16))) float joined[kTeams > 1 ? kTeams * kCols : 4];
     const int lane = static_cast<int>(threadIdx.x) % TPR, team = static_cast<int>(threadIdx.x) / TPR;
     const int64_t stride = static_cast<int64_t>(gridDim.x) * kTeams;
     const float per = 1.f / static_cast<float>(a.cols);
@@ -249,20 +252,21 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
     }
     const auto write = [&](float (&sum)[NV][V::kN], float *part) {
         if (!part) return;
+        float *to = part + static_cast<int64_t>(blockIdx.x) * padded(a.cols);
         if constexpr (kTeams > 1) {   // the teams' sums, added in order
-            for (int t = 0; t < kTeams; ++t) {
-                if (team == t)
 #pragma unroll
-                    for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NV; ++k)
 #pragma unroll
-                        for (int e = 0; e < V::kN; ++e) {
-                            float &j = joined[(k * TPR + lane) * V::kN + e];
-                            j = t == 0 ? sum[k][e] : j + sum[k][e];
-                        }
-                __syncthreads();
+                for (int e = 0; e < V::kN; e += 4)
+                    *reinterpret_cast<f32x4 *>(joined + team * kCols + (k * TPR + lane) * V::kN + e) =
+                        f32x4{sum[k][e], sum[k][e + 1], sum[k][e + 2], sum[k][e + 3]};
+            __syncthreads();
+            for (int c = static_cast<int>(threadIdx.x); c < a.cols; c += kTh) {
+                float t = joined[c];
+#pragma unroll
+                for (int i = 1; i < kTeams; ++i) t += joined[i * kCols + c];
+                to[c] = t;
             }
-            for (int c = static_cast<int>(threadIdx.x); c < a.cols; c += kTh)
-                part[static_cast<int64_t>(blockIdx.x) * a.cols + c] = joined[c];
             __syncthreads();
         } else {
 #pragma unroll
@@ -270,7 +274,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
 #pragma unroll
                 for (int e = 0; e < V::kN; ++e) {
                     const int c = (k * TPR + lane) * V::kN + e;
-                    if (c < a.cols) part[static_cast<int64_t>(blockIdx.x) * a.cols + c] = sum[k][e];
+                    if (c < a.cols) to[c] = sum[k][e];
                 }
         }
     };
@@ -278,25 +282,38 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
     if constexpr (CENTER) write(db, a.part_b);
 }
 
-// dgain and dbias from the workgroups' sums: a workgroup takes 16 columns, its threads' 16 ranges of the parts are added
-// in order.  blockIdx.y: 0 dgain, 1 dbias.
+// dgain and dbias from the workgroups' sums: a workgroup takes 32 columns, eight threads of four for each of 32 ranges of
+// the parts; the ranges are added in order.  blockIdx.y: 0 dgain, 1 dbias.  512 parts of 4096 columns: PARTS us.
 __global__ __launch_bounds__(256) void k_norm_parts(const float *part_g, const float *part_b, int parts, int cols,
                                                     float *dgain, float *dbias, bool accumulate) {
-    __shared__ float sums[16][17];
+    constexpr int kSlots = 32, kAhead = 8;
+    __shared__ float sums[kSlots][33];
     const float *part = blockIdx.y ? part_b : part_g;
     float *out = blockIdx.y ? dbias : dgain;
     if (!out) return;
-    const int c = static_cast<int>(blockIdx.x) * 16 + (threadIdx.x & 15), slot = threadIdx.x >> 4;
-    float s = 0.f;
-    if (c < cols) {
-        const int each = (parts + 15) / 16, end = (slot + 1) * each < parts ? (slot + 1) * each : parts;
-        for (int i = slot * each; i < end; ++i) s += part[static_cast<int64_t>(i) * cols + c];
+    const int quad = threadIdx.x & 7, slot = threadIdx.x >> 3, ld = padded(cols);
+    const int c = static_cast<int>(blockIdx.x) * 32 + quad * 4;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (c < ld) {   // (the last vector of a row may hold unwritten columns, which are not stored)
+        const int each = (parts + kSlots - 1) / kSlots, begin = slot * each, end = begin + each < parts ? begin + each : parts;
+        for (int i = begin; i < end; i += kAhead) {
+            f32x4 v[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                v[j] = i + j < end ? *reinterpret_cast<const f32x4 *>(part + static_cast<int64_t>(i + j) * ld + c)
+                                   : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) s += v[j];
+        }
     }
-    sums[slot][threadIdx.x & 15] = s;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[slot][quad * 4 + e] = s[e];
     __syncthreads();
-    if (slot || c >= cols) return;
-    for (int i = 1; i < 16; ++i) s += sums[i][threadIdx.x];
-    out[c] = accumulate ? out[c] + s : s;
+    const int mine = static_cast<int>(blockIdx.x) * 32 + threadIdx.x;
+    if (threadIdx.x >= 32 || mine >= cols) return;
+    float t = 0.f;
+    for (int i = 0; i < kSlots; ++i) t += sums[i][threadIdx.x];
+    out[mine] = accumulate ? out[mine] + t : t;
 }
 
 // The smallest team whose threads hold a row in at most `most` vectors each, from 32 threads on.
@@ -345,7 +362,7 @@ int bwd_groups(int team, int64_t rows) {
 size_t norm_ws_bytes(int64_t rows, int cols) {
     // (a workgroup has at least one row)
     const int64_t groups = rows < kBwdGroups ? rows : kBwdGroups;
-    return static_cast<size_t>(groups) * cols * 2 * sizeof(float);
+    return static_cast<size_t>(groups) * padded(cols) * 2 * sizeof(float);
 }
 
 hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
@@ -375,7 +392,7 @@ hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s) {
     const int team = team_of(vec, 2);
     const int groups = bwd_groups(team, n.rows);   // (0 without rows: the gradients' sums are empty)
     float *part_g = n.dgain ? static_cast<float *>(n.ws) : nullptr;
-    float *part_b = n.dbias ? static_cast<float *>(n.ws) + static_cast<int64_t>(groups) * n.cols : nullptr;
+    float *part_b = n.dbias ? static_cast<float *>(n.ws) + static_cast<int64_t>(groups) * padded(n.cols) : nullptr;
     BwdArgs a = {static_cast<const char *>(n.h), static_cast<const char *>(n.dy), static_cast<const char *>(n.base),
                  static_cast<char *>(n.dx), n.ld_h, n.ld_dy, n.ld_base, n.ld_dx, n.rows, n.mask,
                  static_cast<const char *>(n.gain), n.mean, n.rstd, part_g, part_b, n.cols};
@@ -389,7 +406,7 @@ hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s) {
     };
     if (n.rows > 0) with_team(team, vec, go);
     if (n.dgain || n.dbias)
-        k_norm_parts<<<dim3(static_cast<uint32_t>(n.cols + 15) / 16, 2), 256, 0, s>>>(part_g, part_b, groups, n.cols, n.dgain,
+        k_norm_parts<<<dim3(static_cast<uint32_t>(n.cols + 31) / 32, n.dbias ? 2 : 1), 256, 0, s>>>(part_g, part_b, groups, n.cols, n.dgain,
                                                                                       n.dbias, n.accumulate);
     return hipGetLastError();
 }

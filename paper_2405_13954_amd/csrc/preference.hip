@@ -18,9 +18,14 @@ namespace {
 constexpr int kMaxSplits = 16;   // ranges of a row that are summed by workgroups of their own
 constexpr int kTh = 256;
 
-struct Row {           // of one token; zeros: no gradient
-    float top, total;  // maximum and sum of exp(z - top); then the factors
-    float factor, hot; // dz = factor exp(z - top) + (hot at the target)
+// Of one token: its maximum, the sum of exp(z - top) and then, in its place, the factor of the gradient
+// dz = factor exp(z - top) + (hot at the target).  Zeros: no gradient.
+struct Row {
+    float top;
+    union {
+        float total, factor;
+    };
+    float hot, unused;
 };
 
 struct PairArgs {
@@ -97,63 +102,90 @@ __global__ __launch_bounds__(kTh) void k_pair_stats(PairArgs a) {
 
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
 
-// One workgroup per pair.
-__global__ __launch_bounds__(kTh) void k_pair_sums(PairArgs a, const float *ref, const float *weight, double beta,
-                                                   double smoothing, float *loss, float *logp) {
+constexpr int kSumTh = 1024;
+
+// One workgroup per pair.  What a row needs is loaded at once, whether the row counts or not; what was found of a thread's
+// first row of each sequence stays in registers.
+__global__ __launch_bounds__(kSumTh) void k_pair_sums(PairArgs a, const float *ref, const float *weight, double beta,
+                                                      double smoothing, float *loss, float *logp) {
     constexpr float kNone = -__builtin_inff();
-    __shared__ double red[kTh / 64];
+    constexpr int kWaves = kSumTh / 64;
+    __shared__ double red[2][kWaves];
     const int pair = static_cast<int>(blockIdx.x);
-    double sum[2];
     int64_t cut[3];
+    const int64_t first = a.offsets[0], last = a.offsets[2 * static_cast<int64_t>(a.pairs)];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {   // whatever the offsets hold, rows outside the logits are not touched
         const int64_t o = a.offsets[2 * static_cast<int64_t>(pair) + i];
         cut[i] = o < 0 ? 0 : o > a.rows ? a.rows : o;
     }
+    const auto stats = [&](int64_t row, float &top, float &total) {   // returns the row's log probability
+        const int64_t t = a.target[row];
+        const float2 *part = a.part + row * a.splits;
+        const float zt = a.zt[row];
+        float2 p[kMaxSplits];
+#pragma unroll
+        for (int i = 0; i < kMaxSplits; ++i) p[i] = i < a.splits ? part[i] : make_float2(kNone, 0.f);
+        float m = kNone, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMaxSplits; ++i) m = fmaxf(m, p[i].x);
+        top = m == kNone ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < kMaxSplits; ++i) sum += p[i].y * exp_from(p[i].x, top);
+        if (t < 0 || t >= a.vocab || row < first || row >= last) {   // never written: whatever was loaded is dropped
+            total = 0.f;
+            return 0.0;
+        }
+        total = sum;
+        // without a finite logit there is no distribution, and no token of it has a chance
+        return sum == 0.f ? -__builtin_inf() : static_cast<double>(zt - top) - static_cast<double>(logf(sum));
+    };
+    float top[2] = {0.f, 0.f}, total[2] = {0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         double mine = 0.0;
-        for (int64_t row = cut[s] + threadIdx.x; row < cut[s + 1]; row += kTh) {
-            if (!counts(a, row, a.target[row])) continue;
-            const float2 *part = a.part + row * a.splits;
-            float top = kNone, total = 0.f;
-            for (int i = 0; i < a.splits; ++i) top = fmaxf(top, part[i].x);
-            const float base = top == kNone ? 0.f : top;
-            for (int i = 0; i < a.splits; ++i) total += part[i].y * exp_from(part[i].x, base);
-            a.row[row].top = base;
-            a.row[row].total = total;
-            // without a finite logit there is no distribution, and no token of it has a chance
-            mine += total == 0.f ? -__builtin_inf() : static_cast<double>(a.zt[row] - base) - log(static_cast<double>(total));
+        const int64_t at = cut[s] + threadIdx.x;
+        if (at < cut[s + 1]) mine = stats(at, top[s], total[s]);
+        for (int64_t row = at + kSumTh; row < cut[s + 1]; row += kSumTh) {
+            float m, q;
+            mine += stats(row, m, q);
+            a.row[row].top = m;
+            a.row[row].total = q;
         }
 #pragma unroll
         for (int m = 32; m; m >>= 1) mine += __shfl_xor(mine, m);
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = mine;
-        __syncthreads();
-        sum[s] = ((red[0] + red[1]) + red[2]) + red[3];
-        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[s][threadIdx.x >> 6] = mine;
     }
-    const double ratio_c = sum[0] - (ref ? static_cast<double>(ref[2 * pair]) : 0.0);
-    const double ratio_r = sum[1] - (ref ? static_cast<double>(ref[2 * pair + 1]) : 0.0);
+    __syncthreads();
+    double sum[2] = {0.0, 0.0};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        sum[0] += red[0][w];
+        sum[1] += red[1][w];
+    }
+    const double ratio_c = sum[0] - (ref ? static_cast<double>(ref[2 * static_cast<int64_t>(pair)]) : 0.0);
+    const double ratio_r = sum[1] - (ref ? static_cast<double>(ref[2 * static_cast<int64_t>(pair) + 1]) : 0.0);
     const double d = beta * (ratio_c - ratio_r);
     const double w = weight ? static_cast<double>(weight[pair]) : 1.0;
     const bool off = w == 0.0;   // a pair that does not count, whatever its logits hold
     const double slope = off ? 0.0 : w * beta * (smoothing - 1.0 / (1.0 + exp(d)));
     if (threadIdx.x == 0) {
-        logp[2 * pair] = static_cast<float>(sum[0]);
-        logp[2 * pair + 1] = static_cast<float>(sum[1]);
+        logp[2 * static_cast<int64_t>(pair)] = static_cast<float>(sum[0]);
+        logp[2 * static_cast<int64_t>(pair) + 1] = static_cast<float>(sum[1]);
         const double flipped = smoothing > 0.0 ? smoothing * softplus(d) : 0.0;
-        if (loss) loss[pair] = off ? 0.f : static_cast<float>(w * ((1.0 - smoothing) * softplus(-d) + flipped));
+        const double kept = smoothing < 1.0 ? (1.0 - smoothing) * softplus(-d) : 0.0;
+        if (loss) loss[pair] = off ? 0.f : static_cast<float>(w * (kept + flipped));
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const float hot = static_cast<float>(s ? -slope : slope);
-        for (int64_t row = cut[s] + threadIdx.x; row < cut[s + 1]; row += kTh) {
-            if (!counts(a, row, a.target[row])) continue;
-            const float total = a.row[row].total;
-            const bool none = total == 0.f || hot == 0.f;
-            a.row[row].factor = none ? 0.f : -hot / total;
-            a.row[row].hot = none ? 0.f : hot;
-        }
+        const auto factors = [&](int64_t row, float m, float q) {
+            const bool none = q == 0.f || hot == 0.f;
+            a.row[row] = {m, none ? 0.f : -hot / q, none ? 0.f : hot, 0.f};
+        };
+        const int64_t at = cut[s] + threadIdx.x;
+        if (at < cut[s + 1]) factors(at, top[s], total[s]);
+        for (int64_t row = at + kSumTh; row < cut[s + 1]; row += kSumTh) factors(row, a.row[row].top, a.row[row].total);
     }
 }
 
@@ -225,7 +257,7 @@ hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s) {
         const dim3 grid = grid_of(p.rows * splits);
         p.bf16 ? k_pair_stats<true><<<grid, kTh, 0, s>>>(a) : k_pair_stats<false><<<grid, kTh, 0, s>>>(a);
     }
-    k_pair_sums<<<p.pairs, kTh, 0, s>>>(a, p.ref, p.weight, p.beta, p.smoothing, p.loss, p.logp);
+    k_pair_sums<<<p.pairs, kSumTh, 0, s>>>(a, p.ref, p.weight, p.beta, p.smoothing, p.loss, p.logp);
     if (p.dlogits && p.rows > 0) {
         const int pieces = (vec + 4 * kTh - 1) / (4 * kTh);
         const dim3 grid = grid_of(p.rows * pieces);

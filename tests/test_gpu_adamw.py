@@ -278,7 +278,7 @@ def test_reruns_streams_graphs_and_one_seed():
 def test_memory_that_is_no_plan():
     import torch
     import paper_2405_13954_amd as P
-    model = Model(np.random.default_rng(11), [(2, 100, 0)], 32)
+    model = Model(np.random.default_rng(11), [(2, 5000, 0)], 32)
     plan = P.logra_adamw_plan(model.tensors, 2)
     before = model.values()
     step = torch.zeros(1, dtype=torch.int64, device="cuda")
