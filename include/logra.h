@@ -719,9 +719,9 @@ int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t row
  *                  words; element i takes word i % 4, its low half for m and its
  *                  high half for v.  What lies r / 65536 of the way to the next
  *                  value in magnitude goes there iff r > that half.  A v that is not
- *                  zero does not become zero: it takes the smallest code.  What is
- *                  not finite in fp32 becomes NaN (m) or infinity or NaN (v).  param
- *                  is computed from m and v before they are rounded
+ *                  zero does not become zero: it takes the smallest code.  Magnitudes
+ *                  from 2^128 on and NaN become NaN (m), or infinity and NaN (v).
+ *                  param is computed from m and v before they are rounded
  *   Elements need their own alignment only: tensors may be parts of flat buffers.
  *
  * logra_adamw_plan lays the list out in device memory, once for all steps; the

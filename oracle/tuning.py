@@ -110,7 +110,7 @@ def values_of(kind):
 
 def block_scale(x, kind):
     """The smallest 2^k, k >= -126, that brings the largest magnitude to the type's largest value or below."""
-    top = np.max(np.abs(x[np.isfinite(x) & (np.abs(x) <= np.finfo(np.float32).max)]), initial=0.0)
+    top = np.max(np.abs(x[np.abs(x) < 2.0 ** 128]), initial=0.0)
     if top == 0.0:
         return 1.0
     k = -126
@@ -124,7 +124,7 @@ def round_at_random(x, scale, kind, draw, never_zero):
     grid = values_of(kind)
     out = np.empty_like(x)
     for i, v in enumerate(x):
-        if not abs(v) <= np.finfo(np.float32).max:
+        if not abs(v) < 2.0 ** 128:
             out[i] = np.nan if kind is E4M3 or np.isnan(v) else np.inf
             continue
         a = abs(v) / scale

@@ -27,54 +27,70 @@ constexpr int kTh = 256, kPer = 8;             // elements of a thread
 static_assert(kAdamwChunk == kTh * kPer, "a workgroup takes one chunk");
 static_assert(kAdamwBlock == 32 * kPer, "a block of the 8-bit states is half a wave's");
 
-// Under-aligned vectors: tensors may be slices of flat buffers, so only the elements themselves are aligned.
+// Under-aligned vectors: tensors may be slices of flat buffers, so only the elements themselves are aligned.  The pointers
+// come out of the plan, so the compiler has to be told that they are global memory's.
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2b __attribute__((ext_vector_type(2), aligned(1)));
-
-__device__ __forceinline__ void load8(const float *p, int n, float (&x)[kPer]) {
-    if (n >= kPer) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const f32x4u v = *reinterpret_cast<const f32x4u *>(p + 4 * k);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * k + e] = v[e];
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] = e < n ? p[e] : 0.f;
+template <typename T>
+using global_ptr = __attribute__((address_space(1))) T *;
+template <typename T, typename P>
+__device__ __forceinline__ global_ptr<T> global(P *p) {
+    return (global_ptr<T>)(T *)p;
 }
 
-__device__ __forceinline__ void store8(float *p, int n, const float (&x)[kPer]) {
-    if (n >= kPer) {
+// What a launch does not write, through the scalar cache.
+template <typename T>
+__device__ __forceinline__ T constant(const T *p) {
+    struct Words {
+        uint32_t w[sizeof(T) / 4];
+    } words;
+    const auto *from = (const __attribute__((address_space(4))) uint32_t *)reinterpret_cast<const uint32_t *>(p);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<f32x4u *>(p + 4 * k) = f32x4u{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
-        return;
+    for (size_t i = 0; i < sizeof(T) / 4; ++i) words.w[i] = from[i];
+    return __builtin_bit_cast(T, words);
+}
+// Keeps a load in front of the branch that follows, so that both wait at once.
+template <typename T>
+__device__ __forceinline__ void loaded(T &x) {
+    asm volatile("" : "+s"(x));
+}
+
+// A thread's elements: kPer of them, or the first n.
+__device__ __forceinline__ void load_all(const float *p, int at, float (&x)[kPer]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const f32x4u v = *global<const f32x4u>(p + at + 4 * k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * k + e] = v[e];
     }
+}
+__device__ __forceinline__ void load_some(const float *p, int at, int n, float (&x)[kPer]) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) x[e] = e < n ? global<const float>(p)[at + e] : 0.f;
+}
+__device__ __forceinline__ void store_all(float *p, int at, const float (&x)[kPer]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        *global<f32x4u>(p + at + 4 * k) = f32x4u{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+}
+__device__ __forceinline__ void store_some(float *p, int at, int n, const float (&x)[kPer]) {
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
-        if (e < n) p[e] = x[e];
+        if (e < n) global<float>(p)[at + e] = x[e];
 }
-
-__device__ __forceinline__ u32x2b load8(const uint8_t *p, int n) {
-    if (n >= kPer) return *reinterpret_cast<const u32x2b *>(p);
+__device__ __forceinline__ u32x2b load_all(const uint8_t *p, int at) { return *global<const u32x2b>(p + at); }
+__device__ __forceinline__ u32x2b load_some(const uint8_t *p, int at, int n) {
     u32x2b v = {0, 0};
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
-        if (e < n) v[e >> 2] |= static_cast<uint32_t>(p[e]) << (8 * (e & 3));
+        if (e < n) v[e >> 2] |= static_cast<uint32_t>(global<const uint8_t>(p)[at + e]) << (8 * (e & 3));
     return v;
 }
-
-__device__ __forceinline__ void store8(uint8_t *p, int n, u32x2b v) {
-    if (n >= kPer) {
-        *reinterpret_cast<u32x2b *>(p) = v;
-        return;
-    }
+__device__ __forceinline__ void store_some(uint8_t *p, int at, int n, u32x2b v) {
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
-        if (e < n) p[e] = static_cast<uint8_t>(v[e >> 2] >> (8 * (e & 3)));
+        if (e < n) global<uint8_t>(p)[at + e] = static_cast<uint8_t>(v[e >> 2] >> (8 * (e & 3)));
 }
 
 // What the kernels find at fixed places of the plan's memory, whatever it holds; `room` chunks lie within it.
@@ -88,57 +104,63 @@ struct PlanArgs {
     const AdamwChunk *chunks;
 };
 
-__device__ __forceinline__ bool is_plan(const PlanArgs &a) {
-    const AdamwHeader *h = a.header;
-    return h->magic == kAdamwMagic && h->bytes <= a.bytes && h->groups == a.groups && h->chunks <= a.room;
+// (One load of the whole header: conditions that are looked at one after the other would wait for one load each.)
+__device__ __forceinline__ bool is_plan(const PlanArgs &a, const AdamwHeader &h) {
+    return (h.magic == kAdamwMagic) & (h.bytes <= a.bytes) & (h.groups == a.groups) & (h.chunks <= a.room);
 }
-__device__ __forceinline__ double *parts_of(const PlanArgs &a) {
-    return reinterpret_cast<double *>(reinterpret_cast<char *>(a.header) + adamw_parts_at(a.groups, a.header->chunks));
+__device__ __forceinline__ double *parts_of(const PlanArgs &a, const AdamwHeader &h) {
+    return reinterpret_cast<double *>(reinterpret_cast<char *>(a.header) + adamw_parts_at(a.groups, h.chunks));
 }
 
 // A wave for each chunk: the sum of its squared gradients in float64, at the chunk's place among its group's.
 __global__ __launch_bounds__(kTh) void k_adamw_norm(PlanArgs a) {
+    constexpr int kVec = kAdamwChunk / 64 / 4;
     const int lane = static_cast<int>(threadIdx.x & 63);
     const uint32_t c = blockIdx.x * (kTh / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (c >= a.room) return;
-    const float *grad = a.chunks[c].grad;   // loaded beside the header; used if this is a plan
-    const int count = a.chunks[c].count;
-    const uint32_t slot = a.chunks[c].slot;
-    if (!is_plan(a) || c >= a.header->chunks) return;
-    float g[kAdamwChunk / 64 / 4][4];
+    const AdamwHeader h = constant(a.header);
+    AdamwChunk k = constant(a.chunks + c);   // loaded beside the header; used if this is a plan
+    loaded(k.grad);
+    loaded(k.count);
+    loaded(k.slot);
+    const float *grad = k.grad;
+    const int count = k.count;
+    if (!is_plan(a, h) || c >= h.chunks) return;
+    f32x4 g[kVec];
+    if (count == kAdamwChunk) {
 #pragma unroll
-    for (int i = 0; i < kAdamwChunk / 64 / 4; ++i) {
-        const int at = (i * 64 + lane) * 4, n = count - at;
-        if (n >= 4) {
-            const f32x4u v = *reinterpret_cast<const f32x4u *>(grad + at);
+        for (int i = 0; i < kVec; ++i) g[i] = *global<const f32x4u>(grad + (i * 64 + lane) * 4);
+    } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) g[i][e] = v[e];
-        } else {
+        for (int i = 0; i < kVec; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) g[i][e] = e < n ? grad[at + e] : 0.f;
-        }
+            for (int e = 0; e < 4; ++e) {
+                const int at = (i * 64 + lane) * 4 + e;
+                g[i][e] = at < count ? global<const float>(grad)[at] : 0.f;
+            }
     }
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < kAdamwChunk / 64 / 4; ++i)
+    for (int i = 0; i < kVec; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s = fma(static_cast<double>(g[i][e]), static_cast<double>(g[i][e]), s);
 #pragma unroll
     for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m);
-    if (lane == 0) parts_of(a)[slot] = s;
+    if (lane == 0) parts_of(a, h)[k.slot] = s;
 }
 
 // A workgroup for each group: its norm, and what its elements are multiplied by.
 __global__ __launch_bounds__(kTh) void k_adamw_head(PlanArgs a, const int64_t *step, AdamwHyper y, bool with_norm,
                                                     const float *lr_scale, float *norms) {
-    if (!is_plan(a)) return;
+    const AdamwHeader h = constant(a.header);
+    if (!is_plan(a, h)) return;
     __shared__ double red[kTh / 64];
     const int group = static_cast<int>(blockIdx.x);
     double clip = 1.0;
     bool skip = false;
     if (with_norm) {
         const uint32_t begin = a.starts[group], end = a.starts[group + 1];
-        const double *parts = parts_of(a);
+        const double *parts = parts_of(a, h);
         double s = 0.0;
         for (uint32_t i = begin + threadIdx.x; i < end; i += kTh) s += parts[i];
 #pragma unroll
@@ -172,16 +194,16 @@ __device__ __forceinline__ float moved(float p, float m, float v, const AdamwGro
     return fmaf(p, keep, -g.rate * m * __builtin_amdgcn_rcpf(fmaf(root, g.root, eps)));
 }
 
-constexpr double kFloatMax = 3.4028234663852886e38;
-
-// |x| as an ordered key: the high word of the double, its last bit set where the low word holds anything, so that 1.75 times
-// a power of two and what is above it differ.
-__device__ __forceinline__ uint32_t key_of(double x) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    return (static_cast<uint32_t>(u >> 32) & 0x7FFFFFFFu) | (static_cast<uint32_t>(u) != 0 ? 1u : 0u);
+// The states' codes are made from the high and low words of m and v in float64.  kHuge: the high word of 2^128, from which on
+// (and for infinities and NaN) a magnitude is not finite in fp32.
+constexpr uint32_t kHuge = 0x47F00000u;
+__device__ __forceinline__ uint32_t low_of(double x) { return static_cast<uint32_t>(__builtin_bit_cast(uint64_t, x)); }
+__device__ __forceinline__ uint32_t high_of(double x) {   // of |x|
+    return static_cast<uint32_t>(__builtin_bit_cast(uint64_t, x) >> 32) & 0x7FFFFFFFu;
 }
 
-// The exponent of the block's scale, from the largest key: the scale brings it to 1.75 * 2^HIGH or below.
+// The exponent of a block's scale, from the high word of its largest magnitude (its last bit set where the low word holds
+// anything): the scale brings it to 1.75 * 2^HIGH or below.
 template <int HIGH>
 __device__ __forceinline__ int scale_of(uint32_t key) {
     if (key < 0x00100000u) return 0;   // only zeros (a double that fp32 numbers give is not subnormal)
@@ -189,23 +211,33 @@ __device__ __forceinline__ int scale_of(uint32_t key) {
     return k < -126 ? -126 : k;
 }
 
-// |x| 2^-k in steps of a float of BITS mantissa bits and exponents from LOW on, rounded up where the part cut off exceeds
-// draw / 65536 of a step; as its code.  LEAST: the smallest code of what is not zero.  The leading 21 bits of x, one more
-// where there are others, give the number of 65536ths of a step, rounded up.
+// An 8-bit type: BITS of mantissa, exponents from LOW on.  LEAST: the smallest code of what is not zero.
 template <int BITS, int LOW, uint32_t LEAST>
-__device__ __forceinline__ uint32_t code_of(double x, int k, uint32_t draw) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t high = static_cast<uint32_t>(u >> 32) & 0x7FFFFFFFu;
-    const int e = static_cast<int>(high >> 20) - 1023 - k, under = LOW - e;   // under > 0: below the smallest exponent
-    int drop = 4 - BITS + (under > 0 ? under : 0);
-    drop = drop < 31 ? drop : 31;
-    const uint32_t lead = ((high & 0xFFFFFu) | 0x100000u) + (static_cast<uint32_t>(u) != 0 ? 1u : 0u);
-    const uint32_t fixed = (lead + ((1u << drop) - 1u)) >> drop;
-    uint32_t n = (fixed + 65535u - draw) >> 16;
-    if (LEAST) n = n < LEAST ? LEAST : n;
-    n += static_cast<uint32_t>(under > 0 ? 0 : -under) << BITS;
-    return high < 0x00100000u ? 0u : n;
-}
+struct Code {
+    static constexpr int kCut = 4 - BITS;   // bits of the high word below 1 / 65536 of a step
+
+    // The high word of the smallest normal number at the scale 2^k.
+    static __device__ __forceinline__ uint32_t normal(int k) { return static_cast<uint32_t>(1023 + LOW + k) << 20; }
+
+    // |x| 2^-k, not below the smallest normal number: x's own bits, rounded up where the part cut off exceeds draw / 65536 of
+    // a step.  65535 - draw of these, and one less than a unit of what lies below them, carry exactly then.
+    static __device__ __forceinline__ uint32_t of_normal(double x, int k, uint32_t draw) {
+        const uint32_t lead = high_of(x) - (normal(k) - 0x100000u) + (low_of(x) != 0 ? 1u : 0u);
+        return (lead + ((65535u - draw) << kCut) + ((1u << kCut) - 1u)) >> (16 + kCut);
+    }
+
+    // The same for any magnitude that is finite in fp32.
+    static __device__ __forceinline__ uint32_t of(double x, int k, uint32_t draw) {
+        const uint32_t high = high_of(x);
+        if (high >= normal(k)) return of_normal(x, k, draw);
+        if (high < 0x00100000u) return 0u;
+        int drop = kCut + LOW + k + 1023 - static_cast<int>(high >> 20);
+        drop = drop < 31 ? drop : 31;
+        const uint32_t lead = ((high & 0xFFFFFu) | 0x100000u) + (low_of(x) != 0 ? 1u : 0u);
+        const uint32_t fixed = (lead + ((1u << drop) - 1u)) >> drop, n = (fixed + 65535u - draw) >> 16;
+        return n < LEAST ? LEAST : n;
+    }
+};
 
 __device__ __forceinline__ uint32_t half_wave_max(uint32_t v) {
 #pragma unroll
@@ -216,36 +248,67 @@ __device__ __forceinline__ uint32_t half_wave_max(uint32_t v) {
     return v;
 }
 
-// The largest key of a block's elements that are finite in fp32.
+// The key of a block's largest magnitude that is finite in fp32, from its threads' n elements each.
 __device__ __forceinline__ uint32_t top_key(const double (&x)[kPer], int n) {
-    double top = 0.0;
+    uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) top = fmax(top, e < n ? fabs(x[e]) : 0.0);   // (the maximum of a NaN and a number is the number)
-    if (__builtin_expect(top > kFloatMax, 0)) {
-        top = 0.0;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) top = fmax(top, e < n && fabs(x[e]) <= kFloatMax ? fabs(x[e]) : 0.0);
+    for (int e = 0; e < kPer; ++e) {
+        const uint32_t h = high_of(x[e]), key = e < n && h < kHuge ? h | (low_of(x[e]) != 0 ? 1u : 0u) : 0u;
+        top = key > top ? key : top;
     }
-    return half_wave_max(key_of(top));
+    return half_wave_max(top);
+}
+
+// The codes of a thread's elements; plain: every one is a normal number of its type.
+template <bool PLAIN>
+__device__ __forceinline__ void codes_of(const double (&m)[kPer], const double (&v)[kPer], int scale_m, int scale_v,
+                                         const u32x4 (&bits)[2], u32x2b &out_m, u32x2b &out_v) {
+    using M = Code<3, -6, 0>;    // e4m3
+    using S = Code<2, -14, 1>;   // e5m2
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const uint32_t w = bits[e >> 2][e & 3];
+        uint32_t one = PLAIN ? M::of_normal(m[e], scale_m, w & 0xFFFFu) : M::of(m[e], scale_m, w & 0xFFFFu);
+        uint32_t two = PLAIN ? S::of_normal(v[e], scale_v, w >> 16) : S::of(v[e], scale_v, w >> 16);
+        one |= static_cast<uint32_t>(__builtin_bit_cast(uint64_t, m[e]) >> 56) & 0x80u;
+        if (!PLAIN) {
+            one = high_of(m[e]) < kHuge ? one : 0x7Fu;                          // NaN (the type has no infinity)
+            two = high_of(v[e]) < kHuge ? two : v[e] > 0.0 ? 0x7Cu : 0x7Fu;     // infinity, NaN
+        }
+        out_m[e >> 2] |= one << (8 * (e & 3));
+        out_v[e >> 2] |= two << (8 * (e & 3));
+    }
 }
 
 __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, int64_t *step, AdamwHyper y) {
-    const AdamwChunk k = a.chunks[blockIdx.x];   // loaded beside the header; used if this is a plan
-    if (!is_plan(a)) return;
+    const AdamwHeader h = constant(a.header);
+    AdamwChunk k = constant(a.chunks + blockIdx.x);   // loaded beside the header; used if this is a plan
+    loaded(k.grad);
+    loaded(k.m_scale);
+    loaded(k.count);
+    if (!is_plan(a, h)) return;
     // k_adamw_head has read the step, and no workgroup of this launch does
     if (blockIdx.x == 0 && threadIdx.x == 0) *step = a.group->step;
-    if (blockIdx.x >= a.header->chunks) return;
+    if (blockIdx.x >= h.chunks) return;
     const int at = static_cast<int>(threadIdx.x) * kPer, n = k.count - at;
-    float p[kPer], g[kPer];
-    load8(k.grad + at, n, g);
-    load8(k.param + at, n, p);
-    const AdamwGroup o = a.group[k.group];
+    const AdamwGroup o = constant(a.group + k.group);
     const float keep = k.decay ? static_cast<float>(1.0 - static_cast<double>(o.lr) * y.decay) : 1.f;
     const float eps = static_cast<float>(y.eps);
+    float p[kPer], g[kPer];
     if (!k.m_scale) {
         float m[kPer], v[kPer];
-        load8(static_cast<const float *>(k.m) + at, n, m);
-        load8(static_cast<const float *>(k.v) + at, n, v);
+        float *pm = static_cast<float *>(k.m), *pv = static_cast<float *>(k.v);
+        if (n >= kPer) {
+            load_all(k.grad, at, g);
+            load_all(k.param, at, p);
+            load_all(pm, at, m);
+            load_all(pv, at, v);
+        } else {
+            load_some(k.grad, at, n, g);
+            load_some(k.param, at, n, p);
+            load_some(pm, at, n, m);
+            load_some(pv, at, n, v);
+        }
         if (o.skip) return;   // a model whose gradient is not finite stays as it is
         const float clip = static_cast<float>(o.clip), b1 = static_cast<float>(y.beta1), b2 = static_cast<float>(y.beta2);
         const float a1 = static_cast<float>(1.0 - y.beta1), a2 = static_cast<float>(1.0 - y.beta2);
@@ -256,14 +319,36 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, int64_t *step, A
             v[e] = fmaf(a2, cg * cg, b2 * v[e]);
             p[e] = moved(p[e], m[e], v[e], o, keep, eps);
         }
-        store8(static_cast<float *>(k.m) + at, n, m);
-        store8(static_cast<float *>(k.v) + at, n, v);
+        if (n >= kPer) {
+            store_all(pm, at, m);
+            store_all(pv, at, v);
+        } else {
+            store_some(pm, at, n, m);
+            store_some(pv, at, n, v);
+        }
     } else {
         const int block = at / kAdamwBlock;   // half a wave has it
         const uint32_t i = k.first + static_cast<uint32_t>(at);
-        const u32x2b cm = load8(static_cast<const uint8_t *>(k.m) + at, n);
-        const u32x2b cv = load8(static_cast<const uint8_t *>(k.v) + at, n);
-        const float sm = n > 0 ? k.m_scale[block] : 0.f, sv = n > 0 ? k.v_scale[block] : 0.f;
+        uint8_t *pm = static_cast<uint8_t *>(k.m), *pv = static_cast<uint8_t *>(k.v);
+        u32x2b cm, cv;
+        float sm = 0.f, sv = 0.f;
+        if (n >= kPer) {
+            load_all(k.grad, at, g);
+            load_all(k.param, at, p);
+            cm = load_all(pm, at);
+            cv = load_all(pv, at);
+            sm = global<const float>(k.m_scale)[block];
+            sv = global<const float>(k.v_scale)[block];
+        } else {
+            load_some(k.grad, at, n, g);
+            load_some(k.param, at, n, p);
+            cm = load_some(pm, at, n);
+            cv = load_some(pv, at, n);
+            if (n > 0) {
+                sm = global<const float>(k.m_scale)[block];
+                sv = global<const float>(k.v_scale)[block];
+            }
+        }
         if (o.skip) return;
         const double b1 = y.beta1 * sm, b2 = y.beta2 * sv, a1 = (1.0 - y.beta1) * o.clip, a2 = (1.0 - y.beta2) * (o.clip * o.clip);
         double m[kPer], v[kPer];
@@ -283,41 +368,58 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, int64_t *step, A
             v[e] = fma(a2, ge * ge, b2 * static_cast<double>(fv));
             p[e] = moved(p[e], static_cast<float>(m[e]), static_cast<float>(v[e]), o, keep, eps);
         }
-        const int scale_m = scale_of<8>(top_key(m, n)), scale_v = scale_of<15>(top_key(v, n));
-        u32x2b out_m = {0, 0}, out_v = {0, 0};
+        // The largest and smallest magnitudes by their high words alone, which is all but always enough.  (Elements past
+        // the tensor's end are zeros, unless a scale was not finite.)
+        uint32_t top_m = 0, top_v = 0, low_m = ~0u, low_v = ~0u;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const u32x4 bits = philox(i / 4 + q, k.slice, k.tensor, static_cast<uint32_t>(o.step), y.key[0], y.key[1]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const double me = m[4 * q + e], ve = v[4 * q + e];
-                uint32_t one = code_of<3, -6, 0>(me, scale_m, bits[e] & 0xFFFFu);
-                one |= static_cast<uint32_t>(__builtin_bit_cast(uint64_t, me) >> 56) & 0x80u;
-                uint32_t two = code_of<2, -14, 1>(ve, scale_v, bits[e] >> 16);
-                one = fabs(me) <= kFloatMax ? one : 0x7Fu;                            // NaN (the type has no infinity)
-                two = ve <= kFloatMax ? two : ve > 0.0 ? 0x7Cu : 0x7Fu;   // infinity, NaN
-                out_m[q] |= one << (8 * e);
-                out_v[q] |= two << (8 * e);
-            }
+        for (int e = 0; e < kPer; ++e) {
+            const uint32_t hm = high_of(m[e]), hv = high_of(v[e]);
+            top_m = hm > top_m ? hm : top_m;
+            top_v = hv > top_v ? hv : top_v;
+            low_m = hm < low_m ? hm : low_m;
+            low_v = hv < low_v ? hv : low_v;
         }
-        store8(static_cast<uint8_t *>(k.m) + at, n, out_m);
-        store8(static_cast<uint8_t *>(k.v) + at, n, out_v);
+        top_m = half_wave_max(top_m);
+        top_v = half_wave_max(top_v);
+        const auto unsure = [](uint32_t top) {   // not finite, or next to 1.75 times a power of two
+             return top >= kHuge || (top & 0xFFFFFu) == 0xC0000u; };
+        const bool sure = !unsure(top_m) && !unsure(top_v);
+        if (__builtin_amdgcn_ballot_w64(!sure)) {
+            top_m = top_key(m, n);
+            top_v = top_key(v, n);
+        }
+        const int scale_m = scale_of<8>(top_m), scale_v = scale_of<15>(top_v);
+        const bool plain = sure && low_m >= Code<3, -6, 0>::normal(scale_m) && low_v >= Code<2, -14, 1>::normal(scale_v);
+        const uint32_t t = static_cast<uint32_t>(o.step);
+        const u32x4 bits[2] = {philox(i / 4, k.slice, k.tensor, t, y.key[0], y.key[1]),
+                               philox(i / 4 + 1, k.slice, k.tensor, t, y.key[0], y.key[1])};
+        u32x2b out_m = {0, 0}, out_v = {0, 0};
+        if (__builtin_amdgcn_ballot_w64(!plain) == 0)
+            codes_of<true>(m, v, scale_m, scale_v, bits, out_m, out_v);
+        else
+            codes_of<false>(m, v, scale_m, scale_v, bits, out_m, out_v);
+        if (n >= kPer) {
+            *global<u32x2b>(pm + at) = out_m;
+            *global<u32x2b>(pv + at) = out_v;
+        } else {
+            store_some(pm, at, n, out_m);
+            store_some(pv, at, n, out_v);
+        }
         if (n > 0 && (threadIdx.x & 31) == 0) {
-            k.m_scale[block] = __uint_as_float(static_cast<uint32_t>(scale_m + 127) << 23);
-            k.v_scale[block] = __uint_as_float(static_cast<uint32_t>(scale_v + 127) << 23);
+            global<float>(k.m_scale)[block] = __uint_as_float(static_cast<uint32_t>(scale_m + 127) << 23);
+            global<float>(k.v_scale)[block] = __uint_as_float(static_cast<uint32_t>(scale_v + 127) << 23);
         }
     }
-    store8(k.param + at, n, p);
-    if (k.work) {
-        bf16_bits *work = static_cast<bf16_bits *>(k.work) + at;
-        const u32x4 v = Vec<true>::pack(p);
-        if (n >= kPer) {
-            *reinterpret_cast<u32x4h *>(work) = v;
-        } else {
+    const u32x4 w = Vec<true>::pack(p);
+    bf16_bits *work = static_cast<bf16_bits *>(k.work);
+    if (n >= kPer) {
+        store_all(k.param, at, p);
+        if (work) *global<u32x4h>(work + at) = w;
+    } else {
+        store_some(k.param, at, n, p);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (e < n) work[e] = static_cast<bf16_bits>(v[e >> 1] >> (16 * (e & 1)));
-        }
+        for (int e = 0; e < kPer; ++e)
+            if (work && e < n) global<bf16_bits>(work)[at + e] = static_cast<bf16_bits>(w[e >> 1] >> (16 * (e & 1)));
     }
 }
 
