@@ -334,6 +334,7 @@ void with_team(int team, int vectors, const Go &go) {
         constexpr int T = decltype(t)::value;
         if (nv <= 1) go(t, int_c<1>{});
         else if (nv <= 2) go(t, int_c<2>{});
+        else if (nv <= 3) go(t, int_c<3>{});
         else if (T < 1024 || nv <= 4) go(t, int_c<4>{});
         else go(t, int_c<8>{});
     };
@@ -389,7 +390,7 @@ hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
 
 hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s) {
     const int vec = vectors_of(n.bf16, n.cols);
-    const int team = team_of(vec, 2);
+    const int team = team_of(vec, 3);
     const int groups = bwd_groups(team, n.rows);   // (0 without rows: the gradients' sums are empty)
     float *part_g = n.dgain ? static_cast<float *>(n.ws) : nullptr;
     float *part_b = n.dbias ? static_cast<float *>(n.ws) + static_cast<int64_t>(groups) * padded(n.cols) : nullptr;

@@ -40,7 +40,8 @@ struct PairArgs {
 
 // Whether the row counts: its target is a token, and it lies in the sequences.
 __device__ __forceinline__ bool counts(const PairArgs &a, int64_t row, int64_t t) {
-    return t >= 0 && t < a.vocab && row >= a.offsets[0] && row < a.offsets[2 * a.pairs];
+    const int64_t first = a.offsets[0], last = a.offsets[2 * static_cast<int64_t>(a.pairs)];
+    return (t >= 0) & (t < a.vocab) & (row >= first) & (row < last);   // (the loads wait together)
 }
 
 template <bool BF16>
@@ -57,17 +58,10 @@ __global__ __launch_bounds__(kTh) void k_pair_stats(PairArgs a) {
     const int64_t t = a.target[row];
     if (!counts(a, row, t)) return;   // nothing of it is read
     const char *z = a.logits + row * a.ld * kEs;
-    const int n_vec = (a.vocab + V::kN - 1) / V::kN, each = (n_vec + a.splits - 1) / a.splits;
-    const int begin = split * each, end = begin + each < n_vec ? begin + each : n_vec;
+    const int n_full = a.vocab / V::kN, odd = a.vocab - n_full * V::kN;   // whole vectors; logits of the last, partial one
+    const int each = (n_full + a.splits - 1) / a.splits, begin = split * each, end = begin + each < n_full ? begin + each : n_full;
     float top = kNone, total = 0.f;
-    for (int i = begin + tid; i < end; i += kGroup * kTh) {
-        u32x4 v[kGroup];
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
-            const int k = i + j * kTh, n = k < end ? a.vocab - k * V::kN : 0;
-            v[j] = n >= V::kN ? ld128(z + static_cast<int64_t>(k) * 16)
-                              : (n > 0 ? V::load(z + static_cast<int64_t>(k) * 16, n) : V::none());
-        }
+    const auto take = [&](const u32x4 (&v)[kGroup]) {
         float m = top;
 #pragma unroll
         for (int j = 0; j < kGroup; ++j)
@@ -83,6 +77,22 @@ __global__ __launch_bounds__(kTh) void k_pair_stats(PairArgs a) {
             total += q;
         }
         top = m;
+    };
+    int i = begin + tid;
+    for (; i + (kGroup - 1) * kTh < end; i += kGroup * kTh) {
+        u32x4 v[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) v[j] = ld128(z + static_cast<int64_t>(i + j * kTh) * 16);
+        take(v);
+    }
+    const bool tail = odd > 0 && split == a.splits - 1 && tid == kTh - 1;   // the thread that has the partial vector
+    if (i < end || tail) {   // (i + 3 kTh is past the end: at most three vectors are left)
+        u32x4 v[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup - 1; ++j) v[j] = i + j * kTh < end ? ld128(z + static_cast<int64_t>(i + j * kTh) * 16) : V::none();
+        v[kGroup - 1] = V::none();
+        if (tail) v[kGroup - 1] = V::load(z + static_cast<int64_t>(n_full) * 16, odd);
+        take(v);
     }
     const float mine = top;
     top = group_reduce<kTh, true>(mine, red);
@@ -210,7 +220,25 @@ __global__ __launch_bounds__(kTh) void k_pair_grad(PairArgs a, char *dlogits, in
         return;
     }
     const int t = static_cast<int>(a.target[row]);
+    const auto gradient = [&](u32x4 v, int i, int n) {
+        float g[V::kN];
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) g[e] = exp_from(V::get(v, e), r.top) * r.factor;
+        const int hit = t - i * V::kN;
+        if (hit >= 0 && hit < V::kN) {
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) g[e] += e == hit ? r.hot : 0.f;
+        }
+        V::store(dz + static_cast<int64_t>(i) * 16, g, n);
+    };
     u32x4 v[kGroup];
+    if ((first - static_cast<int>(threadIdx.x) + kGroup * kTh) * V::kN <= a.vocab) {   // the whole workgroup's vectors are whole
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) v[j] = ld128_nt(z + static_cast<int64_t>(first + j * kTh) * 16);
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) gradient(v[j], first + j * kTh, V::kN);
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < kGroup; ++j) {
         const int i = first + j * kTh, n = a.vocab - i * V::kN;
@@ -220,16 +248,7 @@ __global__ __launch_bounds__(kTh) void k_pair_grad(PairArgs a, char *dlogits, in
 #pragma unroll
     for (int j = 0; j < kGroup; ++j) {
         const int i = first + j * kTh, n = a.vocab - i * V::kN;
-        if (n <= 0) continue;
-        float g[V::kN];
-#pragma unroll
-        for (int e = 0; e < V::kN; ++e) g[e] = exp_from(V::get(v[j], e), r.top) * r.factor;
-        const int hit = t - i * V::kN;
-        if (hit >= 0 && hit < V::kN) {
-#pragma unroll
-            for (int e = 0; e < V::kN; ++e) g[e] += e == hit ? r.hot : 0.f;
-        }
-        V::store(dz + static_cast<int64_t>(i) * 16, g, n);
+        if (n > 0) gradient(v[j], i, n);
     }
 }
 
