@@ -62,7 +62,7 @@ typedef enum { LOGRA_F32 = 0, LOGRA_BF16 = 1, LOGRA_F64 = 2 } logra_dtype;
 #define LOGRA_MAX_ADAPTERS 1023       /* adapters of one plan */
 #define LOGRA_MAX_ADAPTER_RANK 128
 #define LOGRA_MAX_ADAPTER_ROWS 16777216
-#define LOGRA_MAX_NORM_COLS 32768
+#define LOGRA_MAX_NORM_COLS 16384
 #define LOGRA_MAX_ADAMW_GROUPS 65536
 #define LOGRA_ADAMW_BLOCK 256         /* elements that share a scale of the 8-bit states */
 

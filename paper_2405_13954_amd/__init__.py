@@ -736,10 +736,17 @@ def logra_token_loss(logits, target, loss, dlogits=None, weight=None, stream=Non
 
 
 # ------------------------------------------- layer norm, preference loss, AdamW --
-def _on_current(t, stream):
-    """Work on the current device's own streams is for tensors of that device."""
-    if stream is None and t.is_cuda and t.device.index != _torch().cuda.current_device():
-        raise ValueError(f"the tensors are on {t.device}, the current device is {_torch().cuda.current_device()}")
+def _queue(t, stream):
+    """The stream of a call on t, as an integer: `stream`, or the current one of t's device, which has to be the current
+    device."""
+    if stream is not None or not t.is_cuda:
+        return _stream(stream).value
+    torch = _torch()
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
+        raise ValueError(f"the tensors are on {t.device}, the current device is {device}")
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
 def logra_layer_norm_forward(x, y, gain=None, bias=None, eps: float = 1e-5, rms: bool = False, mask=None, residual=None,
@@ -749,11 +756,10 @@ def logra_layer_norm_forward(x, y, gain=None, bias=None, eps: float = 1e-5, rms:
 
     y, residual (None: none) and h (None: not wanted) [rows, cols] of x's dtype; y and h may each be x or residual.  gain
     and bias [cols] of x's dtype, or None.  mask [rows] uint8: rows with 0 are not read, and give zeros.  mean and rstd
-    [rows] fp32 or None: kept for the backward pass.  Any number of columns up to 32768, at row strides that are
+    [rows] fp32 or None: kept for the backward pass.  Any number of columns up to 16384, at row strides that are
     multiples of 16 bytes.
     """
     torch = _torch()
-    _on_current(x, stream)
     rows, cols = x.shape
     dt, f32 = x.dtype, torch.float32
     px, ld_x = _matrix(x, rows, cols, dt, "x")
@@ -763,7 +769,7 @@ def logra_layer_norm_forward(x, y, gain=None, bias=None, eps: float = 1e-5, rms:
     _check(lib().logra_layer_norm_forward(
         px, ld_x, _dtype_code(x), rows, cols, int(rms), eps, _packed(mask, (rows,), torch.uint8, "mask"),
         _packed(gain, (cols,), dt, "gain"), _packed(bias, (cols,), dt, "bias"), pr, ld_r, ph, ld_h, py, ld_y,
-        _packed(mean, (rows,), f32, "mean"), _packed(rstd, (rows,), f32, "rstd"), _stream(stream)))
+        _packed(mean, (rows,), f32, "mean"), _packed(rstd, (rows,), f32, "rstd"), _queue(x, stream)))
 
 
 def logra_layer_norm_ws_size(rows, cols) -> int:
@@ -778,7 +784,6 @@ def logra_layer_norm_backward(h, dy, rstd, mean=None, gain=None, rms: bool = Fal
     row has dx = base.  ws: a workspace of logra_layer_norm_ws_size bytes, allocated for the call when None.
     """
     torch = _torch()
-    _on_current(h, stream)
     rows, cols = h.shape
     dt, f32 = h.dtype, torch.float32
     ph, ld_h = _matrix(h, rows, cols, dt, "h")
@@ -791,7 +796,7 @@ def logra_layer_norm_backward(h, dy, rstd, mean=None, gain=None, rms: bool = Fal
         ph, ld_h, pdy, ld_dy, _dtype_code(h), rows, cols, int(rms), _packed(mask, (rows,), torch.uint8, "mask"),
         _packed(gain, (cols,), dt, "gain"), _packed(mean, (rows,), f32, "mean"), _packed(rstd, (rows,), f32, "rstd"), pb,
         ld_b, pdx, ld_dx, _packed(dgain, (cols,), f32, "dgain"), _packed(dbias, (cols,), f32, "dbias"), int(accumulate),
-        ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+        ws.data_ptr(), ws.numel() * ws.element_size(), _queue(h, stream)))
 
 
 def logra_preference_loss_ws_size(rows, n_pairs) -> int:
@@ -810,7 +815,6 @@ def logra_preference_loss(logits, target, offsets, logp, loss=None, dlogits=None
     the call when None.
     """
     torch = _torch()
-    _on_current(logits, stream)
     rows, vocab = logits.shape
     if offsets.dim() != 1 or offsets.shape[0] % 2 != 1:
         raise ValueError(f"offsets must hold an even number of sequences and an end, got {tuple(offsets.shape)}")
@@ -823,7 +827,7 @@ def logra_preference_loss(logits, target, offsets, logp, loss=None, dlogits=None
         pz, ld, _dtype_code(logits), rows, vocab, _packed(target, (rows,), torch.int64, "target"),
         _packed(offsets, (2 * n + 1,), torch.int64, "offsets"), n, _packed(ref, (2 * n,), f32, "ref"),
         _packed(weight, (n,), f32, "weight"), beta, smoothing, _packed(loss, (n,), f32, "loss"),
-        _packed(logp, (2 * n,), f32, "logp"), pd, ld_d, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+        _packed(logp, (2 * n,), f32, "logp"), pd, ld_d, ws.data_ptr(), ws.numel() * ws.element_size(), _queue(logits, stream)))
 
 
 class AdamwTensor(NamedTuple):
@@ -884,11 +888,10 @@ def logra_adamw_plan(tensors, n_groups: int, stream=None) -> AdamwPlan:
     their own, each clipped by its own norm.  Synchronous."""
     torch = _torch()
     descs = (AdamwDesc * len(tensors))(*[_adamw_desc(t, i) for i, t in enumerate(tensors)])
-    if tensors:
-        _on_current(tensors[0].param, stream)
     device = tensors[0].param.device if tensors else torch.device("cuda")
+    queue = _queue(tensors[0].param, stream) if tensors else _stream(stream).value
     memory = _scratch(int(lib().logra_adamw_plan_size(descs, len(tensors), n_groups)), device, stream)
-    _check(lib().logra_adamw_plan(descs, len(tensors), n_groups, memory.data_ptr(), memory.numel(), _stream(stream)))
+    _check(lib().logra_adamw_plan(descs, len(tensors), n_groups, memory.data_ptr(), memory.numel(), queue))
     return AdamwPlan(memory, tuple(tensors), n_groups)
 
 
@@ -900,9 +903,8 @@ def logra_adamw_step(plan: AdamwPlan, step, lr: float, beta1: float = 0.9, beta2
     norm (0: not); norms [n_groups] fp32 or None: the norms before that.  With either, a group whose norm is not finite is
     left as it is.  seed: of the random rounding of 8-bit states."""
     torch = _torch()
-    _on_current(plan.memory, stream)
     n, f32 = plan.n_groups, torch.float32
     _check(lib().logra_adamw_step(
         plan.memory.data_ptr(), plan.memory.numel(), n, _packed(step, (1,), torch.int64, "step"), lr, beta1, beta2, eps,
         weight_decay, max_norm, _packed(lr_scale, (n,), f32, "lr_scale"), _packed(norms, (n,), f32, "norms"), seed,
-        _stream(stream)))
+        _queue(plan.memory, stream)))

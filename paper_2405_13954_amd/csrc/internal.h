@@ -188,7 +188,7 @@ hipError_t launch_token_loss(const void *logits, int64_t ld, bool bf16, int64_t 
                              const float *weight, float *loss, void *dlogits, int64_t ld_d, hipStream_t s);
 
 // Layer norm (norm.hip), preference loss (preference.hip), AdamW (adamw.hip).
-constexpr int kMaxNormCols = 32768;   // a row is held in one workgroup's registers
+constexpr int kMaxNormCols = 16384;   // a row is held in one workgroup's registers
 struct NormForward {
     const void *x, *residual;
     void *h, *y;

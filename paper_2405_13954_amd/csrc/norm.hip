@@ -51,6 +51,28 @@ __device__ __forceinline__ u32x4 take(const char *p, int n) {
     return n > 0 ? Vec<BF16>::load(p, n, kZero4) : kZero4;
 }
 
+// The same for a row that another one follows: row strides are whole vectors, so what a partial vector's load brings
+// besides lies between the rows.  first_of drops it where the vector is used, so that the load need not be waited for here.
+template <bool BF16>
+__device__ __forceinline__ u32x4 take_inner(const char *p, int n, bool inner) {
+    if (n >= Vec<BF16>::kN || (inner && n > 0)) return ld128(p);
+    return n > 0 ? Vec<BF16>::load(p, n, kZero4) : kZero4;
+}
+
+// The first n elements of v, zeros behind them.
+template <bool BF16>
+__device__ __forceinline__ u32x4 first_of(u32x4 v, int n) {
+    if (n >= Vec<BF16>::kN) return v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (BF16)
+            v[j] = n >= 2 * j + 2 ? v[j] : n == 2 * j + 1 ? v[j] & 0xFFFFu : 0u;
+        else
+            v[j] = n > j ? v[j] : 0u;
+    }
+    return v;
+}
+
 // Sum over a row's team, the same in every thread, in a fixed order.  red: a slot for each wave, of this call alone until
 // the next but one barrier.
 template <int TPR>
@@ -93,14 +115,17 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
         }
         return;
     }
+    const bool inner = row + 1 < a.rows;
     u32x4 h[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) h[k] = take<BF16>(x + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN);
+    for (int k = 0; k < NV; ++k)
+        h[k] = take_inner<BF16>(x + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN, inner);
     if (a.res) {
         const char *r = a.res + row * a.ld_r * kEs;
         u32x4 v[NV];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) v[k] = take<BF16>(r + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN);
+        for (int k = 0; k < NV; ++k)
+            v[k] = take_inner<BF16>(r + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN, inner);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float s[V::kN];
@@ -109,6 +134,8 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
             h[k] = V::pack(s);   // the sum is rounded where it is stored, and the norm is that of the stored sum
         }
     }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) h[k] = first_of<BF16>(h[k], a.cols - (k * TPR + lane) * V::kN);
     const float per = 1.f / static_cast<float>(a.cols);
     float mean = 0.f;
     if constexpr (CENTER) {
@@ -155,7 +182,7 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
 // A team's share of one row.
 template <int NV>
 struct RowPart {
-    u32x4 h[NV], dy[NV], base[NV];
+    u32x4 h[NV], dy[NV];
     float mean, rstd;
     bool live;
 };
@@ -165,51 +192,95 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
     using V = Vec<BF16>;
     constexpr int kTh = TPR < 512 ? 512 : TPR, kTeams = kTh / TPR, kEs = BF16 ? 2 : 4, kW = TPR > 64 ? TPR / 64 : 1;
     constexpr int kCols = TPR * NV * V::kN;
+    // What registers are kept for: up to 24 columns of a thread, the next row and the gain in fp32; from 32 on the gain waits
+    // in LDS, base is not loaded ahead, and the packed row is unpacked again for dx; a workgroup of 1024 threads loads no row
+    // ahead.
+    constexpr bool kAhead = TPR < 1024, kTight = NV * V::kN >= 32 || TPR == 1024;
+    __shared__ u32x4 gains[kTight ? NV * TPR : 1];
     __shared__ float red[2][2][kTh / 64];          // by parity of the row, sum, wave
     __shared__ __attribute__((aligned(16))) float joined[kTeams > 1 ? kTeams * kCols : 4];
     const int lane = static_cast<int>(threadIdx.x) % TPR, team = static_cast<int>(threadIdx.x) / TPR;
     const int64_t stride = static_cast<int64_t>(gridDim.x) * kTeams;
     const float per = 1.f / static_cast<float>(a.cols);
-    u32x4 gain[NV];
+    float gain[kTight ? 1 : NV][V::kN];
     float dg[NV][V::kN] = {}, db[NV][V::kN] = {};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int i = k * TPR + lane;
-        gain[k] = a.gain ? take<BF16>(a.gain + i * 16, a.cols - i * V::kN) : kZero4;
+        const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        const u32x4 v = a.gain ? take<BF16>(a.gain + i * 16, a.cols - i * V::kN) : V::pack(ones);
+        if constexpr (kTight) {
+            gains[i] = v;   // (read by this thread alone: the teams of such rows are whole workgroups)
+        } else {
+#pragma unroll
+            for (int e = 0; e < V::kN; ++e) gain[k][e] = V::get(v, e);
+        }
     }
+    const auto gain_of = [&](int k, float (&g)[V::kN]) {
+        u32x4 v = kZero4;
+        if constexpr (kTight) v = gains[k * TPR + lane];
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) g[e] = kTight ? V::get(v, e) : gain[kTight ? 0 : k][e];
+    };
     const auto load = [&](int64_t row, RowPart<NV> &p) {
         p.live = row < a.rows && (!a.mask || a.mask[row] != 0);
         p.mean = CENTER && p.live ? a.mean[row] : 0.f;
         p.rstd = p.live ? a.rstd[row] : 0.f;
-        const int width = p.live ? a.cols : 0, width_b = row < a.rows && a.base ? a.cols : 0;
+        const int width = p.live ? a.cols : 0;
+        const bool inner = row + 1 < a.rows;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int i = k * TPR + lane;
-            p.h[k] = take<BF16>(a.h + row * a.ld_h * kEs + i * 16, width - i * V::kN);
-            p.dy[k] = take<BF16>(a.dy + row * a.ld_dy * kEs + i * 16, width - i * V::kN);
-            p.base[k] = take<BF16>(a.base + row * a.ld_b * kEs + i * 16, width_b - i * V::kN);
+            p.h[k] = take_inner<BF16>(a.h + row * a.ld_h * kEs + i * 16, width - i * V::kN, inner);
+            p.dy[k] = take_inner<BF16>(a.dy + row * a.ld_dy * kEs + i * 16, width - i * V::kN, inner);
+        }
+    };
+    u32x4 base[NV], next_base[kTight ? 1 : NV];
+    const auto load_base = [&](int64_t row, u32x4 *to) {
+        const int width = row < a.rows && a.base ? a.cols : 0;
+        const bool inner = row + 1 < a.rows;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int i = k * TPR + lane;
+            to[k] = take_inner<BF16>(a.base + row * a.ld_b * kEs + i * 16, width - i * V::kN, inner);
         }
     };
     const int64_t rounds = (a.rows + stride - 1) / stride;   // the same for the whole workgroup: there are barriers inside
     int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team;
     RowPart<NV> cur, next;
-    load(row, cur);
+    if (kAhead) load(row, cur);
+    if (!kTight) load_base(row, base);
     for (int64_t it = 0; it < rounds; ++it, row += stride) {
-        if (it + 1 < rounds) load(row + stride, next);
+        if (!kAhead) load(row, cur);
+        if (kTight) load_base(row, base);
+        if (it + 1 < rounds) {
+            if (kAhead) load(row + stride, next);
+            if (!kTight) load_base(row + stride, next_base);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int n = a.cols - (k * TPR + lane) * V::kN;
+            cur.h[k] = first_of<BF16>(cur.h[k], n);
+            cur.dy[k] = first_of<BF16>(cur.dy[k], n);
+        }
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            float g[V::kN];
+            gain_of(k, g);
 #pragma unroll
             for (int e = 0; e < V::kN; ++e) {
-                const float dy = V::get(cur.dy[k], e), c = a.gain ? dy * V::get(gain[k], e) : dy;
-                const float xh = (V::get(cur.h[k], e) - cur.mean) * cur.rstd;
+                const float dy = V::get(cur.dy[k], e), c = dy * g[e];
+                const float d = CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e);
                 if constexpr (CENTER) {
                     s1 += c;
                     db[k][e] += dy;
                 }
-                s2 = fmaf(c, xh, s2);
-                dg[k][e] = fmaf(dy, xh, dg[k][e]);
+                s2 = fmaf(c, d, s2);
+                dg[k][e] = fmaf(dy, d * cur.rstd, dg[k][e]);
             }
+            if constexpr (kTight) asm volatile("" : "+v"(cur.h[k]), "+v"(cur.dy[k]));   // not its fp32 values are kept
+        }
 #pragma unroll
         for (int m = (TPR < 64 ? TPR : 64) / 2; m; m >>= 1) {
             s2 += __shfl_xor(s2, m);
@@ -230,25 +301,30 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
                 s2 += r[1][team * kW + w];
             }
         }
-        s1 *= per;
-        s2 *= per;
+        // dx - base = rstd (c - avg(c) - xh avg(c xh)) = rstd c + (h - mean) along + level.  (A masked row has zeros in all.)
+        // The sum comes first: it is as small as rstd is large, so that the product of a row without variance stays finite.
+        const float level = -cur.rstd * (s1 * per), along = -(s2 * per) * cur.rstd * cur.rstd * cur.rstd;
         if (a.dx && row < a.rows) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const int i = k * TPR + lane, n = a.cols - i * V::kN;
                 if (n <= 0) continue;
-                float o[V::kN];
+                float o[V::kN], g[V::kN];
+                gain_of(k, g);
 #pragma unroll
                 for (int e = 0; e < V::kN; ++e) {
-                    const float dy = V::get(cur.dy[k], e), c = a.gain ? dy * V::get(gain[k], e) : dy;
-                    const float xh = (V::get(cur.h[k], e) - cur.mean) * cur.rstd;
-                    const float t = cur.rstd * (c - s1 - xh * s2);
-                    o[e] = V::get(cur.base[k], e) + (cur.live ? t : 0.f);
+                    const float c = V::get(cur.dy[k], e) * g[e];
+                    const float d = CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e);
+                    o[e] = V::get(base[k], e) + fmaf(c, cur.rstd, fmaf(d, along, level));
                 }
                 V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
             }
         }
-        cur = next;
+        if (kAhead) cur = next;
+        if constexpr (!kTight) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) base[k] = next_base[k];
+        }
     }
     const auto write = [&](float (&sum)[NV][V::kN], float *part) {
         if (!part) return;
@@ -316,47 +392,31 @@ __global__ __launch_bounds__(256) void k_norm_parts(const float *part_g, const f
     out[mine] = accumulate ? out[mine] + t : t;
 }
 
-// The smallest team whose threads hold a row in at most `most` vectors each, from 32 threads on.
-int team_of(int vectors, int most) {
-    int t = 32;
-    while (t < 1024 && vectors > t * most) t *= 2;
-    return t;
-}
-
 template <int N>
 using int_c = std::integral_constant<int, N>;
 
-// go(team, vectors a thread), as compile-time constants, for a row of `vectors`
-template <class Go>
-void with_team(int team, int vectors, const Go &go) {
-    const int nv = (vectors + team - 1) / team;
-    const auto pick = [&](auto t) {
-        constexpr int T = decltype(t)::value;
-        if (nv <= 1) go(t, int_c<1>{});
-        else if (nv <= 2) go(t, int_c<2>{});
-        else if (nv <= 3) go(t, int_c<3>{});
-        else if (T < 1024 || nv <= 4) go(t, int_c<4>{});
-        else go(t, int_c<8>{});
-    };
-    switch (team) {
-        case 32: return pick(int_c<32>{});
-        case 64: return pick(int_c<64>{});
-        case 128: return pick(int_c<128>{});
-        case 256: return pick(int_c<256>{});
-        case 512: return pick(int_c<512>{});
-        default: return pick(int_c<1024>{});
+// Calls go(team, vectors a thread), as compile-time constants: the smallest team from 32 to LARGEST threads that holds a
+// row of `vectors` in at most MOST vectors a thread.
+template <int MOST, int LARGEST, int TEAM = 32, class Go>
+void with_team(int vectors, const Go &go) {
+    constexpr int kLeast = TEAM == 32 ? 1 : MOST / 2 + 1;   // (fewer, and a smaller team would do)
+    if constexpr (TEAM < LARGEST) {
+        if (vectors > TEAM * MOST) return with_team<MOST, LARGEST, TEAM * 2>(vectors, go);
     }
+    const int nv = (vectors + TEAM - 1) / TEAM;
+    if constexpr (kLeast <= 1 && MOST >= 1)
+        if (nv <= 1) return go(int_c<TEAM>{}, int_c<1>{});
+    if constexpr (kLeast <= 2 && MOST >= 2)
+        if (nv <= 2) return go(int_c<TEAM>{}, int_c<2>{});
+    if constexpr (kLeast <= 3 && MOST >= 3)
+        if (nv <= 3) return go(int_c<TEAM>{}, int_c<3>{});
+    if constexpr (MOST >= 4) go(int_c<TEAM>{}, int_c<4>{});
 }
 
 int vectors_of(bool bf16, int cols) { return (cols + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4); }
 
-// Workgroups of the backward pass: two on each CU, as many as there are rows for.
-constexpr int kBwdGroups = 512;
-int bwd_groups(int team, int64_t rows) {
-    const int teams = team < 512 ? 512 / team : 1;
-    const int64_t g = (rows + teams - 1) / teams;
-    return static_cast<int>(g < kBwdGroups ? g : kBwdGroups);
-}
+// Workgroups of the backward pass: one on each CU, as many as there are rows for.
+constexpr int kBwdGroups = 256;
 
 }  // namespace
 
@@ -371,7 +431,6 @@ hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
                  static_cast<char *>(n.y), n.ld_x, n.ld_res, n.ld_h, n.ld_y, n.rows, n.mask,
                  static_cast<const char *>(n.gain), static_cast<const char *>(n.bias), n.mean, n.rstd, n.cols, n.eps};
     const int vec = vectors_of(n.bf16, n.cols);
-    const int team = team_of(vec, n.rows <= 1024 ? 1 : 4);
     const auto go = [&](auto t, auto v) {
         constexpr int T = decltype(t)::value, NV = decltype(v)::value;
         const int teams = T <= 64 ? 256 / T : 1;
@@ -384,31 +443,45 @@ hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
         else
             n.rms ? k_norm_fwd<false, T, NV, false><<<grid, th, 0, s>>>(a) : k_norm_fwd<false, T, NV, true><<<grid, th, 0, s>>>(a);
     };
-    with_team(team, vec, go);
+    // few rows: one vector a thread, for the shortest way through a row; many: four, for fewer threads that wait
+    if (n.rows <= 1024 && vec <= 1024)
+        with_team<1, 1024>(vec, go);
+    else
+        with_team<4, 1024>(vec, go);
     return hipGetLastError();
 }
 
 hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s) {
     const int vec = vectors_of(n.bf16, n.cols);
-    const int team = team_of(vec, 3);
-    const int groups = bwd_groups(team, n.rows);   // (0 without rows: the gradients' sums are empty)
-    float *part_g = n.dgain ? static_cast<float *>(n.ws) : nullptr;
-    float *part_b = n.dbias ? static_cast<float *>(n.ws) + static_cast<int64_t>(groups) * padded(n.cols) : nullptr;
-    BwdArgs a = {static_cast<const char *>(n.h), static_cast<const char *>(n.dy), static_cast<const char *>(n.base),
-                 static_cast<char *>(n.dx), n.ld_h, n.ld_dy, n.ld_base, n.ld_dx, n.rows, n.mask,
-                 static_cast<const char *>(n.gain), n.mean, n.rstd, part_g, part_b, n.cols};
-    const auto go = [&](auto t, auto v) {
+    int groups = 0;   // (without rows: the gradients' sums are empty)
+    float *part_g = nullptr, *part_b = nullptr;
+    const auto launch = [&](auto t, auto v, auto is_bf16) {
         constexpr int T = decltype(t)::value, NV = decltype(v)::value;
-        constexpr int th = T < 512 ? 512 : T;
-        if (n.bf16)
-            n.rms ? k_norm_bwd<true, T, NV, false><<<groups, th, 0, s>>>(a) : k_norm_bwd<true, T, NV, true><<<groups, th, 0, s>>>(a);
-        else
-            n.rms ? k_norm_bwd<false, T, NV, false><<<groups, th, 0, s>>>(a) : k_norm_bwd<false, T, NV, true><<<groups, th, 0, s>>>(a);
+        constexpr bool B = decltype(is_bf16)::value;
+        constexpr int th = T < 512 ? 512 : T, teams = th / T;
+        const int64_t g = (n.rows + teams - 1) / teams;
+        groups = static_cast<int>(g < kBwdGroups ? g : kBwdGroups);
+        part_g = n.dgain ? static_cast<float *>(n.ws) : nullptr;
+        part_b = n.dbias ? static_cast<float *>(n.ws) + static_cast<int64_t>(groups) * padded(n.cols) : nullptr;
+        const BwdArgs a = {static_cast<const char *>(n.h), static_cast<const char *>(n.dy), static_cast<const char *>(n.base),
+                           static_cast<char *>(n.dx), n.ld_h, n.ld_dy, n.ld_base, n.ld_dx, n.rows, n.mask,
+                           static_cast<const char *>(n.gain), n.mean, n.rstd, part_g, part_b, n.cols};
+        n.rms ? k_norm_bwd<B, T, NV, false><<<groups, th, 0, s>>>(a) : k_norm_bwd<B, T, NV, true><<<groups, th, 0, s>>>(a);
     };
-    if (n.rows > 0) with_team(team, vec, go);
+    const auto go = [&](auto t, auto v) { n.bf16 ? launch(t, v, std::true_type{}) : launch(t, v, std::false_type{}); };
+    if (n.rows > 0) {
+        if (vec <= 3 * 512)
+            with_team<3, 512>(vec, go);
+        else if (vec <= 4 * 512)
+            go(int_c<512>{}, int_c<4>{});
+        else if (vec <= 3 * 1024)   // (fp32)
+            launch(int_c<1024>{}, int_c<3>{}, std::false_type{});
+        else
+            launch(int_c<1024>{}, int_c<4>{}, std::false_type{});
+    }
     if (n.dgain || n.dbias)
-        k_norm_parts<<<dim3(static_cast<uint32_t>(n.cols + 31) / 32, n.dbias ? 2 : 1), 256, 0, s>>>(part_g, part_b, groups, n.cols, n.dgain,
-                                                                                      n.dbias, n.accumulate);
+        k_norm_parts<<<dim3(static_cast<uint32_t>(n.cols + 31) / 32, n.dbias ? 2 : 1), 256, 0, s>>>(
+            part_g, part_b, groups, n.cols, n.dgain, n.dbias, n.accumulate);
     return hipGetLastError();
 }
 

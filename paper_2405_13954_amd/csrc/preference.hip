@@ -265,7 +265,13 @@ size_t preference_ws_bytes(int64_t rows) {
 
 hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s) {
     const int vec = (p.vocab + (p.bf16 ? 7 : 3)) / (p.bf16 ? 8 : 4);
-    int splits = (vec + 16 * kTh - 1) / (16 * kTh);
+    // Ranges of 16 vectors a thread; shorter ones, of four at least, where there are few rows: eight workgroups on a CU.
+    // us of k_pair_stats with at most 4, 8, 16 and 32: 2,048 rows of 128,000 bf16 logits, 0.3 of them masked, 84, 70, 68
+    // and 72; 61 rows of 5,001 fp32 logits 4.0, 4.8, 4.8 and 4.7.
+    const auto ranges = [&](int of) { return (vec + of * kTh - 1) / (of * kTh); };
+    const int64_t wanted = (2048 + p.rows - 1) / (p.rows > 0 ? p.rows : 1);
+    int splits = static_cast<int>(wanted < ranges(4) ? wanted : ranges(4));
+    splits = splits > ranges(16) ? splits : ranges(16);
     splits = splits < kMaxSplits ? splits : kMaxSplits;
     char *ws = static_cast<char *>(p.ws);
     PairArgs a = {static_cast<const char *>(p.logits), p.ld, p.rows, p.target, p.offsets, reinterpret_cast<float2 *>(ws),
