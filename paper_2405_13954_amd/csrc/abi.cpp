@@ -8,6 +8,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <utility>
 #include <vector>
 
@@ -1030,13 +1031,13 @@ Region flat(const void *p, int64_t n, size_t bytes) {
     const uint64_t size = static_cast<uint64_t>(n) * bytes;
     return {static_cast<uint64_t>(reinterpret_cast<uintptr_t>(p)), size > 0 ? size : 1, size, 1};
 }
-int check_operands(const std::vector<Operand> &in, const std::vector<Operand> &out) {
-    for (size_t i = 0; i < out.size(); ++i) {
-        if (!out[i].at.at) continue;
+int check_operands(std::initializer_list<Operand> in, std::initializer_list<Operand> out) {
+    for (const Operand &w : out) {
+        if (!w.at.at) continue;
         for (const Operand &r : in)
-            if (r.at.at) TRY(check_apart(r.name, r.at, out[i].name, out[i].at, r.in_place && out[i].in_place));
-        for (size_t j = 0; j < i; ++j)
-            if (out[j].at.at) TRY(check_apart(out[j].name, out[j].at, out[i].name, out[i].at, false));
+            if (r.at.at) TRY(check_apart(r.name, r.at, w.name, w.at, r.in_place && w.in_place));
+        for (const Operand *o = out.begin(); o != &w; ++o)
+            if (o->at.at) TRY(check_apart(o->name, o->at, w.name, w.at, false));
     }
     return LOGRA_OK;
 }

@@ -112,21 +112,21 @@ __global__ __launch_bounds__(kTh) void k_pair_stats(PairArgs a) {
 
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
 
-constexpr int kSumTh = 1024;
-
 // One workgroup per pair.  What a row needs is loaded at once, whether the row counts or not; what was found of a thread's
 // first row of each sequence stays in registers.
+template <int kSumTh>
 __global__ __launch_bounds__(kSumTh) void k_pair_sums(PairArgs a, const float *ref, const float *weight, double beta,
                                                       double smoothing, float *loss, float *logp) {
+    const int64_t pair = blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y;
+    if (pair >= a.pairs) return;
     constexpr float kNone = -__builtin_inff();
     constexpr int kWaves = kSumTh / 64;
     __shared__ double red[2][kWaves];
-    const int pair = static_cast<int>(blockIdx.x);
     int64_t cut[3];
     const int64_t first = a.offsets[0], last = a.offsets[2 * static_cast<int64_t>(a.pairs)];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {   // whatever the offsets hold, rows outside the logits are not touched
-        const int64_t o = a.offsets[2 * static_cast<int64_t>(pair) + i];
+        const int64_t o = a.offsets[2 * pair + i];
         cut[i] = o < 0 ? 0 : o > a.rows ? a.rows : o;
     }
     const auto stats = [&](int64_t row, float &top, float &total) {   // returns the row's log probability
@@ -173,15 +173,15 @@ __global__ __launch_bounds__(kSumTh) void k_pair_sums(PairArgs a, const float *r
         sum[0] += red[0][w];
         sum[1] += red[1][w];
     }
-    const double ratio_c = sum[0] - (ref ? static_cast<double>(ref[2 * static_cast<int64_t>(pair)]) : 0.0);
-    const double ratio_r = sum[1] - (ref ? static_cast<double>(ref[2 * static_cast<int64_t>(pair) + 1]) : 0.0);
+    const double ratio_c = sum[0] - (ref ? static_cast<double>(ref[2 * pair]) : 0.0);
+    const double ratio_r = sum[1] - (ref ? static_cast<double>(ref[2 * pair + 1]) : 0.0);
     const double d = beta * (ratio_c - ratio_r);
     const double w = weight ? static_cast<double>(weight[pair]) : 1.0;
     const bool off = w == 0.0;   // a pair that does not count, whatever its logits hold
     const double slope = off ? 0.0 : w * beta * (smoothing - 1.0 / (1.0 + exp(d)));
     if (threadIdx.x == 0) {
-        logp[2 * static_cast<int64_t>(pair)] = static_cast<float>(sum[0]);
-        logp[2 * static_cast<int64_t>(pair) + 1] = static_cast<float>(sum[1]);
+        logp[2 * pair] = static_cast<float>(sum[0]);
+        logp[2 * pair + 1] = static_cast<float>(sum[1]);
         const double flipped = smoothing > 0.0 ? smoothing * softplus(d) : 0.0;
         const double kept = smoothing < 1.0 ? (1.0 - smoothing) * softplus(-d) : 0.0;
         if (loss) loss[pair] = off ? 0.f : static_cast<float>(w * (kept + flipped));
@@ -282,7 +282,15 @@ hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s) {
         const dim3 grid = grid_of(p.rows * splits);
         p.bf16 ? k_pair_stats<true><<<grid, kTh, 0, s>>>(a) : k_pair_stats<false><<<grid, kTh, 0, s>>>(a);
     }
-    k_pair_sums<<<p.pairs, kSumTh, 0, s>>>(a, p.ref, p.weight, p.beta, p.smoothing, p.loss, p.logp);
+    const auto sums = [&](auto kernel, int threads) {
+        kernel<<<grid_of(p.pairs), threads, 0, s>>>(a, p.ref, p.weight, p.beta, p.smoothing, p.loss, p.logp);
+    };
+    // 256 threads where most sequences have no more rows: 32 pairs in 2,041 rows 5.7 us against 6.1 with 1024, 8 pairs in
+    // 2,048 rows 7.4 against 6.4.
+    if (p.rows <= 128 * static_cast<int64_t>(p.pairs))
+        sums(k_pair_sums<256>, 256);
+    else
+        sums(k_pair_sums<1024>, 1024);
     if (p.dlogits && p.rows > 0) {
         const int pieces = (vec + 4 * kTh - 1) / (4 * kTh);
         const dim3 grid = grid_of(p.rows * pieces);
