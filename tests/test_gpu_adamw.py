@@ -153,6 +153,36 @@ def test_a_tensor_of_many_chunks_and_many_groups():
     check_steps(np.random.default_rng(6), [(9, 2056, 2)], 8, 11, steps=1, max_norm=3.0)
 
 
+def test_a_plan_of_thousands_of_chunks():
+    check_steps(np.random.default_rng(12), [(2, (1 << 20) + 5, 0), (1, 300, 1), (3, 70, 0)], 32, 4, steps=2, max_norm=400.0)
+
+
+def test_the_ways_to_a_groups_factors_agree():
+    # a plan in more memory than it needs counts as one of many chunks, whose groups get a launch of their own
+    import ctypes
+    import torch
+    import paper_2405_13954_amd as P
+    shapes = [(3, 5000, 1), (1, 777, 0), (2, 256, 2)]
+    for bits in (32, 8):
+        runs = []
+        for wide in (False, True):
+            model = Model(np.random.default_rng(13), shapes, bits)
+            plan = P.logra_adamw_plan(model.tensors, 5)
+            if wide:
+                descs = (P.AdamwDesc * len(model.tensors))(*[P._adamw_desc(t, i) for i, t in enumerate(model.tensors)])
+                memory = torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda")
+                stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+                assert P.lib().logra_adamw_plan(descs, len(descs), 5, memory.data_ptr(), memory.numel(), stream) == P.OK
+                plan = plan._replace(memory=memory)
+            step, norms = torch.full((1,), 6, dtype=torch.int64, device="cuda"), torch.full((5,), 9.0, device="cuda")
+            scale = torch.tensor([1.0, 0.5, 2.0, 0.25, 3.0], device="cuda")
+            for _ in range(3):
+                P.logra_adamw_step(plan, step, 1e-2, max_norm=2.0, lr_scale=scale, norms=norms, weight_decay=0.1, seed=3)
+            assert int(step) == 9 and norms[4] == 0            # (no tensor of group 4)
+            runs.append([t.clone().view(torch.uint8) for d in model.dev for t in d.values()] + [norms.view(torch.uint8)])
+        assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
 def test_the_plain_adam_of_small_gradients():
     # gradients of 1e-20: v is below the smallest normal fp32 number, and the move is that of eps
     import torch
