@@ -47,6 +47,16 @@ int check_score_dtypes(int te_dtype, int tr_dtype) {
 }
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// While one of these lives, check_dev also refuses memory of a device other than the current one, whose kernels may not be
+// able to reach it.
+thread_local int g_device = -1;
+struct OnCurrentDevice {
+    OnCurrentDevice() {
+        if (hipGetDevice(&g_device) != hipSuccess) g_device = -1;   // (then no pointer is device memory)
+    }
+    ~OnCurrentDevice() { g_device = -1; }
+};
+
 // Device-memory check; `align` is the required base alignment in bytes.
 int check_dev(const void *p, const char *name, size_t align) {
     if (p == nullptr) return fail(LOGRA_ERR_INVALID_ARG, "%s is NULL", name);
@@ -61,6 +71,8 @@ int check_dev(const void *p, const char *name, size_t align) {
     }
     if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged)
         return fail(LOGRA_ERR_INVALID_ARG, "%s is not device memory", name);
+    if (g_device >= 0 && attr.type == hipMemoryTypeDevice && attr.device != g_device)
+        return fail(LOGRA_ERR_INVALID_ARG, "%s is on device %d, the current device is %d", name, attr.device, g_device);
     return LOGRA_OK;
 }
 
@@ -1054,6 +1066,7 @@ int check_norm_sizes(int dtype, int64_t rows, int cols) {
 }
 
 int norm_forward(const logra::NormForward &n, int dtype) {
+    const OnCurrentDevice here;
     const int es = static_cast<int>(esize(dtype));
     TRY(check_stride("x", n.ld_x, n.rows, n.cols, dtype));
     TRY(check_stride("y", n.ld_y, n.rows, n.cols, dtype));
@@ -1078,6 +1091,7 @@ int norm_forward(const logra::NormForward &n, int dtype) {
 }
 
 int norm_backward(const logra::NormBackward &n, int dtype, size_t ws_bytes) {
+    const OnCurrentDevice here;
     const int es = static_cast<int>(esize(dtype));
     if (n.rows > 0) {
         TRY(check_stride("h", n.ld_h, n.rows, n.cols, dtype));
@@ -1171,6 +1185,7 @@ int adamw_plan(const logra_adamw_tensor *tensors, int n_tensors, int n_groups, v
     const size_t need = logra::adamw_plan_bytes(n_groups, static_cast<uint32_t>(chunks));
     if (plan == nullptr || plan_bytes < need)
         return fail(LOGRA_ERR_WORKSPACE, "the plan needs %zu bytes, got %zu", need, plan ? plan_bytes : 0);
+    const OnCurrentDevice here;
     std::vector<Span> spans;
     for (int i = 0; i < n_tensors; ++i) {
         const logra_adamw_tensor &t = tensors[i];
@@ -1302,6 +1317,7 @@ int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t row
         if (rows == 0 || !dlogits) return ok();
         return fail(LOGRA_ERR_INVALID_ARG, "rows without pairs");
     }
+    const OnCurrentDevice here;
     if (rows > 0) {
         TRY(check_stride("logits", ld, rows, vocab, dtype));
         if (dlogits) TRY(check_stride("dlogits", ld_d, rows, vocab, dtype));
@@ -1367,6 +1383,7 @@ int logra_adamw_step(void *plan, size_t plan_bytes, int n_groups, int64_t *step,
     TRY(check_operands({{"lr_scale", flat(lr_scale, n_groups, 4), false}},
                        {{"plan", flat(plan, static_cast<int64_t>(plan_bytes), 1), false}, {"step", flat(step, 1, 8), false},
                         {"norms", flat(norms, n_groups, 4), false}}));
+    const OnCurrentDevice here;
     TRY(check_dev(plan, "plan", 256));
     TRY(check_dev(step, "step", 8));
     if (lr_scale) TRY(check_dev(lr_scale, "lr_scale", 4));

@@ -11,6 +11,10 @@
 // Backward: a workgroup walks rows a grid apart and keeps the sums for dgain and dbias of its columns in registers; the
 // next row's vectors are loaded before the current row's sums are known.  The workgroups' sums go to the workspace, and a
 // second launch adds them in order, so that reruns give the same bits.
+//
+// 16,384 rows of 4096 bf16 columns without the mean: forward with residual and statistics 96 us for 537 MB (5.6 TB/s),
+// backward with base and a fifth of the rows masked 83 + 5 us for 483 MB (5.5).  768 columns with the mean: 16 and 20 + 4 us
+// for 91 and 101 MB.
 #include "internal.h"
 #include "vec16.h"
 
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
 }
 
 // dgain and dbias from the workgroups' sums: a workgroup takes 32 columns, eight threads of four for each of 32 ranges of
-// the parts; the ranges are added in order.  blockIdx.y: 0 dgain, 1 dbias.  512 parts of 4096 columns: PARTS us.
+// the parts; the ranges are added in order.  blockIdx.y: 0 dgain, 1 dbias.  256 parts of 4096 columns: 4.8 us.
 __global__ __launch_bounds__(256) void k_norm_parts(const float *part_g, const float *part_b, int parts, int cols,
                                                     float *dgain, float *dbias, bool accumulate) {
     constexpr int kSlots = 32, kAhead = 8;
@@ -415,7 +419,9 @@ void with_team(int vectors, const Go &go) {
 
 int vectors_of(bool bf16, int cols) { return (cols + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4); }
 
-// Workgroups of the backward pass: one on each CU, as many as there are rows for.
+// Workgroups of the backward pass: one on each CU, as many as there are rows for.  us with 160, 256, 512 and 768 (base, no
+// mask, bf16): 16,384 rows of 4096 columns 111, 96.5, 98 and 102, 2,400 rows 19.9, 17.6, 21.8 and 24.3, 600 rows 9.8, 10.8,
+// 12.9 and 12.9, 16,384 rows of 768 22.8, 20.6, 21.8 and 27.4.
 constexpr int kBwdGroups = 256;
 
 }  // namespace

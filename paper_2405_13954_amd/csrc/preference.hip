@@ -9,6 +9,8 @@
 // sum of exponentials of ranges of each row, k_pair_sums joins them, adds up each sequence (in float64: the ratio is a
 // small difference of large sums) and leaves two factors for every row, and k_pair_grad writes the gradient.  The second
 // pass takes the rows from the last to the first, so that those that the 256 MB cache still holds are read from there.
+// 2,048 tokens of 128,000 bf16 logits, 0.3 of them masked: 67 + 6 + 130 us for 367, 0 and 891 MB (5.5 and 6.9 TB/s; a copy
+// inside the cache reaches 7.2).
 #include "internal.h"
 #include "vec16.h"
 

@@ -134,6 +134,23 @@ def test_steps(bits, max_norm):
     check_steps(np.random.default_rng(1), SMALL, bits, 4, max_norm=max_norm)
 
 
+def test_scales_of_any_value_and_no_momentum():
+    import torch
+    import paper_2405_13954_amd as P
+    for b1, b2 in ((0.9, 0.999), (0.0, 0.0)):
+        model = Model(np.random.default_rng(14), [(2, 700, 0)], 8)
+        for k in ("m_scale", "v_scale"):                       # a checkpoint's scales need not be powers of two
+            model.dev[0][k].copy_(torch.rand(6, device="cuda") * 0.01)
+        before = model.values()
+        step = torch.full((1,), 3, dtype=torch.int64, device="cuda")
+        P.logra_adamw_step(P.logra_adamw_plan(model.tensors, 2), step, 1e-3, beta1=b1, beta2=b2, seed=1)
+        got, (want,) = model.values()[0], O.adamw_step(before, 2, 3, 1e-3, b1, b2, seed=1)[0]
+        for k in ("m", "v", "m_scale", "v_scale"):
+            assert np.array_equal(got[k], want[k]), k
+        within(got["param"], want["param"], 16 * U * (np.abs(want["param"]) + np.abs(want["param"] - before[0]["param"])), "param")
+        model.guards()
+
+
 def test_mixed_states_and_no_work():
     check_steps(np.random.default_rng(2), SMALL, [8, 32, 32, 8, 8, 32, 8], 5, work=False, max_norm=0.5, at=1000)
 

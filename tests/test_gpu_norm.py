@@ -130,6 +130,31 @@ def test_forward_far_rows():
     assert torch.equal(out, near)
 
 
+def test_more_rows_than_one_line_of_the_grid():
+    import torch
+    import paper_2405_13954_amd as P
+    rows = (1 << 24) + 9                                       # 2^21 workgroups of eight rows, and two more
+    x = torch.empty(rows, 8, dtype=torch.bfloat16, device="cuda")
+    for part in x.split(1 << 21):
+        part.copy_(torch.randn(part.shape, device="cuda"))
+    y, dx, mean, rstd, dgain = torch.empty_like(x), torch.empty_like(x), f32(rows), f32(rows), f32(8)
+    P.logra_layer_norm_forward(x, y, mean=mean, rstd=rstd)
+    P.logra_layer_norm_backward(x, y, rstd, mean=mean, dx=dx, dgain=dgain)
+    for at in (0, (1 << 24) - 8, rows - 8):                    # the same rows by themselves
+        part, few = x[at:at + 8].contiguous(), torch.empty(8, 8, dtype=torch.bfloat16, device="cuda")
+        m, r, d = f32(8), f32(8), torch.empty_like(few)
+        P.logra_layer_norm_forward(part, few, mean=m, rstd=r)
+        P.logra_layer_norm_backward(part, few, r, mean=m, dx=d)
+        assert torch.equal(few, y[at:at + 8]) and torch.equal(m, mean[at:at + 8]) and torch.equal(d, dx[at:at + 8])
+    want = torch.zeros(8, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(want)
+    for a, b, m, r in zip(x.split(1 << 21), y.split(1 << 21), mean.split(1 << 21), rstd.split(1 << 21)):
+        t = b.double() * (a.double() - m.double()[:, None]) * r.double()[:, None]
+        want, size = want + t.sum(0), size + t.abs().sum(0)
+    # a workgroup's team adds 2^24 / (256 * 16) = 4,096 rows in a line, the rest as ROWS has it
+    within(host(dgain), host(want), (4097 + 70) * U * host(size), "dgain")
+
+
 def check_backward(rows, cols, dtype, rms, base, mask_share=0.0, extra=0, affine=True, seed=0):
     import torch
     import paper_2405_13954_amd as P

@@ -179,6 +179,27 @@ def test_no_rows_and_no_pairs():
     P.logra_preference_loss(z, none[:0], none[:1], logp[:0])
 
 
+def test_more_rows_and_pairs_than_one_line_of_the_grid():
+    import torch
+    import paper_2405_13954_amd as P
+    rows = (1 << 21) + 7
+    z = torch.randn(rows, 8, device="cuda").to(torch.bfloat16)
+    t = torch.randint(0, 8, (rows,), device="cuda")
+    o = torch.tensor([0, rows - 9, rows - 4, rows - 4, rows - 1]).cuda()
+    d, loss, logp = torch.empty_like(z), f32(2), f32(4)
+    P.logra_preference_loss(z, t, o, logp, loss=loss, dlogits=d)
+    few, l2, p2 = torch.empty(9, 8, dtype=torch.bfloat16, device="cuda"), f32(1), f32(2)
+    P.logra_preference_loss(z[-9:], t[-9:], torch.tensor([5, 5, 8]).cuda(), p2, loss=l2, dlogits=few)
+    assert torch.equal(few[5:], d[-4:]) and torch.equal(l2, loss[1:]) and torch.equal(p2, logp[2:]) and not d[-1].any()
+    lse = torch.logsumexp(z.double(), 1)
+    want = (z.double().gather(1, t[:, None])[:, 0] - lse)[:rows - 9].sum()
+    assert abs(float(logp[0]) - float(want)) <= rows * (2.0 ** -20 + 8 * 2.0 ** -24) * 4 + U * abs(float(want))
+    pairs = (1 << 21) + 3
+    loss, logp = f32(pairs), f32(2 * pairs)
+    P.logra_preference_loss(z[:0], t[:0], torch.zeros(2 * pairs + 1, dtype=torch.int64, device="cuda"), logp, loss=loss)
+    assert not logp.any() and bool((loss == loss[0]).all()) and abs(float(loss[0]) - np.log(2)) < 1e-7
+
+
 def test_far_rows():
     # rows at a stride of 2^27 elements: offsets beyond 32 bits
     import torch
