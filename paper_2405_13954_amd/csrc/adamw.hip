@@ -10,7 +10,8 @@
 // sums into each group's factors (k_adamw_head).  Bound by memory: 28 bytes an element with fp32 states, 16 with 8-bit ones,
 // 2 more for the bf16 copy, and 4 to read the gradient twice where it is clipped.  10.5 million elements of 15 tensors with
 // the copy and clipping, fp32 states: 14 + 7 + 54 us, the last 5.9 TB/s; 42 million with 8-bit states: 47 + 7 + 130 us, 5.8.
-// (The sum of the squares pays for the step before it, whose results the caches still write back: 3.6 TB/s.)
+// (The sum of the squares pays for the step before it, whose results the caches still write back: behind a launch that only
+// reads it takes 29 us, 5.8 TB/s.)
 // Sums and factors in one launch, by the workgroup that is the last to finish, took 77 us for the 14 + 7: every workgroup's
 // release of its sum costs some 50 ns, one after the other.
 //
@@ -172,7 +173,14 @@ struct StepArgs {
 __device__ __forceinline__ double square_of(const PlanArgs &a, const AdamwHeader &h, uint32_t begin, uint32_t end, double *red) {
     const double *parts = parts_of(a, h);
     double s = 0.0;
-    for (uint32_t i = begin + threadIdx.x; i < end; i += kTh) s += parts[i];
+    constexpr int kBatch = 8;   // loads on their way together
+    for (uint32_t i = begin + threadIdx.x; i < end; i += kBatch * kTh) {
+        double v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) v[j] = i + j * kTh < end ? parts[i + j * kTh] : 0.0;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) s += v[j];
+    }
 #pragma unroll
     for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
