@@ -9,9 +9,10 @@
 // that squares and adds the gradients (k_adamw_norm: a wave for each chunk) and, for many chunks, a small one that turns the
 // sums into each group's factors (k_adamw_head).  Bound by memory: 28 bytes an element with fp32 states, 16 with 8-bit ones,
 // 2 more for the bf16 copy, and 4 to read the gradient twice where it is clipped.  10.5 million elements of 15 tensors with
-// the copy and clipping, fp32 states: 14 + 7 + 54 us, the last 5.9 TB/s; 42 million with 8-bit states: 47 + 7 + 130 us, 5.8.
-// (The sum of the squares pays for the step before it, whose results the caches still write back: behind a launch that only
-// reads it takes 29 us, 5.8 TB/s.)
+// the copy and clipping, fp32 states: 8 + 5 + 58 us, the last 5.4 TB/s; 42 million with 8-bit states: 30 + 5 + 128 us, 5.9.
+// Parameters and states pass by once a step, non-temporal both ways: a line that a load has brought into the cache and a store
+// has changed there is written back under the next launch, which was the next step's sum of squares (14 and 47 us then, with
+// 54 and 131 for the step).  The gradients are loaded as usual, and what the sum has read of them may still be there.
 // Sums and factors in one launch, by the workgroup that is the last to finish, took 77 us for the 14 + 7: every workgroup's
 // release of its sum costs some 50 ns, one after the other.
 //
@@ -61,11 +62,13 @@ __device__ __forceinline__ void loaded(T &x) {
     asm volatile("" : "+s"(x));
 }
 
-// A thread's elements: kPer of them, or the first n.
+// A thread's elements: kPer of them, or the first n.  ONCE: not read again soon.
+template <bool ONCE = true>
 __device__ __forceinline__ void load_all(const float *p, int at, float (&x)[kPer]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const f32x4u v = *global<const f32x4u>(p + at + 4 * k);
+        const auto *from = global<const f32x4u>(p + at + 4 * k);
+        const f32x4u v = ONCE ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[4 * k + e] = v[e];
     }
@@ -77,14 +80,14 @@ __device__ __forceinline__ void load_some(const float *p, int at, int n, float (
 __device__ __forceinline__ void store_all(float *p, int at, const float (&x)[kPer]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-        *global<f32x4u>(p + at + 4 * k) = f32x4u{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+        __builtin_nontemporal_store(f32x4u{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]}, global<f32x4u>(p + at + 4 * k));
 }
 __device__ __forceinline__ void store_some(float *p, int at, int n, const float (&x)[kPer]) {
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
         if (e < n) global<float>(p)[at + e] = x[e];
 }
-__device__ __forceinline__ u32x2b load_all(const uint8_t *p, int at) { return *global<const u32x2b>(p + at); }
+__device__ __forceinline__ u32x2b load_all(const uint8_t *p, int at) { return __builtin_nontemporal_load(global<const u32x2b>(p + at)); }
 __device__ __forceinline__ u32x2b load_some(const uint8_t *p, int at, int n) {
     u32x2b v = {0, 0};
 #pragma unroll
@@ -346,7 +349,7 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, StepArgs x) {
         float m[kPer], v[kPer];
         float *pm = static_cast<float *>(k.m), *pv = static_cast<float *>(k.v);
         if (n >= kPer) {
-            load_all(k.grad, at, g);
+            load_all<false>(k.grad, at, g);
             load_all(k.param, at, p);
             load_all(pm, at, m);
             load_all(pv, at, v);
@@ -382,7 +385,7 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, StepArgs x) {
         u32x2b cm, cv;
         float sm = 0.f, sv = 0.f;
         if (n >= kPer) {
-            load_all(k.grad, at, g);
+            load_all<false>(k.grad, at, g);
             load_all(k.param, at, p);
             cm = load_all(pm, at);
             cv = load_all(pv, at);
@@ -450,8 +453,8 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, StepArgs x) {
         else
             codes_of<false>(m, v, scale_m, scale_v, bits, out_m, out_v);
         if (n >= kPer) {
-            *global<u32x2b>(pm + at) = out_m;
-            *global<u32x2b>(pv + at) = out_v;
+            __builtin_nontemporal_store(out_m, global<u32x2b>(pm + at));
+            __builtin_nontemporal_store(out_v, global<u32x2b>(pv + at));
         } else {
             store_some(pm, at, n, out_m);
             store_some(pv, at, n, out_v);
@@ -465,7 +468,7 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, StepArgs x) {
     bf16_bits *work = static_cast<bf16_bits *>(k.work);
     if (n >= kPer) {
         store_all(k.param, at, p);
-        if (work) *global<u32x4h>(work + at) = w;
+        if (work) __builtin_nontemporal_store((u32x4h)w, global<u32x4h>(work + at));
     } else {
         store_some(k.param, at, n, p);
 #pragma unroll
