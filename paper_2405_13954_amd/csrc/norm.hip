@@ -12,8 +12,8 @@
 // next row's vectors are loaded before the current row's sums are known.  The workgroups' sums go to the workspace, and a
 // second launch adds them in order, so that reruns give the same bits.
 //
-// 16,384 rows of 4096 bf16 columns without the mean: forward with residual and statistics 96 us for 537 MB (5.6 TB/s),
-// backward with base and a fifth of the rows masked 83 + 5 us for 483 MB (5.5).  768 columns with the mean: 16 and 20 + 4 us
+// 16,384 rows of 4096 bf16 columns without the mean: forward with residual and statistics 93 us for 537 MB (5.8 TB/s),
+// backward with base and a fifth of the rows masked 79 + 5 us for 483 MB (5.8).  768 columns with the mean: 16 and 20 + 4 us
 // for 91 and 101 MB.
 #include "internal.h"
 #include "vec16.h"
@@ -30,6 +30,7 @@ struct FwdArgs {
     float *mean, *rstd;
     int cols;
     float eps;
+    bool stream;
 };
 
 struct BwdArgs {
@@ -57,10 +58,17 @@ __device__ __forceinline__ u32x4 take(const char *p, int n) {
 
 // The same for a row that another one follows: row strides are whole vectors, so what a partial vector's load brings
 // besides lies between the rows.  first_of drops it where the vector is used, so that the load need not be waited for here.
-template <bool BF16>
+template <bool BF16, bool STREAM>
 __device__ __forceinline__ u32x4 take_inner(const char *p, int n, bool inner) {
-    if (n >= Vec<BF16>::kN || (inner && n > 0)) return ld128(p);
+    if (n >= Vec<BF16>::kN || (inner && n > 0)) return STREAM ? ld128_nt(p) : ld128(p);
     return n > 0 ? Vec<BF16>::load(p, n, kZero4) : kZero4;
+}
+// The NV vectors of a thread: those at lane, lane + TPR, ... of a row of `cols` elements.
+template <bool BF16, int TPR, int NV, bool STREAM>
+__device__ __forceinline__ void take_row(const char *row, int lane, int cols, bool inner, u32x4 (&v)[NV]) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        v[k] = take_inner<BF16, STREAM>(row + (k * TPR + lane) * 16, cols - (k * TPR + lane) * Vec<BF16>::kN, inner);
 }
 
 // The first n elements of v, zeros behind them.
@@ -120,16 +128,16 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
         return;
     }
     const bool inner = row + 1 < a.rows;
-    u32x4 h[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-        h[k] = take_inner<BF16>(x + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN, inner);
+    const char *r = a.res + row * a.ld_r * kEs;
+    u32x4 h[NV], v[NV];
+    if (a.stream) {
+        take_row<BF16, TPR, NV, true>(x, lane, a.cols, inner, h);
+        if (a.res) take_row<BF16, TPR, NV, true>(r, lane, a.cols, inner, v);
+    } else {
+        take_row<BF16, TPR, NV, false>(x, lane, a.cols, inner, h);
+        if (a.res) take_row<BF16, TPR, NV, false>(r, lane, a.cols, inner, v);
+    }
     if (a.res) {
-        const char *r = a.res + row * a.ld_r * kEs;
-        u32x4 v[NV];
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            v[k] = take_inner<BF16>(r + (k * TPR + lane) * 16, a.cols - (k * TPR + lane) * V::kN, inner);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float s[V::kN];
@@ -191,7 +199,7 @@ struct RowPart {
     bool live;
 };
 
-template <bool BF16, int TPR, int NV, bool CENTER>
+template <bool BF16, int TPR, int NV, bool CENTER, bool STREAM>
 __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
     using V = Vec<BF16>;
     constexpr int kTh = TPR < 512 ? 512 : TPR, kTeams = kTh / TPR, kEs = BF16 ? 2 : 4, kW = TPR > 64 ? TPR / 64 : 1;
@@ -232,22 +240,14 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
         p.rstd = p.live ? a.rstd[row] : 0.f;
         const int width = p.live ? a.cols : 0;
         const bool inner = row + 1 < a.rows;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int i = k * TPR + lane;
-            p.h[k] = take_inner<BF16>(a.h + row * a.ld_h * kEs + i * 16, width - i * V::kN, inner);
-            p.dy[k] = take_inner<BF16>(a.dy + row * a.ld_dy * kEs + i * 16, width - i * V::kN, inner);
-        }
+        take_row<BF16, TPR, NV, STREAM>(a.h + row * a.ld_h * kEs, lane, width, inner, p.h);
+        take_row<BF16, TPR, NV, STREAM>(a.dy + row * a.ld_dy * kEs, lane, width, inner, p.dy);
     };
-    u32x4 base[NV], next_base[kTight ? 1 : NV];
-    const auto load_base = [&](int64_t row, u32x4 *to) {
+    u32x4 base[NV], next_base[NV];
+    const auto load_base = [&](int64_t row, u32x4 (&to)[NV]) {
         const int width = row < a.rows && a.base ? a.cols : 0;
         const bool inner = row + 1 < a.rows;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int i = k * TPR + lane;
-            to[k] = take_inner<BF16>(a.base + row * a.ld_b * kEs + i * 16, width - i * V::kN, inner);
-        }
+        take_row<BF16, TPR, NV, STREAM>(a.base + row * a.ld_b * kEs, lane, width, inner, to);
     };
     const int64_t rounds = (a.rows + stride - 1) / stride;   // the same for the whole workgroup: there are barriers inside
     int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team;
@@ -417,6 +417,14 @@ void with_team(int vectors, const Go &go) {
     if constexpr (MOST >= 4) go(int_c<TEAM>{}, int_c<4>{});
 }
 
+// Whether a call's matrices are more than the 256 MB cache holds.  Then the loads are non-temporal, as the stores always are:
+// nothing of what they would bring into the cache is read there again.  us of the first launch with and without: 16,384 rows
+// of 4096 bf16 columns forward 93 and 96, backward 79 and 83; of 768 columns, 91 and 101 MB and the next call on the same
+// memory soon, 20.7 and 16, 21.2 and 19.3.
+bool beyond_cache(bool bf16, int64_t rows, int cols, int matrices) {
+    return static_cast<double>(rows) * cols * (bf16 ? 2 : 4) * matrices > 256.0 * (1 << 20);
+}
+
 int vectors_of(bool bf16, int cols) { return (cols + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4); }
 
 // Workgroups of the backward pass: one on each CU, as many as there are rows for.  us with 160, 256, 512 and 768 (base, no
@@ -435,7 +443,8 @@ size_t norm_ws_bytes(int64_t rows, int cols) {
 hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
     FwdArgs a = {static_cast<const char *>(n.x), static_cast<const char *>(n.residual), static_cast<char *>(n.h),
                  static_cast<char *>(n.y), n.ld_x, n.ld_res, n.ld_h, n.ld_y, n.rows, n.mask,
-                 static_cast<const char *>(n.gain), static_cast<const char *>(n.bias), n.mean, n.rstd, n.cols, n.eps};
+                 static_cast<const char *>(n.gain), static_cast<const char *>(n.bias), n.mean, n.rstd, n.cols, n.eps,
+                 beyond_cache(n.bf16, n.rows, n.cols, 2 + (n.residual ? 1 : 0) + (n.h ? 1 : 0))};
     const int vec = vectors_of(n.bf16, n.cols);
     const auto go = [&](auto t, auto v) {
         constexpr int T = decltype(t)::value, NV = decltype(v)::value;
@@ -472,7 +481,14 @@ hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s) {
         const BwdArgs a = {static_cast<const char *>(n.h), static_cast<const char *>(n.dy), static_cast<const char *>(n.base),
                            static_cast<char *>(n.dx), n.ld_h, n.ld_dy, n.ld_base, n.ld_dx, n.rows, n.mask,
                            static_cast<const char *>(n.gain), n.mean, n.rstd, part_g, part_b, n.cols};
-        n.rms ? k_norm_bwd<B, T, NV, false><<<groups, th, 0, s>>>(a) : k_norm_bwd<B, T, NV, true><<<groups, th, 0, s>>>(a);
+        const auto run = [&](auto stream) {
+            constexpr bool S = decltype(stream)::value;
+            n.rms ? k_norm_bwd<B, T, NV, false, S><<<groups, th, 0, s>>>(a) : k_norm_bwd<B, T, NV, true, S><<<groups, th, 0, s>>>(a);
+        };
+        if (beyond_cache(n.bf16, n.rows, n.cols, 2 + (n.base ? 1 : 0) + (n.dx ? 1 : 0)))
+            run(std::true_type{});
+        else
+            run(std::false_type{});
     };
     const auto go = [&](auto t, auto v) { n.bf16 ? launch(t, v, std::true_type{}) : launch(t, v, std::false_type{}); };
     if (n.rows > 0) {
