@@ -9,7 +9,7 @@
 // sum of exponentials of ranges of each row, k_pair_sums joins them, adds up each sequence (in float64: the ratio is a
 // small difference of large sums) and leaves two factors for every row, and k_pair_grad writes the gradient.  The second
 // pass takes the rows from the last to the first, so that those that the 256 MB cache still holds are read from there.
-// 2,048 tokens of 128,000 bf16 logits, 0.3 of them masked: 67 + 6 + 130 us for 367, 0 and 891 MB (5.5 and 6.9 TB/s; a copy
+// 2,048 tokens of 128,000 bf16 logits, 0.3 of them masked: 68 + 6 + 126 us for 367, 0 and 891 MB (5.4 and 7.1 TB/s; a copy
 // inside the cache reaches 7.2).
 #include "internal.h"
 #include "vec16.h"
@@ -46,15 +46,17 @@ __device__ __forceinline__ bool counts(const PairArgs &a, int64_t row, int64_t t
     return (t >= 0) & (t < a.vocab) & (row >= first) & (row < last);   // (the loads wait together)
 }
 
+// Workgroups that take parts of rows: the part in x, the row in y and z.
+__device__ __forceinline__ int64_t row_of() { return blockIdx.y + static_cast<int64_t>(gridDim.y) * blockIdx.z; }
+
 template <bool BF16>
 __global__ __launch_bounds__(kTh) void k_pair_stats(PairArgs a) {
     using V = Vec<BF16>;
     constexpr int kEs = BF16 ? 2 : 4, kGroup = 4;
     constexpr float kNone = -__builtin_inff();
     __shared__ float red[kTh / 64];
-    const int64_t at = blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y;
-    const int64_t row = at / a.splits;
-    const int split = static_cast<int>(at - row * a.splits), tid = static_cast<int>(threadIdx.x);
+    const int64_t row = row_of();
+    const int split = static_cast<int>(blockIdx.x), tid = static_cast<int>(threadIdx.x);
     if (row >= a.rows) return;
     if (split == 0 && tid == 0) a.row[row] = {0.f, 0.f, 0.f, 0.f};   // no gradient, until k_pair_sums says more
     const int64_t t = a.target[row];
@@ -201,15 +203,16 @@ __global__ __launch_bounds__(kSumTh) void k_pair_sums(PairArgs a, const float *r
     }
 }
 
-// A workgroup writes kGroup x kTh vectors of one row.
+// A workgroup writes kGroup x kTh vectors of one row.  us with two, four and eight vectors a thread: 2,048 rows of 128,000
+// bf16 logits 127, 131 and 129, 2,041 rows of 50,257 54, 55 and 65.
+constexpr int kGroup = 2;
 template <bool BF16>
-__global__ __launch_bounds__(kTh) void k_pair_grad(PairArgs a, char *dlogits, int64_t ld_d, int pieces) {
+__global__ __launch_bounds__(kTh) void k_pair_grad(PairArgs a, char *dlogits, int64_t ld_d) {
     using V = Vec<BF16>;
-    constexpr int kEs = BF16 ? 2 : 4, kGroup = 4;
-    const int64_t at = blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y, back = at / pieces;
-    if (back >= a.rows) return;
-    const int64_t row = a.rows - 1 - back;
-    const int first = static_cast<int>(at - back * pieces) * kGroup * kTh + static_cast<int>(threadIdx.x);
+    constexpr int kEs = BF16 ? 2 : 4;
+    const int64_t row = a.rows - 1 - row_of();
+    if (row < 0) return;
+    const int first = static_cast<int>(blockIdx.x) * kGroup * kTh + static_cast<int>(threadIdx.x);
     const char *z = a.logits + row * a.ld * kEs;
     char *dz = dlogits + row * ld_d * kEs;
     const Row r = a.row[row];
@@ -254,9 +257,9 @@ __global__ __launch_bounds__(kTh) void k_pair_grad(PairArgs a, char *dlogits, in
     }
 }
 
-dim3 grid_of(int64_t groups) {
-    const uint32_t gx = static_cast<uint32_t>(groups < (1 << 21) ? groups : (1 << 21));
-    return dim3(gx, static_cast<uint32_t>((groups + gx - 1) / gx));
+dim3 grid_of(int parts, int64_t rows) {
+    const int64_t z = (rows + 65534) / 65535;
+    return dim3(static_cast<uint32_t>(parts), static_cast<uint32_t>((rows + z - 1) / z), static_cast<uint32_t>(z));
 }
 
 }  // namespace
@@ -281,11 +284,12 @@ hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s) {
                   reinterpret_cast<Row *>(ws + align256(p.rows * kMaxSplits * sizeof(float2)) + align256(p.rows * sizeof(float))),
                   p.vocab, splits, p.pairs};
     if (p.rows > 0) {
-        const dim3 grid = grid_of(p.rows * splits);
+        const dim3 grid = grid_of(splits, p.rows);
         p.bf16 ? k_pair_stats<true><<<grid, kTh, 0, s>>>(a) : k_pair_stats<false><<<grid, kTh, 0, s>>>(a);
     }
     const auto sums = [&](auto kernel, int threads) {
-        kernel<<<grid_of(p.pairs), threads, 0, s>>>(a, p.ref, p.weight, p.beta, p.smoothing, p.loss, p.logp);
+        const int64_t gx = p.pairs < (1 << 21) ? p.pairs : (1 << 21);
+        kernel<<<dim3(static_cast<uint32_t>(gx), static_cast<uint32_t>((p.pairs + gx - 1) / gx)), threads, 0, s>>>(a, p.ref, p.weight, p.beta, p.smoothing, p.loss, p.logp);
     };
     // 256 threads where most sequences have no more rows: 32 pairs in 2,041 rows 5.7 us against 6.1 with 1024, 8 pairs in
     // 2,048 rows 7.4 against 6.4.
@@ -294,11 +298,9 @@ hipError_t launch_preference_loss(const PreferenceLoss &p, hipStream_t s) {
     else
         sums(k_pair_sums<1024>, 1024);
     if (p.dlogits && p.rows > 0) {
-        const int pieces = (vec + 4 * kTh - 1) / (4 * kTh);
-        const dim3 grid = grid_of(p.rows * pieces);
+        const dim3 grid = grid_of((vec + kGroup * kTh - 1) / (kGroup * kTh), p.rows);
         char *dz = static_cast<char *>(p.dlogits);
-        p.bf16 ? k_pair_grad<true><<<grid, kTh, 0, s>>>(a, dz, p.ld_d, pieces)
-               : k_pair_grad<false><<<grid, kTh, 0, s>>>(a, dz, p.ld_d, pieces);
+        p.bf16 ? k_pair_grad<true><<<grid, kTh, 0, s>>>(a, dz, p.ld_d) : k_pair_grad<false><<<grid, kTh, 0, s>>>(a, dz, p.ld_d);
     }
     return hipGetLastError();
 }
