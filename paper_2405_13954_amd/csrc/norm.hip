@@ -305,7 +305,8 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
                 s2 += r[1][team * kW + w];
             }
         }
-        // dx - base = rstd (c - avg(c) - xh avg(c xh)) = rstd c + (h - mean) along + level.  (A masked row has zeros in all.)
+        // dx - base = rstd (c - avg(c) - xh avg(c xh)) = rstd c + (h - mean) along + level.  (A masked row has zeros in all, whose
+        // products with a gain that is not finite are dropped.)
         // The sum comes first: it is as small as rstd is large, so that the product of a row without variance stays finite.
         const float level = -cur.rstd * (s1 * per), along = -(s2 * per) * cur.rstd * cur.rstd * cur.rstd;
         if (a.dx && row < a.rows) {
@@ -319,7 +320,8 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
                 for (int e = 0; e < V::kN; ++e) {
                     const float c = V::get(cur.dy[k], e) * g[e];
                     const float d = CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e);
-                    o[e] = V::get(base[k], e) + fmaf(c, cur.rstd, fmaf(d, along, level));
+                    const float to = V::get(base[k], e);
+                    o[e] = cur.live ? to + fmaf(c, cur.rstd, fmaf(d, along, level)) : to;
                 }
                 V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
             }

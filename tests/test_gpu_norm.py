@@ -296,6 +296,29 @@ def test_nan_stays_in_its_row():
     assert torch.isnan(dgain).nonzero().flatten().tolist() == [7] and torch.isnan(dbias).nonzero().flatten().tolist() == [7]
 
 
+@pytest.mark.parametrize("cols", [72, 2048, 8200, 12296])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masked_rows_under_a_gain_that_is_not_finite(dtype, cols):
+    import torch
+    import paper_2405_13954_amd as P
+    g = torch.Generator().manual_seed(cols)
+    h, dy, base = (torch.randn(6, cols, generator=g).to(dt(dtype)).cuda() for _ in range(3))
+    gain = torch.ones(cols, dtype=dt(dtype), device="cuda")
+    gain[3], gain[cols - 2] = float("nan"), float("inf")
+    mask = torch.tensor([1, 0, 1, 0, 0, 1], dtype=torch.uint8, device="cuda")
+    off = mask == 0
+    y, dx, mean, rstd, dgain, dbias = torch.empty_like(h), torch.empty_like(h), f32(6), f32(6), f32(cols), f32(cols)
+    P.logra_layer_norm_forward(h, y, gain=gain, mask=mask, mean=mean, rstd=rstd)
+    assert not y[off].any() and bool(torch.isnan(y[~off][:, 3]).all())
+    for rms in (False, True):
+        args = dict(mean=None if rms else mean, gain=gain, rms=rms, mask=mask, dgain=dgain, dbias=None if rms else dbias)
+        P.logra_layer_norm_backward(h, dy, rstd, dx=dx, base=base, **args)
+        assert torch.equal(dx[off], base[off]) and bool(torch.isnan(dx[~off]).all())
+        assert bool(torch.isfinite(dgain).all()) and bool(torch.isfinite(dbias).all())   # (no gain in them)
+        P.logra_layer_norm_backward(h, dy, rstd, dx=dx, **args)
+        assert not dx[off].any() and bool(torch.isnan(dx[~off]).all())
+
+
 @pytest.mark.parametrize("rms", [False, True])
 def test_gradients_against_differences(rms):
     # sum(y dy) along a direction e of h, with a step of 2^-8 in fp32: y's third derivatives along e are below 40 |e|^3
