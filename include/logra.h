@@ -647,8 +647,8 @@ int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, in
  *            h, so of x and of residual alike; base is what reaches h otherwise.
  *            dx may be h, dy or base, with its stride, and shares no memory with
  *            inputs otherwise (refused)
- *   mask     rows with 0: h, dy and the statistics are not read, dx = base, and
- *            they add nothing to dgain and dbias
+ *   mask     rows with 0: whatever h, dy and the statistics hold there, dx = base,
+ *            and they add nothing to dgain and dbias
  *   mean, rstd  as the forward call left them (mean NULL with rms)
  *   dgain, dbias  device fp32 [cols] or NULL; accumulate 0: overwritten, 1: added to
  *   ws       logra_layer_norm_ws_size bytes, 256-byte aligned, where dgain or dbias

@@ -10,7 +10,7 @@
 //
 // Backward: a workgroup walks rows a grid apart and keeps the sums for dgain and dbias of its columns in registers; the
 // next row's vectors are loaded before the current row's sums are known.  The workgroups' sums go to the workspace, and a
-// second launch adds them in order, so that reruns give the same bits.
+// second launch adds them in order, so that reruns give the same bits.  Few rows: one launch (k_norm_bwd_few).
 //
 // 16,384 rows of 4096 bf16 columns without the mean: forward with residual and statistics 93 us for 537 MB (5.8 TB/s),
 // backward with base and a fifth of the rows masked 79 + 5 us for 483 MB (5.8).  768 columns with the mean: 16 and 20 + 4 us
@@ -99,6 +99,31 @@ __device__ __forceinline__ float team_sum(float v, float *red) {
         for (int w = 1; w < TPR / 64; ++w) v += red[w];
     }
     return v;
+}
+
+// The backward pass's two sums (CENTER: both) over a row's team.  red: a slot of each for every wave of the workgroup.
+template <int TPR, bool CENTER, int WAVES>
+__device__ __forceinline__ void team_sums(float &s1, float &s2, float (&red)[2][WAVES], int team) {
+    constexpr int kW = TPR > 64 ? TPR / 64 : 1;
+#pragma unroll
+    for (int m = (TPR < 64 ? TPR : 64) / 2; m; m >>= 1) {
+        s2 += __shfl_xor(s2, m);
+        if constexpr (CENTER) s1 += __shfl_xor(s1, m);
+    }
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) {
+            red[0][threadIdx.x >> 6] = s1;
+            red[1][threadIdx.x >> 6] = s2;
+        }
+        __syncthreads();
+        s1 = 0.f;
+        s2 = 0.f;
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+            if constexpr (CENTER) s1 += red[0][team * kW + w];
+            s2 += red[1][team * kW + w];
+        }
+    }
 }
 
 template <bool BF16, int TPR, int NV, bool CENTER>
@@ -202,7 +227,7 @@ struct RowPart {
 template <bool BF16, int TPR, int NV, bool CENTER, bool STREAM>
 __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
     using V = Vec<BF16>;
-    constexpr int kTh = TPR < 512 ? 512 : TPR, kTeams = kTh / TPR, kEs = BF16 ? 2 : 4, kW = TPR > 64 ? TPR / 64 : 1;
+    constexpr int kTh = TPR < 512 ? 512 : TPR, kTeams = kTh / TPR, kEs = BF16 ? 2 : 4;
     constexpr int kCols = TPR * NV * V::kN;
     // What registers are kept for: up to 24 columns of a thread, the next row and the gain in fp32; from 32 on the gain waits
     // in LDS, base is not loaded ahead, and the packed row is unpacked again for dx; a workgroup of 1024 threads loads no row
@@ -285,26 +310,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
             }
             if constexpr (kTight) asm volatile("" : "+v"(cur.h[k]), "+v"(cur.dy[k]));   // not its fp32 values are kept
         }
-#pragma unroll
-        for (int m = (TPR < 64 ? TPR : 64) / 2; m; m >>= 1) {
-            s2 += __shfl_xor(s2, m);
-            if constexpr (CENTER) s1 += __shfl_xor(s1, m);
-        }
-        if constexpr (TPR > 64) {
-            float(&r)[2][kTh / 64] = red[it & 1];   // the other half may still be read by a slower wave
-            if ((threadIdx.x & 63) == 0) {
-                r[0][threadIdx.x >> 6] = s1;
-                r[1][threadIdx.x >> 6] = s2;
-            }
-            __syncthreads();
-            s1 = 0.f;
-            s2 = 0.f;
-#pragma unroll
-            for (int w = 0; w < kW; ++w) {
-                if constexpr (CENTER) s1 += r[0][team * kW + w];
-                s2 += r[1][team * kW + w];
-            }
-        }
+        team_sums<TPR, CENTER>(s1, s2, red[it & 1], team);   // (the other half may still be read by a slower wave)
         // dx - base = rstd (c - avg(c) - xh avg(c xh)) = rstd c + (h - mean) along + level.  (A masked row has zeros in all, whose
         // products with a gain that is not finite are dropped.)
         // The sum comes first: it is as small as rstd is large, so that the product of a row without variance stays finite.
@@ -362,6 +368,136 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
     };
     write(dg, a.part_g);
     if constexpr (CENTER) write(db, a.part_b);
+}
+
+// The same for few rows in one launch: the first `column_groups` workgroups sum dgain and dbias of their columns over all rows,
+// which needs the statistics but no row's sums, and the others' teams take one row each for dx.  h and dy are read twice, and
+// the second launch and its wait are saved.
+//
+// Threads of a workgroup and vectors of a row (64 or 128 bytes) that it sums.  us of 512 rows with 128 threads and four, 512
+// and four, 512 and eight, 1024 and eight: 768 bf16 columns 7.4, 4.3, 5.6, 5.2; 4096 columns 12.0, 7.6, 7.9, 7.2; of 4096 fp32
+// columns with 1024 threads and two, four, eight vectors: 26.9, 15.0, 10.5.
+constexpr int few_threads(int team) { return team < 512 ? 512 : team; }
+constexpr int few_vecs(int team) { return team < 1024 ? 4 : 8; }
+template <bool BF16, int TH, int VECS, bool CENTER>
+__device__ void sum_columns(const BwdArgs &a, float *dgain, float *dbias, bool accumulate) {
+    using V = Vec<BF16>;
+    constexpr int kEs = BF16 ? 2 : 4, kSlots = TH / VECS, kAhead = 4, kC = VECS * V::kN, kParts = 8;
+    static_assert(TH / kC >= kParts, "a thread for every column and part");
+    __shared__ __attribute__((aligned(16))) float sums[kSlots][kC + 4];
+    __shared__ float joined[kParts][kC];
+    const int tid = static_cast<int>(threadIdx.x), slot = tid / VECS, mine = tid % VECS;
+    const int i = static_cast<int>(blockIdx.x) * VECS + mine, n = a.cols - i * V::kN;
+    float dg[V::kN] = {}, db[V::kN] = {};
+    const auto add = [&](u32x4 h, u32x4 dy, float mean, float rstd, bool live) {   // what a masked row holds is dropped
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) {
+            const float g = V::get(dy, e), d = CENTER ? V::get(h, e) - mean : V::get(h, e);
+            dg[e] = live ? fmaf(g, d * rstd, dg[e]) : dg[e];
+            if constexpr (CENTER) db[e] += live ? g : 0.f;
+        }
+    };
+    // A partial vector's load brings what lies between the rows besides, for columns that are not stored; behind the last row
+    // nothing may lie.
+    const char *h_at = a.h + i * 16, *dy_at = a.dy + i * 16;
+    const int last = static_cast<int>(a.rows) - 1, whole = n >= V::kN ? last + 1 : n > 0 ? last : 0;
+    for (int first = slot; first < whole; first += kAhead * kSlots) {
+        u32x4 h[kAhead], dy[kAhead];
+        float mean[kAhead], rstd[kAhead];
+        uint8_t mask[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int64_t row = first + j * kSlots < whole ? first + j * kSlots : first;
+            h[j] = ld128(h_at + row * a.ld_h * kEs);
+            dy[j] = ld128(dy_at + row * a.ld_dy * kEs);
+            mean[j] = CENTER ? a.mean[row] : 0.f;
+            rstd[j] = a.rstd[row];
+            mask[j] = a.mask ? a.mask[row] : 1;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) add(h[j], dy[j], mean[j], rstd[j], first + j * kSlots < whole && mask[j] != 0);
+    }
+    if (n > 0 && n < V::kN && slot == last % kSlots)
+        add(take<BF16>(h_at + last * a.ld_h * kEs, n), take<BF16>(dy_at + last * a.ld_dy * kEs, n),
+            CENTER ? a.mean[last] : 0.f, a.rstd[last], !a.mask || a.mask[last] != 0);
+    const auto write = [&](const float (&sum)[V::kN], float *out) {
+        if (!out) return;   // (the same for the whole workgroup)
+#pragma unroll
+        for (int e = 0; e < V::kN; e += 4)
+            *reinterpret_cast<f32x4 *>(&sums[slot][mine * V::kN + e]) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+        __syncthreads();
+        const int c = tid % kC, part = tid / kC;
+        if (part < kParts) {
+            float t = 0.f;
+#pragma unroll
+            for (int k = 0; k < kSlots / kParts; ++k) t += sums[part * (kSlots / kParts) + k][c];
+            joined[part][c] = t;
+        }
+        __syncthreads();
+        const int column = static_cast<int>(blockIdx.x) * kC + c;
+        if (part == 0 && column < a.cols) {
+            float t = joined[0][c];
+#pragma unroll
+            for (int k = 1; k < kParts; ++k) t += joined[k][c];
+            out[column] = accumulate ? out[column] + t : t;
+        }
+        __syncthreads();   // `sums` and `joined` are used again
+    };
+    write(dg, dgain);
+    if constexpr (CENTER) write(db, dbias);
+}
+
+template <bool BF16, int TPR, int NV, bool CENTER>
+__global__ __launch_bounds__(few_threads(TPR)) void k_norm_bwd_few(BwdArgs a, float *dgain, float *dbias, bool accumulate,
+                                                                   int column_groups) {
+    using V = Vec<BF16>;
+    constexpr int kTh = few_threads(TPR), kTeams = kTh / TPR, kEs = BF16 ? 2 : 4;
+    if (static_cast<int>(blockIdx.x) < column_groups) return sum_columns<BF16, kTh, few_vecs(TPR), CENTER>(a, dgain, dbias, accumulate);
+    __shared__ float red[2][kTh / 64];
+    const int lane = static_cast<int>(threadIdx.x) % TPR;
+    const int64_t row = static_cast<int64_t>(static_cast<int>(blockIdx.x) - column_groups) * kTeams + threadIdx.x / TPR;
+    const bool in = row < a.rows, inner = row + 1 < a.rows, live = in && (!a.mask || a.mask[row] != 0);
+    const int width = live ? a.cols : 0;
+    u32x4 h[NV], dy[NV], base[NV], gain[NV];
+    take_row<BF16, TPR, NV, false>(a.h + row * a.ld_h * kEs, lane, width, inner, h);
+    take_row<BF16, TPR, NV, false>(a.dy + row * a.ld_dy * kEs, lane, width, inner, dy);
+    take_row<BF16, TPR, NV, false>(a.base + row * a.ld_b * kEs, lane, in && a.base ? a.cols : 0, inner, base);
+    const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int i = k * TPR + lane;
+        gain[k] = a.gain ? take<BF16>(a.gain + i * 16, a.cols - i * V::kN) : V::pack(ones);
+    }
+    const float mean = CENTER && live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int n = a.cols - (k * TPR + lane) * V::kN;
+        h[k] = first_of<BF16>(h[k], n);
+        dy[k] = first_of<BF16>(dy[k], n);
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) {
+            const float c = V::get(dy[k], e) * V::get(gain[k], e);
+            if constexpr (CENTER) s1 += c;
+            s2 = fmaf(c, V::get(h[k], e) - mean, s2);
+        }
+    }
+    team_sums<TPR, CENTER>(s1, s2, red, static_cast<int>(threadIdx.x) / TPR);
+    const float per = 1.f / static_cast<float>(a.cols);
+    const float level = -rstd * (s1 * per), along = -(s2 * per) * rstd * rstd * rstd;   // as in k_norm_bwd
+    if (!in) return;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int i = k * TPR + lane, n = a.cols - i * V::kN;
+        if (n <= 0) continue;
+        float o[V::kN];
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) {
+            const float c = V::get(dy[k], e) * V::get(gain[k], e), to = V::get(base[k], e);
+            o[e] = live ? to + fmaf(c, rstd, fmaf(V::get(h[k], e) - mean, along, level)) : to;
+        }
+        V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
+    }
 }
 
 // dgain and dbias from the workgroups' sums: a workgroup takes 32 columns, eight threads of four for each of 32 ranges of
@@ -434,6 +570,12 @@ int vectors_of(bool bf16, int cols) { return (cols + (bf16 ? 7 : 3)) / (bf16 ? 8
 // 12.9 and 12.9, 16,384 rows of 768 22.8, 20.6, 21.8 and 27.4.
 constexpr int kBwdGroups = 256;
 
+// Up to so many rows k_norm_bwd_few takes the backward pass.  us of a pass with it and with k_norm_bwd and k_norm_parts, of
+// 16, 512, 1,024 and 2,048 rows: 768 bf16 columns with the mean 3.7 and 8.1, 4.3 and 8.4, 7.6 and 8.6, 13.5 and 9.3; 4096 rms
+// 3.3 and 6.7, 7.6 and 9.3, 12.0 and 11.3, 20.6 and 15.7; 14,336 rms 4.5 and 14.5, 16.3 and 26.4, 30.4 and 37.4, 62 and 60.
+// A launch less is also 2.6 us less of the host's time.
+constexpr int kFewRows = 1024;
+
 }  // namespace
 
 size_t norm_ws_bytes(int64_t rows, int cols) {
@@ -468,7 +610,45 @@ hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
     return hipGetLastError();
 }
 
+// One launch, or, where dx takes the place of what the columns' sums read, one for these before it.
+static hipError_t launch_few(const NormBackward &n, hipStream_t s) {
+    const int vec = vectors_of(n.bf16, n.cols);
+    const BwdArgs a = {static_cast<const char *>(n.h), static_cast<const char *>(n.dy), static_cast<const char *>(n.base),
+                       static_cast<char *>(n.dx), n.ld_h, n.ld_dy, n.ld_base, n.ld_dx, n.rows, n.mask,
+                       static_cast<const char *>(n.gain), n.mean, n.rstd, nullptr, nullptr, n.cols};
+    const bool sums = n.dgain || n.dbias, apart = sums && n.dx && (n.dx == n.h || n.dx == n.dy);
+    const auto launch = [&](auto t, auto v, auto is_bf16) {
+        constexpr int T = decltype(t)::value, NV = decltype(v)::value, th = few_threads(T), teams = th / T;
+        constexpr bool B = decltype(is_bf16)::value;
+        const int rows = n.dx ? (static_cast<int>(n.rows) + teams - 1) / teams : 0;
+        const int columns = sums ? (vec + few_vecs(T) - 1) / few_vecs(T) : 0;
+        const auto run = [&](int groups, int column_groups) {
+            if (n.rms)
+                k_norm_bwd_few<B, T, NV, false><<<groups, th, 0, s>>>(a, n.dgain, n.dbias, n.accumulate, column_groups);
+            else
+                k_norm_bwd_few<B, T, NV, true><<<groups, th, 0, s>>>(a, n.dgain, n.dbias, n.accumulate, column_groups);
+        };
+        if (apart) {
+            run(columns, columns);
+            run(rows, 0);
+        } else {
+            run(columns + rows, columns);
+        }
+    };
+    const auto go = [&](auto t, auto v) { n.bf16 ? launch(t, v, std::true_type{}) : launch(t, v, std::false_type{}); };
+    if (vec <= 1024)
+        with_team<1, 1024>(vec, go);
+    else if (vec <= 2 * 1024)
+        go(int_c<1024>{}, int_c<2>{});
+    else if (vec <= 3 * 1024)   // (fp32)
+        launch(int_c<1024>{}, int_c<3>{}, std::false_type{});
+    else
+        launch(int_c<1024>{}, int_c<4>{}, std::false_type{});
+    return hipGetLastError();
+}
+
 hipError_t launch_norm_backward(const NormBackward &n, hipStream_t s) {
+    if (n.rows > 0 && n.rows <= kFewRows) return launch_few(n, s);
     const int vec = vectors_of(n.bf16, n.cols);
     int groups = 0;   // (without rows: the gradients' sums are empty)
     float *part_g = nullptr, *part_b = nullptr;

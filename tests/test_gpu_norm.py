@@ -4,8 +4,8 @@ Tolerances count roundings of u = 2^-24.  A sum over a row is at most 64 additio
 between waves, and its terms have a few roundings each: 95 u of the terms' magnitudes (`ROW`).  So, forward: mean within
 ROW avg|h| (em); the variance within its own ROW and 3 em^2 (the difference of means enters squared); rstd by half of that,
 relative, and 4 u; y by its terms.  Backward, from exact statistics: xh and c carry 2 u and u, their averages ROW, and dgain and dbias are
-sums of at most rows / 512 + 1 additions in a thread, 16 between teams, 512 / 16 + 16 between workgroups (`ROWS`).  Then
-one rounding to the output's type.
+sums of at most rows / 512 + 1 additions in a thread, 16 between teams, 512 / 16 + 16 between workgroups (`ROWS`); of up to 1,024 rows
+8 in a thread, 16 and 8 between threads.  Then one rounding to the output's type.
 """
 import numpy as np
 import pytest
@@ -223,6 +223,13 @@ def check_backward(rows, cols, dtype, rms, base, mask_share=0.0, extra=0, affine
 def test_backward_widths(cols, dtype):
     check_backward(5, cols, dtype, False, True, mask_share=0.3)
     check_backward(3, cols, dtype, True, False, extra=24)
+
+
+# (more rows than one launch takes)
+@pytest.mark.parametrize("dtype,cols", [("bf16", c) for c in (1, 33, 257, 520, 1001, 2049, 4104, 8200, 12289, 16384)] +
+                         [("f32", c) for c in (3, 129, 513, 1001, 2049, 4100, 6145, 8193, 12289, 16381)])
+def test_backward_widths_of_many_rows(cols, dtype):
+    check_backward(1030, cols, dtype, cols % 2 == 0, True, mask_share=0.3, extra=8)
 
 
 @pytest.mark.parametrize("rows", [1, 2, 17, 511, 513, 1025, 9000])
