@@ -102,6 +102,22 @@ def test_rows_and_pairs(rows, n, vocab):
         check(z, z64, target, offsets, dtype, ref=ref, weight=g.uniform(0.5, 2, n).astype(np.float32), beta=0.05, smoothing=0.3)
 
 
+# on either side of the limits of the form for few rows: pairs, rows a pair, the gradient's workgroups (1,536 rows in one
+# piece each, 40 rows in 39)
+@pytest.mark.parametrize("rows,n,vocab", [(1, 1, 9), (40, 127, 300), (40, 128, 300), (256, 2, 130), (257, 2, 130),
+                                          (1536, 20, 520), (1537, 20, 520), (39, 3, 159700), (40, 3, 159700)])
+def test_few_rows_and_more(rows, n, vocab):
+    g = np.random.default_rng([rows, n])
+    z, z64, _ = mk(g, rows, vocab, 2.0, "bf16", 8)
+    target = np.where(g.random(rows) < 0.3, vocab, g.integers(0, vocab, rows))
+    ref = (g.standard_normal(2 * n) * 3).astype(np.float32)
+    weight = np.where(g.random(n) < 0.2, 0.0, g.uniform(0.5, 2, n)).astype(np.float32)
+    check(z, z64, target, ragged(g, rows, n, min(1, rows // 3)), "bf16", ref=ref, weight=weight, smoothing=0.1)
+    if vocab < 1000:   # all rows in one sequence, the others empty; then in place of the logits
+        for s in (0, 2 * n - 1):
+            check(z, z64, target, [0] * (s + 1) + [rows] * (2 * n - s), "bf16", ref=ref, inplace=s > 0)
+
+
 @pytest.mark.parametrize("smoothing", [0.0, 1.0])
 def test_far_ratios(smoothing):
     # d of thousands: the loss is linear on one side and zero on the other, with no overflow
@@ -250,13 +266,14 @@ def test_one_pair_against_the_token_loss():
     within(host(logp), -np.array([host(loss)[:4].sum() * 4, -host(loss)[4:].sum() * 4]), 6 * 4 * 20 * (2.0 ** -20 + 1000 * 2.0 ** -24), "logp")
 
 
-def test_reruns_streams_and_graphs():
+@pytest.mark.parametrize("rows", [300, 150])
+def test_reruns_streams_and_graphs(rows):
     import torch
     import paper_2405_13954_amd as P
-    z = torch.randn(300, 9000, device="cuda").to(torch.bfloat16)
-    t, o = torch.randint(0, 9000, (300,), device="cuda"), torch.tensor([0, 40, 100, 200, 300]).cuda()
+    z = torch.randn(rows, 9000, device="cuda").to(torch.bfloat16)
+    t, o = torch.randint(0, 9000, (rows,), device="cuda"), torch.tensor([0, 40, 100, 120, rows]).cuda()
     d, loss, logp = torch.empty_like(z), f32(2), f32(4)
-    ws = torch.empty(P.logra_preference_loss_ws_size(300, 2), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(P.logra_preference_loss_ws_size(rows, 2), dtype=torch.uint8, device="cuda")
 
     def step(ws=ws):
         P.logra_preference_loss(z, t, o, logp, loss=loss, dlogits=d, ws=ws)
