@@ -102,8 +102,8 @@ __device__ __forceinline__ void store_some(uint8_t *p, int at, int n, u32x2b v) 
 }
 
 // Up to so many chunks every workgroup adds its group's sums up itself, while its elements are on their way, instead of a
-// launch between.  us a step without and with: 20 chunks of 4 groups 10.2 and 8.0, 128 of 64 groups 9.8 and 7.8, 512 of 8
-// groups 15.2 and 13.3, 1,024 of 16 groups 19.5 and 18.4.
+// launch between.  us a step without and with, fp32 and 8-bit states: 76 chunks of one group 9.6 and 8.3, 12.1 and 10.5, 608
+// of 8 groups 17.2 and 13.4, 15.4 and 14.4, 1,216 of 16 groups 24.4 and 22.0, 19.5 and 21.6.
 constexpr uint32_t kJoinChunks = 1024;
 
 // What the kernels find at fixed places of the plan's memory, whatever it holds; `room` chunks lie within it.
@@ -172,17 +172,29 @@ struct StepArgs {
     float *norms;
 };
 
-// A group's sum of squares, from its chunks' in order: the same in every thread.  red: a workgroup's.
-__device__ __forceinline__ double square_of(const PlanArgs &a, const AdamwHeader &h, uint32_t begin, uint32_t end, double *red) {
+// A group's sum of squares, from its chunks' in order: the same in every thread.  red: a workgroup's.  meanwhile() is called
+// while the first of them are on their way.
+template <class Meanwhile>
+__device__ __forceinline__ double square_of(const PlanArgs &a, const AdamwHeader &h, uint32_t begin, uint32_t end, double *red,
+                                            const Meanwhile &meanwhile) {
     const double *parts = parts_of(a, h);
     double s = 0.0;
     constexpr int kBatch = 8;   // loads on their way together
-    for (uint32_t i = begin + threadIdx.x; i < end; i += kBatch * kTh) {
-        double v[kBatch];
+    double v[kBatch];
+    const auto load = [&](uint32_t i) {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) v[j] = i + j * kTh < end ? parts[i + j * kTh] : 0.0;
+    };
+    const auto add = [&] {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) s += v[j];
+    };
+    load(begin + threadIdx.x);
+    meanwhile();
+    add();
+    for (uint32_t i = begin + kBatch * kTh + threadIdx.x; i < end; i += kBatch * kTh) {
+        load(i);
+        add();
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m);
@@ -191,20 +203,24 @@ __device__ __forceinline__ double square_of(const PlanArgs &a, const AdamwHeader
     return ((red[0] + red[1]) + red[2]) + red[3];
 }
 
-// What a group's elements are multiplied by in step t.
-__device__ __forceinline__ AdamwGroup record_of(const StepArgs &x, int group, bool with_norm, double norm, int64_t t) {
+// What a group's elements are multiplied by in step t, but for what its norm decides.
+__device__ __forceinline__ AdamwGroup rates_of(const StepArgs &x, int group, int64_t t) {
     const AdamwHyper &y = x.y;
     const double fix1 = 1.0 - pow(y.beta1, static_cast<double>(t)), fix2 = 1.0 - pow(y.beta2, static_cast<double>(t));
     // lr lr_scale is one rounding, as a caller's own product of the two would be
     const double lr = static_cast<double>(x.lr_scale ? static_cast<float>(y.lr) * x.lr_scale[group] : static_cast<float>(y.lr));
     AdamwGroup o;
-    o.clip = with_norm && y.max_norm > 0.0 && norm > y.max_norm ? y.max_norm / norm : 1.0;
+    o.clip = 1.0;
     o.lr = static_cast<float>(lr);
     o.rate = static_cast<float>(lr / fix1);
     o.root = static_cast<float>(1.0 / sqrt(fix2));
-    o.skip = with_norm && !(norm < __builtin_inf());
+    o.skip = false;
     o.step = t;
     return o;
+}
+__device__ __forceinline__ void set_norm(AdamwGroup &o, double max_norm, double norm) {
+    if (max_norm > 0.0 && norm > max_norm) o.clip = max_norm / norm;
+    o.skip = !(norm < __builtin_inf());
 }
 
 // A workgroup for each group: its norm, and its record.
@@ -214,11 +230,15 @@ __global__ __launch_bounds__(kTh) void k_adamw_head(PlanArgs a, StepArgs x, bool
     __shared__ double red[kTh / 64];
     const int group = static_cast<int>(blockIdx.x);
     const int64_t done = *x.step;
-    double norm = 0.0;
-    if (with_norm) norm = sqrt(square_of(a, h, a.starts[group], a.starts[group + 1], red));
-    if (threadIdx.x) return;
-    if (x.norms) x.norms[group] = static_cast<float>(norm);
-    a.group[group] = record_of(x, group, with_norm, norm, done + 1);
+    AdamwGroup o;
+    if (with_norm) {
+        const double norm = sqrt(square_of(a, h, a.starts[group], a.starts[group + 1], red, [&] { o = rates_of(x, group, done + 1); }));
+        set_norm(o, x.y.max_norm, norm);
+        if (x.norms && threadIdx.x == 0) x.norms[group] = static_cast<float>(norm);
+    } else {
+        o = rates_of(x, group, done + 1);
+    }
+    if (threadIdx.x == 0) a.group[group] = o;
 }
 
 // param after its move.  The hardware's root and reciprocal are within one last bit, and what they make is a correction of
@@ -336,9 +356,16 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, StepArgs x) {
         if constexpr (!JOIN) return constant(a.group + k.group);
         __shared__ double red[kTh / 64];
         const uint32_t begin = a.starts[k.group], end = a.starts[k.group + 1];
-        const double norm = sqrt(square_of(a, h, begin, end, red));
+        __shared__ AdamwGroup rates;   // one wave's work: the powers take as long as a chunk's elements
+        const double norm = sqrt(square_of(a, h, begin, end, red, [&] {
+            if (threadIdx.x < kTh - 64) return;
+            const AdamwGroup of = rates_of(x, static_cast<int>(k.group), a.group->step);
+            if (threadIdx.x == kTh - 1) rates = of;
+        }));
+        AdamwGroup of = rates;
+        set_norm(of, y.max_norm, norm);
         if (x.norms && threadIdx.x == 0 && k.slot == begin) x.norms[k.group] = static_cast<float>(norm);
-        return record_of(x, static_cast<int>(k.group), true, norm, a.group->step);
+        return of;
     };
     AdamwGroup o;
     if (!JOIN) o = record();
