@@ -269,15 +269,16 @@ def test_backward_of_masked_batches_and_no_rows():
     P.logra_layer_norm_forward(empty, y[:0])
 
 
-def test_backward_of_rows_without_variance():
+@pytest.mark.parametrize("rows", [4, 1040])
+def test_backward_of_rows_without_variance(rows):
     # rstd = 1 / sqrt(eps) up to 10^15, whose cube no fp32 holds: dx = rstd (c - avg(c))
     import torch
     import paper_2405_13954_amd as P
     g = torch.Generator().manual_seed(3)
-    dy = torch.randn(4, 96, generator=g).cuda()
-    h = torch.tensor([0.0, 3.0, -1e-3, 1e4]).cuda()[:, None].expand(4, 96).contiguous()
+    dy = torch.randn(rows, 96, generator=g).cuda()
+    h = torch.tensor([0.0, 3.0, -1e-3, 1e4]).cuda().repeat(rows // 4)[:, None].expand(rows, 96).contiguous()
     for eps in (1e-5, 1e-20, 1e-30):
-        y, mean, rstd, dx, dgain = torch.empty_like(h), f32(4), f32(4), torch.empty_like(h), f32(96)
+        y, mean, rstd, dx, dgain = torch.empty_like(h), f32(rows), f32(rows), torch.empty_like(h), f32(96)
         P.logra_layer_norm_forward(h, y, eps=eps, mean=mean, rstd=rstd)
         P.logra_layer_norm_backward(h, dy, rstd, mean=mean, dx=dx, dgain=dgain)
         c = host(dy)
@@ -303,18 +304,18 @@ def test_nan_stays_in_its_row():
     assert torch.isnan(dgain).nonzero().flatten().tolist() == [7] and torch.isnan(dbias).nonzero().flatten().tolist() == [7]
 
 
-@pytest.mark.parametrize("cols", [72, 2048, 8200, 12296])
+@pytest.mark.parametrize("rows,cols", [(6, 72), (6, 2048), (6, 8200), (6, 12296), (1100, 72), (1100, 2048), (1100, 12296)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_masked_rows_under_a_gain_that_is_not_finite(dtype, cols):
+def test_masked_rows_under_a_gain_that_is_not_finite(dtype, rows, cols):
     import torch
     import paper_2405_13954_amd as P
     g = torch.Generator().manual_seed(cols)
-    h, dy, base = (torch.randn(6, cols, generator=g).to(dt(dtype)).cuda() for _ in range(3))
+    h, dy, base = (torch.randn(rows, cols, generator=g).to(dt(dtype)).cuda() for _ in range(3))
     gain = torch.ones(cols, dtype=dt(dtype), device="cuda")
     gain[3], gain[cols - 2] = float("nan"), float("inf")
-    mask = torch.tensor([1, 0, 1, 0, 0, 1], dtype=torch.uint8, device="cuda")
+    mask = torch.tensor([1, 0, 1, 0, 0, 1], dtype=torch.uint8, device="cuda").repeat(rows // 6 + 1)[:rows]
     off = mask == 0
-    y, dx, mean, rstd, dgain, dbias = torch.empty_like(h), torch.empty_like(h), f32(6), f32(6), f32(cols), f32(cols)
+    y, dx, mean, rstd, dgain, dbias = torch.empty_like(h), torch.empty_like(h), f32(rows), f32(rows), f32(cols), f32(cols)
     P.logra_layer_norm_forward(h, y, gain=gain, mask=mask, mean=mean, rstd=rstd)
     assert not y[off].any() and bool(torch.isnan(y[~off][:, 3]).all())
     for rms in (False, True):
@@ -357,14 +358,15 @@ def test_gradients_against_differences(rms):
     assert abs(float(up - (y.double() * dy.double()).sum() - dgain.double().sum())) <= 400 * U * float((y * dy).abs().sum() + mag.sum())
 
 
-def test_reruns_streams_and_graphs():
+@pytest.mark.parametrize("rows", [700, 1300])
+def test_reruns_streams_and_graphs(rows):
     import torch
     import paper_2405_13954_amd as P
     g = torch.Generator().manual_seed(9)
-    h, dy, r = (torch.randn(700, 1032, generator=g).to(torch.bfloat16).cuda() for _ in range(3))
+    h, dy, r = (torch.randn(rows, 1032, generator=g).to(torch.bfloat16).cuda() for _ in range(3))
     gain, bias = torch.randn(1032, generator=g).to(torch.bfloat16).cuda(), torch.randn(1032, generator=g).to(torch.bfloat16).cuda()
-    ws = torch.empty(P.logra_layer_norm_ws_size(700, 1032), dtype=torch.uint8, device="cuda")
-    out = dict(y=torch.empty_like(h), hs=torch.empty_like(h), dx=torch.empty_like(h), mean=f32(700), rstd=f32(700),
+    ws = torch.empty(P.logra_layer_norm_ws_size(rows, 1032), dtype=torch.uint8, device="cuda")
+    out = dict(y=torch.empty_like(h), hs=torch.empty_like(h), dx=torch.empty_like(h), mean=f32(rows), rstd=f32(rows),
                dgain=f32(1032), dbias=f32(1032))
 
     def both(ws=ws):

@@ -153,34 +153,36 @@ def test_forbidden_and_extreme_logits(vocab, dtype):
     check(z, zt.double().numpy(), target, [0, 3, 5, 6, 8, 9, 10], dtype, smoothing=0.25, beta=-0.5)
 
 
-def test_what_is_not_read_may_hold_anything():
+@pytest.mark.parametrize("rows", [9, 300])   # (three launches from 257 rows of two pairs on)
+def test_what_is_not_read_may_hold_anything(rows):
     import torch
     import paper_2405_13954_amd as P
-    full = torch.randn(9, 780, generator=torch.Generator().manual_seed(0)).cuda()
+    full = torch.randn(rows, 780, generator=torch.Generator().manual_seed(0)).cuda()
     z = full[:, :777]
-    z[0], z[8], z[3] = float("nan"), float("nan"), float("nan")     # before, behind, masked
+    z[0], z[8:], z[3] = float("nan"), float("nan"), float("nan")     # before, behind, masked
     z[6, 5] = float("nan")                                          # in pair 1
-    target = torch.tensor([3, 4, 5, -1, 776, 0, 9, 2, 1]).cuda()
+    target = torch.tensor([3, 4, 5, -1, 776, 0, 9, 2] + [1] * (rows - 8)).cuda()
     offsets = torch.tensor([1, 3, 5, 6, 8]).cuda()
-    loss, logp, d = f32(2), f32(4), torch.empty(9, 780, device="cuda")[:, :777]
+    loss, logp, d = f32(2), f32(4), torch.empty(rows, 780, device="cuda")[:, :777]
     P.logra_preference_loss(z, target, offsets, logp, loss=loss, dlogits=d)
     assert torch.isnan(loss).tolist() == [False, True] and torch.isnan(logp).tolist() == [False, False, False, True]
-    assert not d[[0, 3, 8]].any() and bool(torch.isfinite(d[[1, 2, 4]]).all())
+    assert not d[[0, 3]].any() and not d[8:].any() and bool(torch.isfinite(d[[1, 2, 4]]).all())
     # a pair that does not count, whatever it holds
     P.logra_preference_loss(z, target, offsets, logp, loss=loss, dlogits=d, weight=torch.tensor([1.0, 0.0]).cuda())
     assert loss[1] == 0 and not d[5:8].any() and bool(torch.isfinite(d).all())
 
 
-def test_offsets_of_any_kind_are_safe():
+@pytest.mark.parametrize("rows", [6, 300])
+def test_offsets_of_any_kind_are_safe(rows):
     # values out of range or decreasing: results are unspecified, memory is not touched outside the outputs
     import torch
     import paper_2405_13954_amd as P
     for cuts in ([-5, 3, 100, 2, 1 << 40], [-(1 << 62), 1 << 62, 0, 6, 3], [6, 6, 6, 6, 6], [9, 9, 9, 9, 9], [5, 4, 3, 2, 1]):
-        z, _, _ = mk(np.random.default_rng(0), 6, 50, 1.0, "f32")
-        d, full = room(6, 50, "f32")
+        z, _, _ = mk(np.random.default_rng(0), rows, 50, 1.0, "f32")
+        d, full = room(rows, 50, "f32")
         loss, logp = f32(3), f32(5)
-        P.logra_preference_loss(z, torch.arange(6).cuda(), torch.tensor(cuts).cuda(), logp[:4], loss=loss[:2], dlogits=d)
-        guarded(full, 6, 50)
+        P.logra_preference_loss(z, (torch.arange(rows) % 50).cuda(), torch.tensor(cuts).cuda(), logp[:4], loss=loss[:2], dlogits=d)
+        guarded(full, rows, 50)
         assert loss[2] == 12345.0 and logp[4] == 12345.0
     assert logp[:4].tolist() == [0.0] * 4
 
