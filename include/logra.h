@@ -634,8 +634,8 @@ int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, in
  *   gain, bias  device [cols] of dtype, 16-byte aligned, or NULL (1, 0)
  *   mean, rstd  device fp32 [rows] or NULL: for the backward pass
  *   eps      in [1e-30, 1e30]
- * Statistics are fp32: where the average of the squares is beyond it (magnitudes
- * from 1.8e19 on), rstd is 0.
+ * Statistics are fp32: where the average of (h_t - mean_t)^2 is beyond it
+ * (magnitudes from 1.8e19 on, whatever cols is), rstd is 0 and y the bias.
  *
  * logra_layer_norm_backward, with xh_t = (h_t - mean_t) rstd_t and c_t = dy_t gain:
  *

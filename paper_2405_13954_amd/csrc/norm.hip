@@ -6,7 +6,9 @@
 //
 // (rms: mean = 0, and no avg(c).)  A row is held in the registers of a team of threads, each with NV of its 16-byte
 // vectors, so memory sees every tensor once, which is what bounds both passes.  The variance is that of the differences
-// from the mean, formed after the mean: no cancellation.  Sums and statistics are fp32.
+// from the mean, formed after the mean: no cancellation.  Sums and statistics are fp32.  The statistics' terms are scaled by a
+// power of two (exact for normal numbers; of smaller terms eps leaves nothing), so that their sums stay near the averages: what
+// overflows is an average beyond fp32, and not the sum of a wide row.
 //
 // Backward: a workgroup walks rows a grid apart and keeps the sums for dgain and dbias of its columns in registers; the
 // next row's vectors are loaded before the current row's sums are known.  The workgroups' sums go to the workspace, and a
@@ -30,6 +32,7 @@ struct FwdArgs {
     float *mean, *rstd;
     int cols;
     float eps;
+    float down, per;   // 2^-k, 2^k / cols for the smallest 2^k >= cols
     bool stream;
 };
 
@@ -173,15 +176,14 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) h[k] = first_of<BF16>(h[k], a.cols - (k * TPR + lane) * V::kN);
-    const float per = 1.f / static_cast<float>(a.cols);
     float mean = 0.f;
     if constexpr (CENTER) {
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < V::kN; ++e) s += V::get(h[k], e);
-        mean = team_sum<TPR>(s, red[0]) * per;
+            for (int e = 0; e < V::kN; ++e) s = fmaf(V::get(h[k], e), a.down, s);
+        mean = team_sum<TPR>(s, red[0]) * a.per;
     }
     float q = 0.f;
 #pragma unroll
@@ -190,10 +192,10 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
 #pragma unroll
         for (int e = 0; e < V::kN; ++e) {
             const float d = V::get(h[k], e) - mean;
-            q += e < n ? d * d : 0.f;
+            q += e < n ? (d * a.down) * d : 0.f;
         }
     }
-    const float var = team_sum<TPR>(q, red[1]) * per;
+    const float var = team_sum<TPR>(q, red[1]) * a.per;
     const float rstd = 1.f / sqrtf(var + a.eps);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -585,9 +587,12 @@ size_t norm_ws_bytes(int64_t rows, int cols) {
 }
 
 hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
+    float width = 1.f;
+    while (width < static_cast<float>(n.cols)) width *= 2.f;
     FwdArgs a = {static_cast<const char *>(n.x), static_cast<const char *>(n.residual), static_cast<char *>(n.h),
                  static_cast<char *>(n.y), n.ld_x, n.ld_res, n.ld_h, n.ld_y, n.rows, n.mask,
                  static_cast<const char *>(n.gain), static_cast<const char *>(n.bias), n.mean, n.rstd, n.cols, n.eps,
+                 1.f / width, width / static_cast<float>(n.cols),
                  beyond_cache(n.bf16, n.rows, n.cols, 2 + (n.residual ? 1 : 0) + (n.h ? 1 : 0))};
     const int vec = vectors_of(n.bf16, n.cols);
     const auto go = [&](auto t, auto v) {

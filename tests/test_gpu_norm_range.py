@@ -1,0 +1,61 @@
+"""Layer norm over the whole range of fp32 magnitudes, against the float64 oracle: squares whose sum no fp32 number holds but
+whose average does, and what lies beyond the range.
+
+The bounds are those of test_gpu_norm.py: nothing in them depends on the size of the numbers.
+"""
+import numpy as np
+import pytest
+
+from oracle import tuning as O
+from test_gpu_norm import ROW, forward_bounds
+from tuning_util import HALF, U, dt, f32, host, room, vector, within
+
+pytestmark = pytest.mark.gpu
+
+
+def rows_of(g, rows, cols, size, dtype, shift=0.0):
+    """([rows, cols] of N(shift, 1) size on the device, at a stride of whole vectors, and its float64 values)."""
+    import torch
+    t = torch.from_numpy(((g.standard_normal((rows, cols)) + shift) * size).astype(np.float32)).to(dt(dtype))
+    view, _ = room(rows, cols, dtype)
+    view.copy_(t)
+    return view, t.double().numpy()
+
+
+# 64 columns: the sum of the squares is in range where a row's average is; 16,377 and 16,384: four vectors a thread
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("rows,cols", [(5, 64), (5, 4096), (5, 9001), (5, 16384), (1030, 768), (1030, 4104), (1030, 16377)])
+def test_forward_where_the_average_of_the_squares_is_in_range(rows, cols, rms, dtype):
+    import torch
+    import paper_2405_13954_amd as P
+    g = np.random.default_rng([rows, cols, rms])
+    for size, eps in ((1e17, 1e-5), (1e18, 1e-5), (1e19, 1e-5), (1e19, 1e30), (1e-12, 1e-30)):
+        print("[norm range, forward]", rows, cols, dtype, rms, size, eps, flush=True)
+        x, x64 = rows_of(g, rows, cols, size, dtype, 0.5)
+        gain, gain64 = vector(g, cols, 0.3, dtype, 1.0)
+        y, mean, rstd = room(rows, cols, dtype)[0], (None if rms else f32(rows)), f32(rows)
+        P.logra_layer_norm_forward(x, y, gain=gain, eps=eps, rms=rms, mean=mean, rstd=rstd)
+        eps32 = float(np.float32(eps))
+        want, want_mean, want_rstd = O.norm_forward(x64, gain64, None, eps32, rms)
+        em, er, ey = forward_bounds(x64, want, want_mean, want_rstd, gain64, None, eps32, rms)
+        within(host(rstd), want_rstd, er, "rstd")
+        if not rms:
+            within(host(mean), want_mean, em, "mean")
+        within(host(y), want, ey + HALF[dtype] * (np.abs(want) + ey), "y")
+    assert torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(5, 64), (5, 4096), (1030, 4104)])
+def test_forward_beyond_the_range(rows, cols, dtype):
+    # the average of the squares is beyond fp32: rstd is 0 and y the bias; the mean is in range up to the largest numbers
+    import paper_2405_13954_amd as P
+    g = np.random.default_rng([rows, cols])
+    for size in (1e20, 1e37):
+        x, x64 = rows_of(g, rows, cols, size, dtype, 6.0)
+        bias, bias64 = vector(g, cols, 0.3, dtype)
+        y, mean, rstd = room(rows, cols, dtype)[0], f32(rows), f32(rows)
+        P.logra_layer_norm_forward(x, y, bias=bias, mean=mean, rstd=rstd)
+        assert not rstd.any() and np.array_equal(host(y), np.broadcast_to(bias64, y.shape))
+        within(host(mean), x64.mean(1), ROW * np.abs(x64).mean(1), "mean")
