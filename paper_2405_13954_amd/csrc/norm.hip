@@ -302,21 +302,21 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
 #pragma unroll
             for (int e = 0; e < V::kN; ++e) {
                 const float dy = V::get(cur.dy[k], e), c = dy * g[e];
-                const float d = CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e);
+                const float xh = (CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e)) * cur.rstd;
                 if constexpr (CENTER) {
                     s1 += c;
                     db[k][e] += dy;
                 }
-                s2 = fmaf(c, d, s2);
-                dg[k][e] = fmaf(dy, d * cur.rstd, dg[k][e]);
+                s2 = fmaf(c, xh, s2);
+                dg[k][e] = fmaf(dy, xh, dg[k][e]);
             }
             if constexpr (kTight) asm volatile("" : "+v"(cur.h[k]), "+v"(cur.dy[k]));   // not its fp32 values are kept
         }
         team_sums<TPR, CENTER>(s1, s2, red[it & 1], team);   // (the other half may still be read by a slower wave)
-        // dx - base = rstd (c - avg(c) - xh avg(c xh)) = rstd c + (h - mean) along + level.  (A masked row has zeros in all, whose
-        // products with a gain that is not finite are dropped.)
-        // The sum comes first: it is as small as rstd is large, so that the product of a row without variance stays finite.
-        const float level = -cur.rstd * (s1 * per), along = -(s2 * per) * cur.rstd * cur.rstd * cur.rstd;
+        // dx - base = rstd (c - avg(c) - xh avg(c xh)) = rstd c + xh along + level, from xh itself: the cube of rstd, which stands
+        // before h - mean otherwise, leaves fp32 on both sides.  (A masked row has zeros in all, whose products with a gain that is
+        // not finite are dropped.)
+        const float level = -cur.rstd * (s1 * per), along = -cur.rstd * (s2 * per);
         if (a.dx && row < a.rows) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -327,9 +327,9 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
 #pragma unroll
                 for (int e = 0; e < V::kN; ++e) {
                     const float c = V::get(cur.dy[k], e) * g[e];
-                    const float d = CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e);
+                    const float xh = (CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e)) * cur.rstd;
                     const float to = V::get(base[k], e);
-                    o[e] = cur.live ? to + fmaf(c, cur.rstd, fmaf(d, along, level)) : to;
+                    o[e] = cur.live ? to + fmaf(c, cur.rstd, fmaf(xh, along, level)) : to;
                 }
                 V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
             }
@@ -481,12 +481,12 @@ __global__ __launch_bounds__(few_threads(TPR)) void k_norm_bwd_few(BwdArgs a, fl
         for (int e = 0; e < V::kN; ++e) {
             const float c = V::get(dy[k], e) * V::get(gain[k], e);
             if constexpr (CENTER) s1 += c;
-            s2 = fmaf(c, V::get(h[k], e) - mean, s2);
+            s2 = fmaf(c, (V::get(h[k], e) - mean) * rstd, s2);
         }
     }
     team_sums<TPR, CENTER>(s1, s2, red, static_cast<int>(threadIdx.x) / TPR);
     const float per = 1.f / static_cast<float>(a.cols);
-    const float level = -rstd * (s1 * per), along = -(s2 * per) * rstd * rstd * rstd;   // as in k_norm_bwd
+    const float level = -rstd * (s1 * per), along = -rstd * (s2 * per);   // as in k_norm_bwd
     if (!in) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(few_threads(TPR)) void k_norm_bwd_few(BwdArgs a, fl
 #pragma unroll
         for (int e = 0; e < V::kN; ++e) {
             const float c = V::get(dy[k], e) * V::get(gain[k], e), to = V::get(base[k], e);
-            o[e] = live ? to + fmaf(c, rstd, fmaf(V::get(h[k], e) - mean, along, level)) : to;
+            o[e] = live ? to + fmaf(c, rstd, fmaf((V::get(h[k], e) - mean) * rstd, along, level)) : to;
         }
         V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
     }
