@@ -877,10 +877,13 @@ def logra_adamw_plan_size(tensors, n_groups: int) -> int:
 
 
 class AdamwPlan(NamedTuple):
-    """What logra_adamw_plan returns: the plan's memory, and the tensors, which have to outlive it."""
+    """What logra_adamw_plan returns: the plan's memory, and the tensors, which have to outlive it.  Both have to outlive the
+    captured graphs that hold its steps; of steps on other streams than the plan's own (queue), its memory is kept until they
+    have run, the tensors are the caller's to keep."""
     memory: object
     tensors: tuple
     n_groups: int
+    queue: object = None   # the stream that the memory is of; None: the caller's own memory
 
 
 def logra_adamw_plan(tensors, n_groups: int, stream=None) -> AdamwPlan:
@@ -892,7 +895,7 @@ def logra_adamw_plan(tensors, n_groups: int, stream=None) -> AdamwPlan:
     queue = _queue(tensors[0].param, stream) if tensors else _stream(stream).value
     memory = _scratch(int(lib().logra_adamw_plan_size(descs, len(tensors), n_groups)), device, stream)
     _check(lib().logra_adamw_plan(descs, len(tensors), n_groups, memory.data_ptr(), memory.numel(), queue))
-    return AdamwPlan(memory, tuple(tensors), n_groups)
+    return AdamwPlan(memory, tuple(tensors), n_groups, queue or 0)
 
 
 def logra_adamw_step(plan: AdamwPlan, step, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -904,7 +907,10 @@ def logra_adamw_step(plan: AdamwPlan, step, lr: float, beta1: float = 0.9, beta2
     left as it is.  seed: of the random rounding of 8-bit states."""
     torch = _torch()
     n, f32 = plan.n_groups, torch.float32
+    queue = _queue(plan.memory, stream)
+    if plan.queue is not None and plan.queue != (queue or 0):   # the chunks' pointers must not be overwritten before they are read
+        plan.memory.record_stream(torch.cuda.ExternalStream(queue) if queue else torch.cuda.default_stream(plan.memory.device))
     _check(lib().logra_adamw_step(
         plan.memory.data_ptr(), plan.memory.numel(), n, _packed(step, (1,), torch.int64, "step"), lr, beta1, beta2, eps,
         weight_decay, max_norm, _packed(lr_scale, (n,), f32, "lr_scale"), _packed(norms, (n,), f32, "norms"), seed,
-        _queue(plan.memory, stream)))
+        queue))
