@@ -1044,12 +1044,13 @@ Region flat(const void *p, int64_t n, size_t bytes) {
     return {static_cast<uint64_t>(reinterpret_cast<uintptr_t>(p)), size > 0 ? size : 1, size, 1};
 }
 int check_operands(std::initializer_list<Operand> in, std::initializer_list<Operand> out) {
+    const auto some = [](const Region &r) { return r.at && r.rows > 0 && r.width > 0; };
     for (const Operand &w : out) {
-        if (!w.at.at) continue;
+        if (!some(w.at)) continue;
         for (const Operand &r : in)
-            if (r.at.at) TRY(check_apart(r.name, r.at, w.name, w.at, r.in_place && w.in_place));
+            if (some(r.at)) TRY(check_apart(r.name, r.at, w.name, w.at, r.in_place && w.in_place));
         for (const Operand *o = out.begin(); o != &w; ++o)
-            if (o->at.at) TRY(check_apart(o->name, o->at, w.name, w.at, false));
+            if (some(o->at)) TRY(check_apart(o->name, o->at, w.name, w.at, false));
     }
     return LOGRA_OK;
 }
@@ -1098,14 +1099,17 @@ int norm_backward(const logra::NormBackward &n, int dtype, size_t ws_bytes) {
         TRY(check_stride("dy", n.ld_dy, n.rows, n.cols, dtype));
         if (n.dx) TRY(check_stride("dx", n.ld_dx, n.rows, n.cols, dtype));
         if (n.base) TRY(check_stride("base", n.ld_base, n.rows, n.cols, dtype));
-        const auto matrix = [&](const void *p, int64_t ld) { return region(p, ld, n.cols, n.rows, dtype); };
-        TRY(check_operands({{"h", matrix(n.h, n.ld_h), true}, {"dy", matrix(n.dy, n.ld_dy), true},
-                            {"base", matrix(n.base, n.ld_base), true}, {"gain", flat(n.gain, n.cols, es), false},
-                            {"mask", flat(n.mask, n.rows, 1), false}, {"mean", flat(n.mean, n.rows, 4), false},
-                            {"rstd", flat(n.rstd, n.rows, 4), false}},
-                           {{"dx", matrix(n.dx, n.ld_dx), true}, {"dgain", flat(n.dgain, n.cols, 4), false},
-                            {"dbias", flat(n.dbias, n.cols, 4), false},
-                            {"ws", flat(n.ws, static_cast<int64_t>(ws_bytes), 1), false}}));
+    }
+    // (without rows the matrices have no memory, but dgain and dbias are cleared)
+    const auto matrix = [&](const void *p, int64_t ld) { return region(p, ld, n.cols, n.rows, dtype); };
+    TRY(check_operands({{"h", matrix(n.h, n.ld_h), true}, {"dy", matrix(n.dy, n.ld_dy), true},
+                        {"base", matrix(n.base, n.ld_base), true}, {"gain", flat(n.gain, n.cols, es), false},
+                        {"mask", flat(n.mask, n.rows, 1), false}, {"mean", flat(n.mean, n.rows, 4), false},
+                        {"rstd", flat(n.rstd, n.rows, 4), false}},
+                       {{"dx", matrix(n.dx, n.ld_dx), true}, {"dgain", flat(n.dgain, n.cols, 4), false},
+                        {"dbias", flat(n.dbias, n.cols, 4), false},
+                        {"ws", flat(n.ws, static_cast<int64_t>(ws_bytes), 1), false}}));
+    if (n.rows > 0) {
         TRY(check_matrix(n.h, "h", n.rows, n.ld_h, n.cols, dtype));
         TRY(check_matrix(n.dy, "dy", n.rows, n.ld_dy, n.cols, dtype));
         if (n.dx) TRY(check_matrix(n.dx, "dx", n.rows, n.ld_dx, n.cols, dtype));
