@@ -1325,13 +1325,14 @@ int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t row
     if (rows > 0) {
         TRY(check_stride("logits", ld, rows, vocab, dtype));
         if (dlogits) TRY(check_stride("dlogits", ld_d, rows, vocab, dtype));
-        const int64_t n = n_pairs;
-        TRY(check_operands({{"logits", region(logits, ld, vocab, rows, dtype), true}, {"target", flat(target, rows, 8), false},
-                            {"offsets", flat(offsets, 2 * n + 1, 8), false}, {"ref", flat(ref, 2 * n, 4), false},
-                            {"weight", flat(weight, n, 4), false}},
-                           {{"dlogits", region(dlogits, ld_d, vocab, rows, dtype), true}, {"loss", flat(loss, n, 4), false},
-                            {"logp", flat(logp, 2 * n, 4), false},
-                            {"ws", flat(ws, static_cast<int64_t>(ws_bytes), 1), false}}));
+    }
+    const int64_t n = n_pairs;   // (without rows there are their losses still)
+    TRY(check_operands({{"logits", region(logits, ld, vocab, rows, dtype), true}, {"target", flat(target, rows, 8), false},
+                        {"offsets", flat(offsets, 2 * n + 1, 8), false}, {"ref", flat(ref, 2 * n, 4), false},
+                        {"weight", flat(weight, n, 4), false}},
+                       {{"dlogits", region(dlogits, ld_d, vocab, rows, dtype), true}, {"loss", flat(loss, n, 4), false},
+                        {"logp", flat(logp, 2 * n, 4), false}, {"ws", flat(ws, static_cast<int64_t>(ws_bytes), 1), false}}));
+    if (rows > 0) {
         TRY(check_matrix(logits, "logits", rows, ld, vocab, dtype));
         TRY(check_dev(target, "target", 8));
         if (dlogits) TRY(check_matrix(dlogits, "dlogits", rows, ld_d, vocab, dtype));
