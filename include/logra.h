@@ -730,7 +730,7 @@ int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t row
  *   Elements need their own alignment only: tensors may be parts of flat buffers.
  *
  * logra_adamw_plan lays the list out in device memory, once for all steps; the
- *   tensors must stay where they are while the plan is used.  No two of the step's
+ *   tensors must stay where they are while the plan is used.  No two of the list's
  *   arrays may share memory, except gradients with each other (refused).
  *   Synchronous, and refused while the stream is captured.  plan: device memory of
  *   logra_adamw_plan_size bytes, 256-byte aligned; it is also the step's workspace,
@@ -745,6 +745,10 @@ int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t row
  *             as it is, parameters and states; otherwise what is not finite stays
  *             in its own elements
  *   beta1, beta2 in [0, 1), eps in [1e-30, 1e30], weight_decay >= 0
+ *   step, lr_scale, norms and the plan share no memory (refused), and none with the
+ *   listed tensors either, but lr_scale with gradients: the call, which has the
+ *   list on the device alone, leaves that to its caller (the Python binding, which
+ *   has the tensors, refuses it)
  * Memory that holds no plan for n_groups is recognised on the device: nothing is
  * written then.  Reruns from the same state are bitwise identical. */
 typedef struct {

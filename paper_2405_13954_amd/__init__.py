@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from bisect import bisect_right
 from typing import NamedTuple
 
 import numpy as np
@@ -884,6 +885,25 @@ class AdamwPlan(NamedTuple):
     tensors: tuple
     n_groups: int
     queue: object = None   # the stream that the memory is of; None: the caller's own memory
+    read: tuple = (1 << 64,)      # where the tensors' arrays begin and end, as _edges gives it
+    written: tuple = (1 << 64,)   # the same without the gradients
+
+
+def _edges(arrays) -> tuple:
+    """Begin and end of each stretch of memory that the tensors cover, in order of address, and then the last address of all."""
+    out = []
+    for begin, end in sorted((a.data_ptr(), a.data_ptr() + a.numel() * a.element_size()) for a in arrays if a is not None and a.numel()):
+        if out and begin < out[-1]:
+            out[-1] = max(out[-1], end)
+        else:
+            out += (begin, end)
+    return (*out, 1 << 64)
+
+
+def _inside(edges: tuple, at: int, nbytes: int) -> bool:
+    """Whether memory lies within the edges, in part or whole."""
+    i = bisect_right(edges, at)
+    return i & 1 == 1 or edges[i] < at + nbytes
 
 
 def logra_adamw_plan(tensors, n_groups: int, stream=None) -> AdamwPlan:
@@ -895,7 +915,8 @@ def logra_adamw_plan(tensors, n_groups: int, stream=None) -> AdamwPlan:
     queue = _queue(tensors[0].param, stream) if tensors else _stream(stream).value
     memory = _scratch(int(lib().logra_adamw_plan_size(descs, len(tensors), n_groups)), device, stream)
     _check(lib().logra_adamw_plan(descs, len(tensors), n_groups, memory.data_ptr(), memory.numel(), queue))
-    return AdamwPlan(memory, tuple(tensors), n_groups, queue or 0)
+    own = [a for t in tensors for a in (t.param, t.work, t.m, t.v, t.m_scale, t.v_scale)]
+    return AdamwPlan(memory, tuple(tensors), n_groups, queue or 0, _edges(own + [t.grad for t in tensors]), _edges(own))
 
 
 def logra_adamw_step(plan: AdamwPlan, step, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -907,10 +928,16 @@ def logra_adamw_step(plan: AdamwPlan, step, lr: float, beta1: float = 0.9, beta2
     left as it is.  seed: of the random rounding of 8-bit states."""
     torch = _torch()
     n, f32 = plan.n_groups, torch.float32
+    at, scales, out = _packed(step, (1,), torch.int64, "step"), _packed(lr_scale, (n,), f32, "lr_scale"), _packed(norms, (n,), f32, "norms")
+    if at is not None and _inside(plan.read, at, 8):
+        raise ValueError("step and the plan's tensors share memory")
+    if scales is not None and _inside(plan.written, scales, 4 * n):
+        raise ValueError("lr_scale and the plan's tensors share memory")
+    if out is not None and _inside(plan.read, out, 4 * n):
+        raise ValueError("norms and the plan's tensors share memory")
     queue = _queue(plan.memory, stream)
     if plan.queue is not None and plan.queue != (queue or 0):   # the chunks' pointers must not be overwritten before they are read
         plan.memory.record_stream(torch.cuda.ExternalStream(queue) if queue else torch.cuda.default_stream(plan.memory.device))
     _check(lib().logra_adamw_step(
-        plan.memory.data_ptr(), plan.memory.numel(), n, _packed(step, (1,), torch.int64, "step"), lr, beta1, beta2, eps,
-        weight_decay, max_norm, _packed(lr_scale, (n,), f32, "lr_scale"), _packed(norms, (n,), f32, "norms"), seed,
+        plan.memory.data_ptr(), plan.memory.numel(), n, at, lr, beta1, beta2, eps, weight_decay, max_norm, scales, out, seed,
         queue))
