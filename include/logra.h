@@ -631,7 +631,8 @@ int logra_token_loss(const void *logits, int64_t ld, int dtype, int64_t rows, in
  *            outputs share no memory with inputs or each other (refused)
  *   mask     device uint8 [rows] or NULL: a row with 0 is not read, its y, h,
  *            mean and rstd are zeros
- *   gain, bias  device [cols] of dtype, 16-byte aligned, or NULL (1, 0)
+ *   gain, bias  device [cols] of dtype, at any alignment of its elements, or NULL
+ *            (1, 0)
  *   mean, rstd  device fp32 [rows] or NULL: for the backward pass
  *   eps      in [1e-30, 1e30]
  * Statistics are fp32: where the average of (h_t - mean_t)^2 is beyond it

@@ -1084,8 +1084,8 @@ int norm_forward(const logra::NormForward &n, int dtype) {
     if (n.residual) TRY(check_matrix(n.residual, "residual", n.rows, n.ld_res, n.cols, dtype));
     if (n.h) TRY(check_matrix(n.h, "h", n.rows, n.ld_h, n.cols, dtype));
     if (n.mask) TRY(check_dev(n.mask, "mask", 1));
-    if (n.gain) TRY(check_dev(n.gain, "gain", 16));
-    if (n.bias) TRY(check_dev(n.bias, "bias", 16));
+    if (n.gain) TRY(check_dev(n.gain, "gain", es));
+    if (n.bias) TRY(check_dev(n.bias, "bias", es));
     if (n.mean) TRY(check_dev(n.mean, "mean", 4));
     if (n.rstd) TRY(check_dev(n.rstd, "rstd", 4));
     return LOGRA_OK;
@@ -1115,7 +1115,7 @@ int norm_backward(const logra::NormBackward &n, int dtype, size_t ws_bytes) {
         if (n.dx) TRY(check_matrix(n.dx, "dx", n.rows, n.ld_dx, n.cols, dtype));
         if (n.base) TRY(check_matrix(n.base, "base", n.rows, n.ld_base, n.cols, dtype));
         if (n.mask) TRY(check_dev(n.mask, "mask", 1));
-        if (n.gain) TRY(check_dev(n.gain, "gain", 16));
+        if (n.gain) TRY(check_dev(n.gain, "gain", es));
         if (!n.rms) TRY(check_dev(n.mean, "mean", 4));
         TRY(check_dev(n.rstd, "rstd", 4));
     }

@@ -52,10 +52,12 @@ __host__ __device__ inline int padded(int cols) { return (cols + 3) & ~3; }
 
 constexpr u32x4 kZero4 = {0, 0, 0, 0};
 
-// The vector of n elements at p (n <= 0: zeros, nothing is read).
+// The vector of n elements at p (n <= 0: zeros, nothing is read).  p need have the elements' alignment only: a gain may be
+// one of several models' of an odd width, one behind the other.
+typedef uint32_t u32x4e __attribute__((ext_vector_type(4), aligned(2)));
 template <bool BF16>
 __device__ __forceinline__ u32x4 take(const char *p, int n) {
-    if (n >= Vec<BF16>::kN) return ld128(p);
+    if (n >= Vec<BF16>::kN) return *reinterpret_cast<const u32x4e *>(p);
     return n > 0 ? Vec<BF16>::load(p, n, kZero4) : kZero4;
 }
 
