@@ -14,7 +14,7 @@
 // next row's vectors are loaded before the current row's sums are known.  The workgroups' sums go to the workspace, and a
 // second launch adds them in order, so that reruns give the same bits.  Few rows: one launch (k_norm_bwd_few).
 //
-// 16,384 rows of 4096 bf16 columns without the mean: forward with residual and statistics 93 us for 537 MB (5.8 TB/s),
+// 16,384 rows of 4096 bf16 columns without the mean: forward with residual and statistics 94 us for 537 MB (5.7 TB/s),
 // backward with base and a fifth of the rows masked 79 + 5 us for 483 MB (5.8).  768 columns with the mean: 16 and 20 + 4 us
 // for 91 and 101 MB.
 #include "internal.h"
@@ -32,7 +32,7 @@ struct FwdArgs {
     float *mean, *rstd;
     int cols;
     float eps;
-    float down, per;   // 2^-k, 2^k / cols for the smallest 2^k >= cols
+    float root, per;   // 2^-k, 4^k / cols for the smallest 4^k >= cols
     bool stream;
 };
 
@@ -184,17 +184,18 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < V::kN; ++e) s = fmaf(V::get(h[k], e), a.down, s);
+            for (int e = 0; e < V::kN; ++e) s = fmaf(V::get(h[k], e), a.root * a.root, s);
         mean = team_sum<TPR>(s, red[0]) * a.per;
     }
     float q = 0.f;
+    const float level = -mean * a.root;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int n = a.cols - (k * TPR + lane) * V::kN;
 #pragma unroll
         for (int e = 0; e < V::kN; ++e) {
-            const float d = V::get(h[k], e) - mean;
-            q += e < n ? (d * a.down) * d : 0.f;
+            const float d = fmaf(V::get(h[k], e), a.root, level);   // 2^-k (h - mean), one rounding
+            q += e < n ? d * d : 0.f;
         }
     }
     const float var = team_sum<TPR>(q, red[1]) * a.per;
@@ -311,14 +312,15 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
                 }
                 s2 = fmaf(c, xh, s2);
                 dg[k][e] = fmaf(dy, xh, dg[k][e]);
+                if constexpr (!BF16) cur.h[k][e] = __float_as_uint(xh);   // (fp32: xh in the place of h)
             }
             if constexpr (kTight) asm volatile("" : "+v"(cur.h[k]), "+v"(cur.dy[k]));   // not its fp32 values are kept
         }
         team_sums<TPR, CENTER>(s1, s2, red[it & 1], team);   // (the other half may still be read by a slower wave)
-        // dx - base = rstd (c - avg(c) - xh avg(c xh)) = rstd c + xh along + level, from xh itself: the cube of rstd, which stands
-        // before h - mean otherwise, leaves fp32 on both sides.  (A masked row has zeros in all, whose products with a gain that is
-        // not finite are dropped.)
-        const float level = -cur.rstd * (s1 * per), along = -cur.rstd * (s2 * per);
+        // dx - base = rstd (c - avg(c) - xh avg(c xh)), as it stands: h - mean under one factor, rstd^3 avg(c (h - mean)), would take
+        // a cube that leaves fp32 on both sides.  (A masked row has zeros in all, whose products with a gain that is not finite are
+        // dropped.)
+        const float level = -(s1 * per), along = -(s2 * per);
         if (a.dx && row < a.rows) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -328,10 +330,10 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
                 gain_of(k, g);
 #pragma unroll
                 for (int e = 0; e < V::kN; ++e) {
-                    const float c = V::get(cur.dy[k], e) * g[e];
-                    const float xh = (CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e)) * cur.rstd;
+                    const float c = CENTER ? fmaf(V::get(cur.dy[k], e), g[e], level) : V::get(cur.dy[k], e) * g[e];
+                    const float at = V::get(cur.h[k], e), xh = BF16 ? (CENTER ? at - cur.mean : at) * cur.rstd : at;
                     const float to = V::get(base[k], e);
-                    o[e] = cur.live ? to + fmaf(c, cur.rstd, fmaf(xh, along, level)) : to;
+                    o[e] = cur.live ? fmaf(fmaf(xh, along, c), cur.rstd, to) : to;
                 }
                 V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
             }
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(few_threads(TPR)) void k_norm_bwd_few(BwdArgs a, fl
     }
     team_sums<TPR, CENTER>(s1, s2, red, static_cast<int>(threadIdx.x) / TPR);
     const float per = 1.f / static_cast<float>(a.cols);
-    const float level = -rstd * (s1 * per), along = -rstd * (s2 * per);   // as in k_norm_bwd
+    const float level = -(s1 * per), along = -(s2 * per);   // as in k_norm_bwd
     if (!in) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -497,8 +499,9 @@ __global__ __launch_bounds__(few_threads(TPR)) void k_norm_bwd_few(BwdArgs a, fl
         float o[V::kN];
 #pragma unroll
         for (int e = 0; e < V::kN; ++e) {
-            const float c = V::get(dy[k], e) * V::get(gain[k], e), to = V::get(base[k], e);
-            o[e] = live ? to + fmaf(c, rstd, fmaf((V::get(h[k], e) - mean) * rstd, along, level)) : to;
+            const float g = V::get(gain[k], e), to = V::get(base[k], e);
+            const float c = CENTER ? fmaf(V::get(dy[k], e), g, level) : V::get(dy[k], e) * g;
+            o[e] = live ? fmaf(fmaf((V::get(h[k], e) - mean) * rstd, along, c), rstd, to) : to;
         }
         V::store(a.dx + row * a.ld_dx * kEs + i * 16, o, n);
     }
@@ -560,7 +563,9 @@ void with_team(int vectors, const Go &go) {
 }
 
 // Whether a call's matrices are more than the 256 MB cache holds.  Then the loads are non-temporal, as the stores always are:
-// nothing of what they would bring into the cache is read there again.  us of the first launch with and without: 16,384 rows
+// a call reads nothing twice, and lines that it would bring into the cache or change there cost its later loads their room.
+// (Measured on the norm alone: what the projection that reads y next would gain by ordinary stores is not in these figures.)
+// us of the first launch with and without: 16,384 rows
 // of 4096 bf16 columns forward 93 and 96, backward 79 and 83; of 768 columns, 91 and 101 MB and the next call on the same
 // memory soon, 20.7 and 16, 21.2 and 19.3.
 bool beyond_cache(bool bf16, int64_t rows, int cols, int matrices) {
@@ -577,7 +582,8 @@ constexpr int kBwdGroups = 256;
 // Up to so many rows k_norm_bwd_few takes the backward pass.  us of a pass with it and with k_norm_bwd and k_norm_parts, of
 // 16, 512, 1,024 and 2,048 rows: 768 bf16 columns with the mean 3.7 and 8.1, 4.3 and 8.4, 7.6 and 8.6, 13.5 and 9.3; 4096 rms
 // 3.3 and 6.7, 7.6 and 9.3, 12.0 and 11.3, 20.6 and 15.7; 14,336 rms 4.5 and 14.5, 16.3 and 26.4, 30.4 and 37.4, 62 and 60.
-// A launch less is also 2.6 us less of the host's time.
+// A launch less is also 2.6 us less of the host's time, which decides at 1,024 rows of 4096; a captured call, which does not pay
+// the host, takes those 0.7 us longer.  Where dx takes the place of h or dy there are two launches.
 constexpr int kFewRows = 1024;
 
 }  // namespace
@@ -589,12 +595,12 @@ size_t norm_ws_bytes(int64_t rows, int cols) {
 }
 
 hipError_t launch_norm_forward(const NormForward &n, hipStream_t s) {
-    float width = 1.f;
-    while (width < static_cast<float>(n.cols)) width *= 2.f;
+    float root = 1.f;
+    while (1.f / (root * root) < static_cast<float>(n.cols)) root *= 0.5f;
     FwdArgs a = {static_cast<const char *>(n.x), static_cast<const char *>(n.residual), static_cast<char *>(n.h),
                  static_cast<char *>(n.y), n.ld_x, n.ld_res, n.ld_h, n.ld_y, n.rows, n.mask,
                  static_cast<const char *>(n.gain), static_cast<const char *>(n.bias), n.mean, n.rstd, n.cols, n.eps,
-                 1.f / width, width / static_cast<float>(n.cols),
+                 root, 1.f / (root * root) / static_cast<float>(n.cols),
                  beyond_cache(n.bf16, n.rows, n.cols, 2 + (n.residual ? 1 : 0) + (n.h ? 1 : 0))};
     const int vec = vectors_of(n.bf16, n.cols);
     const auto go = [&](auto t, auto v) {
