@@ -890,7 +890,8 @@ class AdamwPlan(NamedTuple):
 
 
 def _edges(arrays) -> tuple:
-    """Begin and end of each stretch of memory that the tensors cover, in order of address, and then the last address of all."""
+    """Begin and end of each stretch of memory that the tensors cover, in order of address, and then the last address of all: an
+    address is within one if an odd number of edges are at or before it."""
     out = []
     for begin, end in sorted((a.data_ptr(), a.data_ptr() + a.numel() * a.element_size()) for a in arrays if a is not None and a.numel()):
         if out and begin < out[-1]:
@@ -898,12 +899,6 @@ def _edges(arrays) -> tuple:
         else:
             out += (begin, end)
     return (*out, 1 << 64)
-
-
-def _inside(edges: tuple, at: int, nbytes: int) -> bool:
-    """Whether memory lies within the edges, in part or whole."""
-    i = bisect_right(edges, at)
-    return i & 1 == 1 or edges[i] < at + nbytes
 
 
 def logra_adamw_plan(tensors, n_groups: int, stream=None) -> AdamwPlan:
@@ -929,14 +924,21 @@ def logra_adamw_step(plan: AdamwPlan, step, lr: float, beta1: float = 0.9, beta2
     torch = _torch()
     n, f32 = plan.n_groups, torch.float32
     at, scales, out = _packed(step, (1,), torch.int64, "step"), _packed(lr_scale, (n,), f32, "lr_scale"), _packed(norms, (n,), f32, "norms")
-    if at is not None and _inside(plan.read, at, 8):
-        raise ValueError("step and the plan's tensors share memory")
-    if scales is not None and _inside(plan.written, scales, 4 * n):
-        raise ValueError("lr_scale and the plan's tensors share memory")
-    if out is not None and _inside(plan.read, out, 4 * n):
-        raise ValueError("norms and the plan's tensors share memory")
-    queue = _queue(plan.memory, stream)
-    if plan.queue is not None and plan.queue != (queue or 0):   # the chunks' pointers must not be overwritten before they are read
+    read, written = plan.read, plan.written
+    if at is not None:
+        i = bisect_right(read, at)
+        if i & 1 or read[i] < at + 8:
+            raise ValueError("step and the plan's tensors share memory")
+    if scales is not None:
+        i = bisect_right(written, scales)
+        if i & 1 or written[i] < scales + 4 * n:
+            raise ValueError("lr_scale and the plan's tensors share memory")
+    if out is not None:
+        i = bisect_right(read, out)
+        if i & 1 or read[i] < out + 4 * n:
+            raise ValueError("norms and the plan's tensors share memory")
+    queue, home = _queue(plan.memory, stream), plan.queue
+    if home != (queue or 0) and home is not None:   # the chunks' pointers must not be overwritten before they are read
         plan.memory.record_stream(torch.cuda.ExternalStream(queue) if queue else torch.cuda.default_stream(plan.memory.device))
     _check(lib().logra_adamw_step(
         plan.memory.data_ptr(), plan.memory.numel(), n, at, lr, beta1, beta2, eps, weight_decay, max_norm, scales, out, seed,

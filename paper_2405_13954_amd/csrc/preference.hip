@@ -10,7 +10,7 @@
 // small difference of large sums) and leaves two factors for every row, and k_pair_grad writes the gradient.  The second
 // pass takes the rows from the last to the first, so that those that the 256 MB cache still holds are read from there.  Small
 // calls have the second and third launch in one (k_pair_few).
-// 2,048 tokens of 128,000 bf16 logits, 0.3 of them masked: 68 + 6 + 126 us for 367, 0 and 891 MB (5.4 and 7.1 TB/s; a copy
+// 2,048 tokens of 128,000 bf16 logits, 0.3 of them masked: 68 + 6 + 128 us for 367, 0 and 891 MB (5.4 and 6.9 TB/s; a copy
 // inside the cache reaches 7.2).
 #include "internal.h"
 #include "vec16.h"

@@ -65,5 +65,3 @@ def test_a_plan_lists_where_its_tensors_are():
     at = x.data_ptr()
     assert P._edges([]) == P._edges([x[:0]]) == (end,)
     assert P._edges([x[8:16], None, x[0:8], x[12:20], x[13:14]]) == (at, at + 32, at + 32, at + 80, end)
-    for first, n, inside in ((-8, 8, False), (-8, 9, True), (0, 4, True), (252, 8, True), (256, 8, False), (-8, 400, True)):
-        assert P._inside(P._edges([x]), at + first, n) == inside
