@@ -727,7 +727,8 @@ int logra_preference_loss(const void *logits, int64_t ld, int dtype, int64_t row
  *                  value in magnitude goes there iff r > that half.  A v that is not
  *                  zero does not become zero: it takes the smallest code.  Magnitudes
  *                  from 2^128 on and NaN become NaN (m), or infinity and NaN (v).
- *                  param is computed from m and v before they are rounded
+ *                  param is computed from m and v before they are rounded, which are
+ *                  float64 here, every product and sum of the formula rounded by itself
  *   Elements need their own alignment only: tensors may be parts of flat buffers.
  *
  * logra_adamw_plan lays the list out in device memory, once for all steps; the

@@ -21,7 +21,9 @@
 // thousand times the others', and their squares need the wider exponent more than the third bit.  Both are rounded at
 // random, up with the probability of the part that is cut off: to nearest, a v whose step adds less than half of its last
 // bit (an eighth) would never move again.  A v that is not zero keeps at least the smallest code, so that no element divides
-// by eps alone.  One last bit of m or v can tip a code, so this path is float64 up to the code; it is still bound by memory.
+// by eps alone.  One last bit of m or v can tip a code, so this path is float64 up to the code, each product and sum rounded by
+// itself as the formula is written (with beta = 0.9 and few digits in m and the gradient, sums on the very boundary that the random
+// bits set are common: some in a million); it is still bound by memory.
 #include "counter_rng.h"
 #include "internal.h"
 #include "vec16.h"
@@ -249,6 +251,13 @@ __device__ __forceinline__ float moved(float p, float m, float v, const AdamwGro
     return fmaf(p, keep, -g.rate * m * __builtin_amdgcn_rcpf(fmaf(root, g.root, eps)));
 }
 
+// beta state + rest now.
+__device__ __forceinline__ double mixed(double beta, double state, double rest, double now) {
+#pragma clang fp contract(off)
+    const double a = beta * state, b = rest * now;
+    return a + b;
+}
+
 // The states' codes are made from the high and low words of m and v in float64.  kHuge: the high word of 2^128, from which on
 // (and for infinities and NaN) a magnitude is not finite in fp32.
 constexpr uint32_t kHuge = 0x47F00000u;
@@ -431,7 +440,7 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, StepArgs x) {
         if (JOIN) o = record();
         if (o.skip) return;
         keep = kept();
-        const double b1 = y.beta1 * sm, b2 = y.beta2 * sv, a1 = (1.0 - y.beta1) * o.clip, a2 = (1.0 - y.beta2) * (o.clip * o.clip);
+        const double a1 = 1.0 - y.beta1, a2 = 1.0 - y.beta2, dm = sm, dv = sv;
         double m[kPer], v[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
@@ -444,9 +453,9 @@ __global__ __launch_bounds__(kTh) void k_adamw_step(PlanArgs a, StepArgs x) {
                              : (e & 3) == 1 ? __builtin_amdgcn_cvt_f32_bf8(u, 1)
                              : (e & 3) == 2 ? __builtin_amdgcn_cvt_f32_bf8(u, 2)
                                             : __builtin_amdgcn_cvt_f32_bf8(u, 3);
-            const double ge = static_cast<double>(g[e]);
-            m[e] = fma(a1, ge, b1 * static_cast<double>(fm));
-            v[e] = fma(a2, ge * ge, b2 * static_cast<double>(fv));
+            const double cg = o.clip * static_cast<double>(g[e]);
+            m[e] = mixed(y.beta1, dm * static_cast<double>(fm), a1, cg);
+            v[e] = mixed(y.beta2, dv * static_cast<double>(fv), a2, cg * cg);
             p[e] = moved(p[e], static_cast<float>(m[e]), static_cast<float>(v[e]), o, keep, eps);
         }
         // The largest and smallest magnitudes by their high words alone, which is all but always enough.  (Elements past
