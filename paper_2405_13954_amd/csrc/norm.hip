@@ -221,6 +221,9 @@ __global__ __launch_bounds__(TPR <= 64 ? 256 : TPR) void k_norm_fwd(FwdArgs a) {
     }
 }
 
+// -avg(c xh) from avg(c (h - mean)).  A row beyond the range of its statistics (rstd 0) may have any sum, and has none here.
+__device__ __forceinline__ float mean_along(float avg, float rstd) { return rstd == 0.f ? 0.f : -avg * rstd; }
+
 // A team's share of one row.
 template <int NV>
 struct RowPart {
@@ -305,12 +308,12 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
 #pragma unroll
             for (int e = 0; e < V::kN; ++e) {
                 const float dy = V::get(cur.dy[k], e), c = dy * g[e];
-                const float xh = (CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e)) * cur.rstd;
+                const float d = CENTER ? V::get(cur.h[k], e) - cur.mean : V::get(cur.h[k], e), xh = d * cur.rstd;
                 if constexpr (CENTER) {
                     s1 += c;
                     db[k][e] += dy;
                 }
-                s2 = fmaf(c, xh, s2);
+                s2 = fmaf(c, d, s2);   // (not xh, which may be infinite behind the row's end, where d is -mean and c 0)
                 dg[k][e] = fmaf(dy, xh, dg[k][e]);
                 if constexpr (!BF16) cur.h[k][e] = __float_as_uint(xh);   // (fp32: xh in the place of h)
             }
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_norm_bwd(BwdArgs a) {
         // dx - base = rstd (c - avg(c) - xh avg(c xh)), as it stands: h - mean under one factor, rstd^3 avg(c (h - mean)), would take
         // a cube that leaves fp32 on both sides.  (A masked row has zeros in all, whose products with a gain that is not finite are
         // dropped.)
-        const float level = -(s1 * per), along = -(s2 * per);
+        const float level = -(s1 * per), along = mean_along(s2 * per, cur.rstd);
         if (a.dx && row < a.rows) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -485,12 +488,12 @@ __global__ __launch_bounds__(few_threads(TPR)) void k_norm_bwd_few(BwdArgs a, fl
         for (int e = 0; e < V::kN; ++e) {
             const float c = V::get(dy[k], e) * V::get(gain[k], e);
             if constexpr (CENTER) s1 += c;
-            s2 = fmaf(c, (V::get(h[k], e) - mean) * rstd, s2);
+            s2 = fmaf(c, V::get(h[k], e) - mean, s2);
         }
     }
     team_sums<TPR, CENTER>(s1, s2, red, static_cast<int>(threadIdx.x) / TPR);
     const float per = 1.f / static_cast<float>(a.cols);
-    const float level = -(s1 * per), along = -(s2 * per);   // as in k_norm_bwd
+    const float level = -(s1 * per), along = mean_along(s2 * per, rstd);   // as in k_norm_bwd
     if (!in) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {

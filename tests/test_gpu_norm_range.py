@@ -104,3 +104,21 @@ def test_backward_beyond_the_range(rows, cols):
     P.logra_layer_norm_forward(h, y, mean=mean, rstd=rstd)
     P.logra_layer_norm_backward(h, dy, rstd, mean=mean, dx=dx, base=base, dgain=dgain)
     assert not rstd.any() and torch.equal(dx, base) and not dgain.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(5, 75), (5, 1001), (5, 12289), (1030, 75), (1030, 1001), (1030, 4109), (1030, 12289)])
+def test_backward_of_rows_far_from_zero_at_odd_widths(rows, cols, dtype):
+    # rows of 2^123 and no variance: (h - mean) rstd is 0, while what lies behind a row's end, 0 - mean, times rstd is beyond fp32
+    import torch
+    import paper_2405_13954_amd as P
+    g = np.random.default_rng(cols)
+    h, _ = rows_of(g, rows, cols, 0.0, dtype)
+    h[::2] = 2.0 ** 123
+    dy, dy64 = rows_of(g, rows, cols, 1.0, dtype)
+    mean, rstd = h[:, 0].float().contiguous(), torch.full((rows,), 300.0, device="cuda")
+    dx, dgain, dbias = room(rows, cols, dtype)[0], f32(cols), f32(cols)
+    P.logra_layer_norm_backward(h, dy, rstd, mean=mean, dx=dx, dgain=dgain, dbias=dbias)
+    want = 300.0 * (dy64 - dy64.mean(1, keepdims=True))
+    within(host(dx), want, 300.0 * ROW * (np.abs(dy64) + np.abs(dy64).mean(1, keepdims=True)) + (HALF[dtype] + 2 * U) * np.abs(want), "dx")
+    assert not dgain.any() and bool(torch.isfinite(dbias).all())
