@@ -9,7 +9,7 @@
 // that squares and adds the gradients (k_adamw_norm: a wave for each chunk) and, for many chunks, a small one that turns the
 // sums into each group's factors (k_adamw_head).  Bound by memory: 28 bytes an element with fp32 states, 16 with 8-bit ones,
 // 2 more for the bf16 copy, and 4 to read the gradient twice where it is clipped.  10.5 million elements of 15 tensors with
-// the copy and clipping, fp32 states: 8 + 5 + 58 us, the last 5.4 TB/s; 42 million with 8-bit states: 30 + 5 + 129 us, 5.9.
+// the copy and clipping, fp32 states: 8 + 5 + 58 us, the last 5.4 TB/s; 42 million with 8-bit states: 30 + 5 + 130 us, 5.8.
 // Parameters and states pass by once a step, non-temporal both ways: a line that a load has brought into the cache and a store
 // has changed there is written back under the next launch, which was the next step's sum of squares (14 and 47 us then, with
 // 54 and 131 for the step).  The gradients are loaded as usual, and what the sum has read of them may still be there.

@@ -15,7 +15,7 @@
 // second launch adds them in order, so that reruns give the same bits.  Few rows: one launch (k_norm_bwd_few).
 //
 // 16,384 rows of 4096 bf16 columns without the mean: forward with residual and statistics 94 us for 537 MB (5.7 TB/s),
-// backward with base and a fifth of the rows masked 80 + 5 us for 483 MB (5.7).  768 columns with the mean: 16 and 20 + 4 us
+// backward with base and a fifth of the rows masked 79 + 5 us for 483 MB (5.7).  768 columns with the mean: 16 and 20 + 4 us
 // for 91 and 101 MB.
 #include "internal.h"
 #include "vec16.h"
